@@ -20,7 +20,8 @@
  *    before anything is launched.  Conditions only the device can see (a sequence that
  *    would overflow `capacity`) are latched into the bound `status` word: bit 0 = an
  *    append was dropped because the cache was full; bit 1 (value 2) = keep_idx too short for a sequence
- *    (dynts_select_evict left it alone); bit 2 (value 4) = the page pool of the paged layout ran dry.
+ *    (dynts_select_evict left it alone); bit 2 (value 4) = the page pool of the paged layout ran dry; bit 3
+ *    (value 8) = a chunk of question tokens behind thinking tokens (dynts_chunk_append).
  *  - Layout (C order, L = n_layers, Nb = batch, Hkv = n_kv_heads, cap = capacity, d = head_dim):
  *      K, V      bf16  [L][Nb][Hkv][cap][d]   rows in position order
  *      S         fp32  [L][Nb][Hkv][cap]      importance score; +inf on question slots
@@ -310,6 +311,95 @@ size_t dynts_predict_scratch_bytes(const dynts_predictor *w, int32_t batch);
 int dynts_predict_scores(const dynts_predictor *w, const uint16_t *h, int32_t batch, float *s_out,
                          int32_t n_rep, void *scratch, size_t scratch_bytes, void *start, void *stop,
                          void *stream);
+
+/* ---- chunks of new tokens ----------------------------------------------------------------------------------------
+ * Several new tokens of every sequence at once: a prompt, the next question, a tool's answer, drafted tokens to be
+ * checked, a known answer that is scored.  A chunk of m tokens is what m single steps are (Eq. attn-score, Eq. attn-o,
+ * Eq. importance-score): every token enters the cache, attends to what is there and to itself, and its attention
+ * weights are added to the scores of the thinking slots; but K and V are read once a chunk.  Dense and paged layouts.
+ *   n_tokens: tokens of the longest chunk, the row count of the arrays, 1 <= n_tokens <= 2^20.
+ *   n_new int32 [Nb] or NULL (= n_tokens each): tokens of each sequence (clamped to [0, n_tokens]); the rows behind
+ *     them are padding, not read as keys or written as outputs.  A sequence with none is left alone.
+ *   scratch: >= dynts_chunk_scratch_bytes(cfg, n_tokens) bytes of device memory, 256-byte aligned, contents irrelevant
+ *     before and after (what serves a chunk serves every smaller one; it may be shared by calls that are
+ *     stream-ordered with respect to each other).
+ * Outputs are bf16, as what a projection reads next; the weights are rounded to bf16 for their product with V, sums,
+ * products and statistics are fp32. */
+
+/* What is done to the logits of a chunk, in this order (s the scaled product of a query at position p and a key at
+ * position j; positions are those of the `pos` array, not slots: evictions leave gaps in them):
+ *   softcap > 0      s = softcap * tanh(s / softcap)
+ *   slope            s = s - slope[hq] * |p - j|
+ *   hidden keys      s = -inf unless max(first[b][i], p - window + 1) <= j <= last[b][i]
+ * first, last: positions token i of the chunk sees from and up to (`last` may lie behind the token's own position: a
+ * prefix whose tokens see each other; `first` at the start of a document keeps documents apart).  Positions are taken to
+ * be 0 or more and below 2^31 - 1.  A token that sees nothing gets zeros and lse = -inf.  Rows of V that are hidden from a token have
+ * to be finite; rows of K need not.  n_tokens = 1 is the form for single tokens. */
+typedef struct dynts_shaping {
+  float softcap;        /* 0: none */
+  int32_t window;       /* positions a token sees, its own the last of them; 0: all */
+  const float *slope;   /* fp32 [Hq] or NULL */
+  const int32_t *first; /* int32 [Nb][n_tokens] or NULL: 0 */
+  const int32_t *last;  /* int32 [Nb][n_tokens] or NULL: the token's own position */
+} dynts_shaping;
+
+/* Bytes of scratch for chunks of up to n_tokens tokens; 0 if cfg or n_tokens is invalid. */
+size_t dynts_chunk_scratch_bytes(const dynts_config *cfg, int32_t n_tokens);
+
+/* dynts_append for a chunk: k_new, v_new bf16 [Nb][n_tokens][Hkv][d] go to slots seq_len[b] and on; score 0, or s_new fp32
+ * [Nb][n_tokens][Hkv] when score_mode is DYNTS_SCORE_EXTERNAL (then required); pos = next_pos and on; both lengths advance.
+ * question != 0: the tokens are question slots (score +inf, never evicted; s_new is not read) and n_prompt[b] becomes the new length,
+ * so a sequence may get its question in several chunks, or another one before its first thinking token.
+ * A chunk that does not fit leaves its whole sequence alone, and latches in the status word: bit 0 = more than `capacity` slots, bit 2
+ * (value 4) = more pages than the pool has (the sequence keeps what it had, unlike after a dry dynts_append),
+ * bit 3 (value 8) = a question behind thinking tokens (seq_len[b] > n_prompt[b]). */
+int dynts_chunk_append(dynts_ctx *ctx, int32_t layer, const uint16_t *k_new, const uint16_t *v_new, const float *s_new,
+                       int32_t n_tokens, const int32_t *n_new, int32_t question, void *scratch, size_t scratch_bytes,
+                       void *stream);
+
+/* Attention of the LAST n_new[b] tokens in the cache (at most seq_len[b]): token i of them sees the slots up to its own, or what
+ * `shaping` (host struct of device pointers, or NULL) says.  q bf16 [Nb][n_tokens][Hq][d]; out bf16 [Nb][n_tokens][Hq][d];
+ * lse fp32 [Nb][n_tokens][Hq] or NULL: log of the softmax denominators.  Reads the cache only; what dynts_update_scores owes is
+ * not touched. */
+int dynts_chunk_attend(dynts_ctx *ctx, int32_t layer, const uint16_t *q, int32_t n_tokens, const int32_t *n_new,
+                       const dynts_shaping *shaping, uint16_t *out, float *lse, void *scratch, size_t scratch_bytes,
+                       void *stream);
+
+/* The attention weight that every cached slot receives from those tokens, summed over them and over the heads of its group:
+ *   dst[b][h][j] (+)= sum over tokens i and heads g of exp(logit - lse[b][i][hq]),  j < seq_len[b],
+ * with the lse of dynts_chunk_attend for the same arguments.  dst fp32 [Nb][Hkv][cap], or NULL: the layer's scores S, then slots
+ * below n_prompt[b] keep their +inf.  accumulate != 0 adds to dst, 0 overwrites it.  Commutes with what
+ * dynts_update_scores owes. */
+int dynts_chunk_scores(dynts_ctx *ctx, int32_t layer, const uint16_t *q, int32_t n_tokens, const int32_t *n_new,
+                       const dynts_shaping *shaping, const float *lse, float *dst, int32_t accumulate, void *stream);
+
+/* A chunk's whole step: dynts_chunk_append, dynts_chunk_attend and, unless the tokens are question slots or scores come from outside,
+ * dynts_chunk_scores into S.  A sequence whose chunk does not fit is left alone in all of them. */
+int dynts_chunk_step(dynts_ctx *ctx, int32_t layer, const uint16_t *q, const uint16_t *k_new, const uint16_t *v_new,
+                     const float *s_new, int32_t n_tokens, const int32_t *n_new, int32_t question,
+                     const dynts_shaping *shaping, uint16_t *out, float *lse, void *scratch, size_t scratch_bytes,
+                     void *stream);
+
+/* Rotary positions with several axes (time, height and width of an image's patches, say): pair p of every head, elements (a, b), is
+ * turned by theta = positions[axis[p]][t] * freq[p],
+ *   a' = a cos theta - b sin theta,  b' = b cos theta + a sin theta,
+ * elements behind the pairs are copied.  inverse != 0 turns by -theta: the gradient with respect to the input.  Whole turns are
+ * taken off in 64 bits, one rounding to bf16 at the end.
+ *   q bf16 [n_tokens][q_heads][head_dim], k bf16 [n_tokens][k_heads][head_dim] or NULL; q_out, k_out of the same shapes, the same
+ *   arrays or others (that do not overlap).  positions int32 [n_axes][n_tokens].
+ * head_dim a multiple of 8, n_pairs a multiple of 8, at most 128 and head_dim / 2.  An axis[p] past the last one counts as that one. */
+#define DYNTS_PAIR_HALVES 0   /* pair p: elements p and n_pairs + p */
+#define DYNTS_PAIR_ADJACENT 1 /* pair p: elements 2 p and 2 p + 1 */
+typedef struct dynts_rotary {
+  int32_t head_dim, n_pairs;
+  int32_t pairing; /* DYNTS_PAIR_* */
+  int32_t n_axes;
+  const float *freq;   /* device fp32 [n_pairs], radians a position */
+  const uint8_t *axis; /* device [n_pairs] or NULL: all of axis 0 */
+} dynts_rotary;
+int dynts_rotate(const dynts_rotary *r, const uint16_t *q, int32_t q_heads, const uint16_t *k, int32_t k_heads,
+                 const int32_t *positions, int32_t n_tokens, int32_t inverse, uint16_t *q_out, uint16_t *k_out,
+                 void *stream);
 
 /* Measurement aid, not part of the method: one launch of a plain read stream over `bytes` (a multiple
  * of 16, buf 16-byte aligned) of device memory, 16 bytes per lane per load, n_workgroups x 256 lanes,

@@ -26,6 +26,8 @@ EXPORTS = [
     "dynts_predict_scratch_bytes", "dynts_predict_scores", "dynts_predictor_pack", "dynts_bind_paged",
     "dynts_set_launch_shape", "dynts_ctx_workspace_bytes",
     "dynts_decode_step_static", "dynts_probe_exp_rate", "dynts_probe_issue_mix", "dynts_hint_trigger",
+    "dynts_chunk_scratch_bytes", "dynts_chunk_append", "dynts_chunk_attend", "dynts_chunk_scores", "dynts_chunk_step",
+    "dynts_rotate",
 ]
 
 
@@ -36,6 +38,19 @@ class dynts_predictor(C.Structure):
 
 
 DYNTS_ACT_NONE, DYNTS_ACT_RELU, DYNTS_ACT_SILU = 0, 1, 2
+
+
+class dynts_shaping(C.Structure):
+    _fields_ = [("softcap", C.c_float), ("window", C.c_int32), ("slope", C.c_void_p), ("first", C.c_void_p),
+                ("last", C.c_void_p)]
+
+
+class dynts_rotary(C.Structure):
+    _fields_ = [("head_dim", C.c_int32), ("n_pairs", C.c_int32), ("pairing", C.c_int32), ("n_axes", C.c_int32),
+                ("freq", C.c_void_p), ("axis", C.c_void_p)]
+
+
+DYNTS_PAIR_HALVES, DYNTS_PAIR_ADJACENT = 0, 1
 
 
 class dynts_config(C.Structure):
@@ -87,6 +102,14 @@ def _load():
     lib.dynts_probe_read_stream.argtypes = [vp, sz, i32, C.c_uint32, vp, vp, vp, vp]
     lib.dynts_probe_exp_rate.argtypes = [i32, i32, vp, vp, vp, vp]
     lib.dynts_probe_issue_mix.argtypes = [i32, i32, i32, vp, vp, vp, vp]
+    shaping = C.POINTER(dynts_shaping)
+    lib.dynts_chunk_scratch_bytes.restype = sz
+    lib.dynts_chunk_scratch_bytes.argtypes = [C.POINTER(dynts_config), i32]
+    lib.dynts_chunk_append.argtypes = [vp, i32, vp, vp, vp, i32, vp, i32, vp, sz, vp]
+    lib.dynts_chunk_attend.argtypes = [vp, i32, vp, i32, vp, shaping, vp, vp, vp, sz, vp]
+    lib.dynts_chunk_scores.argtypes = [vp, i32, vp, i32, vp, shaping, vp, vp, i32, vp]
+    lib.dynts_chunk_step.argtypes = [vp, i32, vp, vp, vp, vp, i32, vp, i32, shaping, vp, vp, vp, sz, vp]
+    lib.dynts_rotate.argtypes = [C.POINTER(dynts_rotary), vp, i32, vp, i32, vp, i32, i32, vp, vp, vp]
     for name in EXPORTS:
         getattr(lib, name)
     return lib
@@ -426,6 +449,81 @@ def dynts_probe_issue_mix(n_workgroups, iters, what, sink, start=None, stop=None
     """what: 1 = the MFMAs of a block-scoring chunk, 2 = its vector instructions, 3 = both; sink: device float tensor."""
     _check(lib.dynts_probe_issue_mix(n_workgroups, iters, what, sink.data_ptr(), start, stop, _stream(stream)),
            "dynts_probe_issue_mix")
+
+
+class Shaping:
+    """What is done to a chunk's logits (dynts_shaping): its tensors, kept alive here; marshalling only.
+    slope fp32 [Hq]; first, last int32 [Nb][T], the T of the chunk it is used with."""
+
+    def __init__(self, softcap=0.0, window=0, slope=None, first=None, last=None):
+        self.t = (slope, first, last)
+        self.s = dynts_shaping(softcap, window, _ptr(slope, torch.float32), _ptr(first, torch.int32),
+                               _ptr(last, torch.int32))
+
+
+def dynts_chunk_scratch_bytes(cfg, n_tokens):
+    return int(lib.dynts_chunk_scratch_bytes(C.byref(cfg), n_tokens))
+
+
+def _shaping(shaping):
+    return None if shaping is None else C.byref(shaping.s)
+
+
+def dynts_chunk_append(ctx, layer, k_new, v_new, scratch, n_new=None, s_new=None, question=False, stream=None):
+    """k_new, v_new bf16 [Nb][T][Hkv][d], s_new fp32 [Nb][T][Hkv], n_new int32 [Nb]; scratch: device tensor of at least
+    dynts_chunk_scratch_bytes bytes."""
+    _check(lib.dynts_chunk_append(ctx, layer, _ptr(k_new, torch.bfloat16), _ptr(v_new, torch.bfloat16),
+                                  _ptr(s_new, torch.float32), k_new.shape[1], _ptr(n_new, torch.int32),
+                                  1 if question else 0, scratch.data_ptr(), scratch.numel() * scratch.element_size(),
+                                  _stream(stream)), "dynts_chunk_append")
+
+
+def dynts_chunk_attend(ctx, layer, q, out, scratch, lse=None, n_new=None, shaping=None, stream=None):
+    """q, out bf16 [Nb][T][Hq][d], lse fp32 [Nb][T][Hq] or None, shaping: Shaping or None."""
+    _check(lib.dynts_chunk_attend(ctx, layer, _ptr(q, torch.bfloat16), q.shape[1], _ptr(n_new, torch.int32),
+                                  _shaping(shaping), _ptr(out, torch.bfloat16), _ptr(lse, torch.float32),
+                                  scratch.data_ptr(), scratch.numel() * scratch.element_size(), _stream(stream)),
+           "dynts_chunk_attend")
+
+
+def dynts_chunk_scores(ctx, layer, q, lse, dst=None, accumulate=True, n_new=None, shaping=None, stream=None):
+    """q and lse as in dynts_chunk_attend; dst fp32 [Nb][Hkv][cap] or None (= the layer's S)."""
+    _check(lib.dynts_chunk_scores(ctx, layer, _ptr(q, torch.bfloat16), q.shape[1], _ptr(n_new, torch.int32),
+                                  _shaping(shaping), _ptr(lse, torch.float32), _ptr(dst, torch.float32),
+                                  1 if accumulate else 0, _stream(stream)), "dynts_chunk_scores")
+
+
+def dynts_chunk_step(ctx, layer, q, k_new, v_new, out, scratch, lse=None, n_new=None, s_new=None, question=False,
+                     shaping=None, stream=None):
+    assert q.shape[:2] == k_new.shape[:2] == v_new.shape[:2], "q, k_new and v_new are of one chunk"
+    _check(lib.dynts_chunk_step(ctx, layer, _ptr(q, torch.bfloat16), _ptr(k_new, torch.bfloat16),
+                                _ptr(v_new, torch.bfloat16), _ptr(s_new, torch.float32), q.shape[1],
+                                _ptr(n_new, torch.int32), 1 if question else 0, _shaping(shaping),
+                                _ptr(out, torch.bfloat16), _ptr(lse, torch.float32), scratch.data_ptr(),
+                                scratch.numel() * scratch.element_size(), _stream(stream)), "dynts_chunk_step")
+
+
+class Rotary:
+    """The tables of rotary positions (dynts_rotary), kept alive here; marshalling only.  freq fp32 [n_pairs] on the device,
+    axis uint8 [n_pairs] or None."""
+
+    def __init__(self, head_dim, freq, axis=None, n_axes=1, pairing=DYNTS_PAIR_HALVES):
+        assert axis is None or axis.shape == freq.shape
+        self.t = (freq, axis)
+        self.r = dynts_rotary(head_dim, freq.numel(), pairing, n_axes, _ptr(freq, torch.float32), _ptr(axis, torch.uint8))
+
+
+def dynts_rotate(rotary, q, k, positions, q_out, k_out, inverse=False, stream=None):
+    """q bf16 [...][q_heads][d], k bf16 [...][k_heads][d] or None, positions int32 [n_axes][...]; q_out may be q, k_out k."""
+    d = rotary.r.head_dim
+    n = positions.numel() // rotary.r.n_axes
+    assert q.shape[-1] == d and q.numel() == n * q.shape[-2] * d and q_out.shape == q.shape, "one position a token"
+    if k is not None:
+        assert k.shape[-1] == d and k.numel() == n * k.shape[-2] * d and k_out.shape == k.shape, "one position a token"
+    _check(lib.dynts_rotate(C.byref(rotary.r), _ptr(q, torch.bfloat16), q.shape[-2], _ptr(k, torch.bfloat16),
+                            k.shape[-2] if k is not None else 0, _ptr(positions, torch.int32), n, 1 if inverse else 0,
+                            _ptr(q_out, torch.bfloat16), _ptr(k_out, torch.bfloat16) if k is not None else None,
+                            _stream(stream)), "dynts_rotate")
 
 
 class Cache:

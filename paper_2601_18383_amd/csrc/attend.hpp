@@ -115,6 +115,16 @@ constexpr int kStream = 1, kBurst = 2;  // forms of the kernel for large caches
 
 constexpr int kPageSlots = 64;  // slots per page: two tiles, so a tile never straddles pages
 
+__device__ __forceinline__ int safe_page(int pg, int n_pages) { return pg < 0 ? 0 : (pg >= n_pages ? n_pages - 1 : pg); }
+
+// element offset of slot j of a unit inside a pool
+template <int D>
+__device__ __forceinline__ size_t paged_row(const int32_t *tb, int j, int max_pages, int n_pages) {
+  int pi = j / kPageSlots;
+  pi = pi < max_pages ? pi : max_pages - 1;
+  return ((size_t)safe_page(tb[pi], n_pages) * kPageSlots + j % kPageSlots) * D;
+}
+
 
 __device__ __forceinline__ u32x4 load_u32x4(const uint16_t *p) { return *reinterpret_cast<const u32x4 *>(p); }
 __device__ __forceinline__ void store_u32x4(uint16_t *p, u32x4 v) { *reinterpret_cast<u32x4 *>(p) = v; }
@@ -997,7 +1007,7 @@ __global__ __launch_bounds__(W * 64, min_waves(D, W, APPEND, PAGED, LARGE, SPILL
 // statistics -- the same arithmetic as the deferred update inside attend_kernel, fed from 4 * G bytes per slot
 // instead of a K row.  grid (ceil(cap / (256 * kApplyPerThread)), Hkv * Nb), 256 threads.
 constexpr int kApplyPerThread = 4;
-__global__ __launch_bounds__(256) void apply_spill_kernel(float *S, const float *spill, const float *mlprev,
+static __global__ __launch_bounds__(256) void apply_spill_kernel(float *S, const float *spill, const float *mlprev,
                                                           const int32_t *nprev, const int32_t *n_prompt, int Hkv, int Hq,
                                                           int G, int cap, int cap_pad) {
   const int unit = blockIdx.y, b = unit / Hkv, h = unit - b * Hkv;

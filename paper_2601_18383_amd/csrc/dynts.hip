@@ -14,6 +14,7 @@
 #include <vector>
 
 #include "attend.hpp"
+#include "chunk.hpp"
 #include "compact.hpp"
 #include "paged.hpp"
 #include "predictor.hpp"
@@ -821,6 +822,23 @@ unsigned char *static_scratch(hipStream_t st) {
 }
 
 }  // namespace
+
+namespace dynts {
+
+int chunk_check_config(const dynts_config *cfg) { return check_config(cfg); }
+
+int chunk_cache(const dynts_ctx *ctx, int32_t layer, ChunkCache *out) {
+  const int rc = check_call(ctx, layer);
+  if (rc != DYNTS_OK) return rc;
+  const dynts_config &c = ctx->cfg;
+  const LayerView lv = layer_view(ctx, layer);
+  *out = ChunkCache{lv.K, lv.V, lv.S, lv.pos, lv.seq_len, lv.next_pos, ctx->n_prompt, ctx->status, lv.block_table, ctx->free_stack, ctx->free_top,
+                    ctx->max_pages, ctx->n_pages, c.batch, c.n_q_heads, c.n_kv_heads, ctx->plan.G, c.head_dim, c.capacity, c.score_mode,
+                    c.softmax_scale > 0.f ? c.softmax_scale : 1.0f / std::sqrt((float)c.head_dim)};
+  return DYNTS_OK;
+}
+
+}  // namespace dynts
 
 extern "C" {
 

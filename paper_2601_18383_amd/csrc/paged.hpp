@@ -20,16 +20,6 @@ struct PagedView {
   int max_pages, n_pages;
 };
 
-__device__ __forceinline__ int safe_page(int pg, int n_pages) { return pg < 0 ? 0 : (pg >= n_pages ? n_pages - 1 : pg); }
-
-// element offset of slot j of a unit inside a pool
-template <int D>
-__device__ __forceinline__ size_t paged_row(const int32_t *tb, int j, int max_pages, int n_pages) {
-  int pi = j / kPageSlots;
-  pi = pi < max_pages ? pi : max_pages - 1;
-  return ((size_t)safe_page(tb[pi], n_pages) * kPageSlots + j % kPageSlots) * D;
-}
-
 // One thread per unit takes the pages for slots [have[b], want[b]) of its unit (have = NULL: 0).
 // Returns with status bit 2 (value 4) latched when the pool runs dry; the unit then keeps what it got.
 // grid (ceil(Nb * Hkv / 64)), 64 threads.
