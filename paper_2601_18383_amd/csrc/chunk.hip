@@ -23,16 +23,44 @@ int launch_status() { return hipGetLastError() == hipSuccess ? DYNTS_OK : DYNTS_
 
 // scratch of a chunk's calls
 struct ChunkPlan {
-  size_t off_taken = 0, off_lse = 0, bytes = 0;
+  bool few;          // chunk_attend_few_kernel
+  int blocks, n_split, Rpad;
+  size_t off_lse = 0, off_ml = 0, off_o = 0, bytes = 0;
 };
 
-ChunkPlan chunk_plan(int Nb, int Hq, int n_tokens) {
+// At most this many workgroups take a share of a row block's keys.
+constexpr int kMostShares = 512;
+
+ChunkPlan chunk_plan(const dynts_config &c, int n_tokens) {
   ChunkPlan pl;
-  size_t off = align_up((size_t)Nb * sizeof(int32_t));
+  const long long R = (long long)n_tokens * (c.n_q_heads / c.n_kv_heads), units = (long long)c.batch * c.n_kv_heads;
+  pl.few = R <= 64;
+  const int rows = pl.few ? dynts::kFewRows : dynts::kChRows;
+  pl.blocks = (int)((R + rows - 1) / rows);
+  pl.Rpad = pl.blocks * rows;
+  pl.n_split = 1;
+  if (pl.few) {
+    const long long want = 256 / (units * pl.blocks), most = (c.capacity + 255) / 256;
+    pl.n_split = (int)(want < most ? want : most);
+    pl.n_split = pl.n_split < 1 ? 1 : pl.n_split;
+  }
+  size_t off = align_up((size_t)c.batch * sizeof(int32_t));
   pl.off_lse = off;
-  off += align_up((size_t)Nb * n_tokens * Hq * sizeof(float));
+  off += align_up((size_t)c.batch * n_tokens * c.n_q_heads * sizeof(float));
+  // (room for the shares of any shorter chunk, too)
+  const long long most = (long long)kMostShares * dynts::kFewRows;
+  pl.off_ml = off;
+  off += align_up((size_t)most * 2 * sizeof(float));
+  pl.off_o = off;
+  off += align_up((size_t)most * c.head_dim * sizeof(float));
   pl.bytes = off;
   return pl;
+}
+
+ChunkPlan chunk_plan(const ChunkCache &c, int n_tokens) {
+  dynts_config cfg{};
+  cfg.batch = c.Nb; cfg.n_q_heads = c.Hq; cfg.n_kv_heads = c.Hkv; cfg.head_dim = c.D; cfg.capacity = c.cap;
+  return chunk_plan(cfg, n_tokens);
 }
 
 int check_shaping(const dynts_shaping *s) {
@@ -96,21 +124,33 @@ unsigned chunk_grid(const ChunkCache &c, long long blocks) {
   const long long wgs = blocks * (((long long)c.Nb * c.Hkv + 7) / 8 * 8);
   return wgs >= (1LL << 32) / 256 ? 0u : (unsigned)wgs;
 }
-unsigned attend_grid(const ChunkCache &c, int n_tokens) { return chunk_grid(c, ((long long)n_tokens * c.G + dynts::kChRows - 1) / dynts::kChRows); }
+unsigned attend_grid(const ChunkCache &c, const ChunkPlan &pl) { return chunk_grid(c, (long long)pl.blocks * pl.n_split); }
 unsigned scores_grid(const ChunkCache &c) { return chunk_grid(c, (c.cap + dynts::kCsKeys - 1) / dynts::kCsKeys); }
 
+template <int D, bool SHAPED>
+void launch_attend_d(const dynts::ChunkAttendParams &p, const ChunkPlan &pl, unsigned grid, hipStream_t st) {
+  if (pl.few) hipLaunchKernelGGL((dynts::chunk_attend_few_kernel<D, SHAPED>), dim3(grid), dim3(dynts::kFewThreads), 0, st, p);
+  else hipLaunchKernelGGL((dynts::chunk_attend_kernel<D, SHAPED>), dim3(grid), dim3(dynts::kChThreads), 0, st, p);
+  if (p.n_split > 1) {
+    constexpr int rows = dynts::kMergeThreads / (D / 8);
+    hipLaunchKernelGGL(dynts::chunk_merge_kernel<D>, dim3((p.T * p.c.G + rows - 1) / rows, p.c.Nb * p.c.Hkv), dim3(dynts::kMergeThreads), 0, st, p);
+  }
+}
+
 int launch_attend(const ChunkCache &c, const uint16_t *q, int n_tokens, const int32_t *n_new, const dynts_shaping *shaping, uint16_t *out,
-                  float *lse, hipStream_t st) {
-  const dynts::ChunkAttendParams p{c, q, n_new, out, lse, chunk_shape(shaping, c.scale), n_tokens, c.scale * kLog2E};
-  const unsigned grid = attend_grid(c, n_tokens);
+                  float *lse, void *scratch, hipStream_t st) {
+  const ChunkPlan pl = chunk_plan(c, n_tokens);
+  char *const base = static_cast<char *>(scratch);
+  const dynts::ChunkAttendParams p{c, q, n_new, out, lse, chunk_shape(shaping, c.scale), n_tokens, c.scale * kLog2E, pl.n_split, pl.Rpad,
+                                   reinterpret_cast<float *>(base + pl.off_o), reinterpret_cast<float *>(base + pl.off_ml)};
+  const unsigned grid = attend_grid(c, pl);
   if (!grid) return DYNTS_EINVAL;
-  const dim3 block(dynts::kChThreads);
   if (c.D == 128) {
-    if (shaped(shaping)) hipLaunchKernelGGL((dynts::chunk_attend_kernel<128, true>), dim3(grid), block, 0, st, p);
-    else hipLaunchKernelGGL((dynts::chunk_attend_kernel<128, false>), dim3(grid), block, 0, st, p);
+    if (shaped(shaping)) launch_attend_d<128, true>(p, pl, grid, st);
+    else launch_attend_d<128, false>(p, pl, grid, st);
   } else {
-    if (shaped(shaping)) hipLaunchKernelGGL((dynts::chunk_attend_kernel<64, true>), dim3(grid), block, 0, st, p);
-    else hipLaunchKernelGGL((dynts::chunk_attend_kernel<64, false>), dim3(grid), block, 0, st, p);
+    if (shaped(shaping)) launch_attend_d<64, true>(p, pl, grid, st);
+    else launch_attend_d<64, false>(p, pl, grid, st);
   }
   return launch_status();
 }
@@ -140,7 +180,7 @@ extern "C" {
 
 size_t dynts_chunk_scratch_bytes(const dynts_config *cfg, int32_t n_tokens) {
   if (dynts::chunk_check_config(cfg) != DYNTS_OK || check_tokens(n_tokens) != DYNTS_OK) return 0;
-  return chunk_plan(cfg->batch, cfg->n_q_heads, n_tokens).bytes;
+  return chunk_plan(*cfg, n_tokens).bytes;
 }
 
 int dynts_chunk_append(dynts_ctx *ctx, int32_t layer, const uint16_t *k_new, const uint16_t *v_new, const float *s_new, int32_t n_tokens,
@@ -149,7 +189,7 @@ int dynts_chunk_append(dynts_ctx *ctx, int32_t layer, const uint16_t *k_new, con
   int rc = dynts::chunk_cache(ctx, layer, &c);
   if (rc == DYNTS_OK) rc = check_tokens(n_tokens);
   if (rc == DYNTS_OK) rc = check_append(c, k_new, v_new, s_new, question);
-  if (rc == DYNTS_OK) rc = check_scratch(scratch, scratch_bytes, chunk_plan(c.Nb, c.Hq, n_tokens).bytes);
+  if (rc == DYNTS_OK) rc = check_scratch(scratch, scratch_bytes, chunk_plan(c, n_tokens).bytes);
   if (rc != DYNTS_OK) return rc;
   return launch_append(c, k_new, v_new, s_new, n_tokens, n_new, question, static_cast<int32_t *>(scratch), static_cast<hipStream_t>(stream));
 }
@@ -163,9 +203,9 @@ int dynts_chunk_attend(dynts_ctx *ctx, int32_t layer, const uint16_t *q, int32_t
   if (rc != DYNTS_OK) return rc;
   if (!q || !out) return DYNTS_ENULL;
   if (misaligned(q, 16) || misaligned(out, 16)) return DYNTS_EINVAL;
-  rc = check_scratch(scratch, scratch_bytes, chunk_plan(c.Nb, c.Hq, n_tokens).bytes);
+  rc = check_scratch(scratch, scratch_bytes, chunk_plan(c, n_tokens).bytes);
   if (rc != DYNTS_OK) return rc;
-  return launch_attend(c, q, n_tokens, n_new, shaping, out, lse, static_cast<hipStream_t>(stream));
+  return launch_attend(c, q, n_tokens, n_new, shaping, out, lse, scratch, static_cast<hipStream_t>(stream));
 }
 
 int dynts_chunk_scores(dynts_ctx *ctx, int32_t layer, const uint16_t *q, int32_t n_tokens, const int32_t *n_new, const dynts_shaping *shaping,
@@ -191,16 +231,16 @@ int dynts_chunk_step(dynts_ctx *ctx, int32_t layer, const uint16_t *q, const uin
   if (rc != DYNTS_OK) return rc;
   if (!q || !out) return DYNTS_ENULL;
   if (misaligned(q, 16) || misaligned(out, 16)) return DYNTS_EINVAL;
-  const ChunkPlan pl = chunk_plan(c.Nb, c.Hq, n_tokens);
+  const ChunkPlan pl = chunk_plan(c, n_tokens);
   rc = check_scratch(scratch, scratch_bytes, pl.bytes);
   if (rc != DYNTS_OK) return rc;
   hipStream_t st = static_cast<hipStream_t>(stream);
   int32_t *taken = static_cast<int32_t *>(scratch);
   const bool scores = c.score_mode == DYNTS_SCORE_ACCUMULATE && !question;
-  if (!attend_grid(c, n_tokens) || (scores && !scores_grid(c))) return DYNTS_EINVAL;  // (before the append)
+  if (!attend_grid(c, pl) || (scores && !scores_grid(c))) return DYNTS_EINVAL;  // (before the append)
   if (scores && !lse) lse = reinterpret_cast<float *>(static_cast<char *>(scratch) + pl.off_lse);
   rc = launch_append(c, k_new, v_new, s_new, n_tokens, n_new, question, taken, st);
-  if (rc == DYNTS_OK) rc = launch_attend(c, q, n_tokens, taken, shaping, out, lse, st);
+  if (rc == DYNTS_OK) rc = launch_attend(c, q, n_tokens, taken, shaping, out, lse, scratch, st);
   if (rc == DYNTS_OK && scores) rc = launch_scores(c, q, n_tokens, taken, shaping, lse, nullptr, 1, st);
   return rc;
 }
