@@ -70,6 +70,8 @@ int check_shaping(const dynts_shaping *s) {
   return DYNTS_OK;
 }
 
+uint32_t group_magic(int G) { return G == 1 ? 0u : (uint32_t)(((1ull << 32) + G - 1) / G); }
+
 bool shaped(const dynts_shaping *s) { return s && (s->softcap > 0.f || s->window > 0 || s->slope || s->first || s->last); }
 
 dynts::ChunkShape chunk_shape(const dynts_shaping *s, float scale) {
@@ -141,7 +143,7 @@ int launch_attend(const ChunkCache &c, const uint16_t *q, int n_tokens, const in
                   float *lse, void *scratch, hipStream_t st) {
   const ChunkPlan pl = chunk_plan(c, n_tokens);
   char *const base = static_cast<char *>(scratch);
-  const dynts::ChunkAttendParams p{c, q, n_new, out, lse, chunk_shape(shaping, c.scale), n_tokens, c.scale * kLog2E, pl.n_split, pl.Rpad,
+  const dynts::ChunkAttendParams p{c, q, n_new, out, lse, chunk_shape(shaping, c.scale), n_tokens, c.scale * kLog2E, group_magic(c.G), pl.n_split, pl.Rpad,
                                    reinterpret_cast<float *>(base + pl.off_o), reinterpret_cast<float *>(base + pl.off_ml)};
   const unsigned grid = attend_grid(c, pl);
   if (!grid) return DYNTS_EINVAL;
@@ -158,7 +160,7 @@ int launch_attend(const ChunkCache &c, const uint16_t *q, int n_tokens, const in
 int launch_scores(const ChunkCache &c, const uint16_t *q, int n_tokens, const int32_t *n_new, const dynts_shaping *shaping, const float *lse,
                   float *dst, int accumulate, hipStream_t st) {
   const dynts::ChunkScoreParams p{c, q, n_new, lse, dst ? dst : c.S, chunk_shape(shaping, c.scale), n_tokens, dst ? 0 : 1, accumulate ? 1 : 0,
-                                  c.scale * kLog2E};
+                                  c.scale * kLog2E, group_magic(c.G)};
   const unsigned grid = scores_grid(c);
   if (!grid) return DYNTS_EINVAL;
   const dim3 block(dynts::kSbWaves * 64);

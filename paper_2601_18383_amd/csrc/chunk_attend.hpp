@@ -42,6 +42,7 @@ struct ChunkAttendParams {
   ChunkShape shape;
   int T;
   float scale_log2;
+  uint32_t g_magic;       // ceil(2^32 / G), 0 for G = 1
   // Keys of a row block cut into n_split shares, a workgroup each: unnormalised outputs and (shift, sum) of unit u, share s and row r in row
   // (u * n_split + s) * Rpad + r
   int n_split, Rpad;
@@ -50,7 +51,8 @@ struct ChunkAttendParams {
 
 constexpr int kChWaves = 4, kChThreads = kChWaves * 64;
 constexpr int kChRows = 32 * kChWaves;  // query rows a workgroup
-constexpr int kChTile = 64;             // slots staged at a time
+constexpr int kChTile = 32;             // slots staged at a time
+constexpr float kChLimit = 1e9f;        // a lane's weights of a tile that sum to this or more raise the shift
 constexpr int kNowhere = 0x7fffffff;    // a position that no key has
 
 // New tokens of sequence b that are queries, and its length.
@@ -62,10 +64,15 @@ __device__ __forceinline__ int chunk_tokens(const ChunkCache &c, const int32_t *
   return m < n ? m : n;
 }
 
-// Where slot t (a multiple of kChTile, and of a page's rows) of a unit begins, in elements.
+// Where slot t (the same in every lane) of a unit begins, in elements.  The page number comes by the scalar cache: by the vector caches it would be
+// waited for behind every load in flight.
 template <int D>
 __device__ __forceinline__ size_t chunk_tile(const ChunkCache &c, size_t unit, int t) {
-  return c.block_table ? paged_row<D>(c.block_table + unit * c.max_pages, t, c.max_pages, c.n_pages) : (unit * (size_t)c.cap + t) * D;
+  if (!c.block_table) return (unit * (size_t)c.cap + t) * D;
+  int pi = t / kPageSlots;
+  pi = pi < c.max_pages ? pi : c.max_pages - 1;
+  const int pg = *(const __attribute__((address_space(4))) int32_t *)(uintptr_t)(c.block_table + unit * c.max_pages + pi);
+  return ((size_t)safe_page(pg, c.n_pages) * kPageSlots + t % kPageSlots) * D;
 }
 
 // Byte of LDS at which 16-byte piece `piece` of row `row` of a tile lies.  The pieces of a row are permuted so that what is read together lies in
@@ -76,25 +83,46 @@ __device__ __forceinline__ int chunk_lds(int row, int piece) {
   return row * (2 * D) + 16 * (piece ^ f);
 }
 
-// The interval of positions that token i sees, as its lower end and the distance to its upper one; own: the token's position.
-__device__ __forceinline__ void chunk_interval(const ChunkShape &s, size_t at, int own, int &lo, uint32_t &span) {
+// LDS by its address, so that what differs between a lane's reads is a constant in the instruction.
+typedef __attribute__((address_space(3))) const u32x4 LdsPiece;
+typedef __attribute__((address_space(3))) i16x4 LdsQuad;
+__device__ __forceinline__ bf16x8 lds_piece(uint32_t at) { return __builtin_bit_cast(bf16x8, *(LdsPiece *)(uintptr_t)at); }
+__device__ __forceinline__ bf16x8 lds_columns(uint32_t at, uint32_t further) {
+  const i16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuad *)(uintptr_t)at), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuad *)(uintptr_t)(at + further));
+  return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// 16 (or 4) bytes a lane from a buffer straight to LDS, lane after lane from `to` on (`to` and `further` the same in every lane).  The compiler does not know of these loads:
+// who reads what they bring waits for them by s_waitcnt vmcnt, and whoever else reads it, behind a barrier.
+__device__ __forceinline__ void lds_bring16(RowBuffer buf, uint32_t offset, uint32_t further, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to), "v"(offset), "s"(buf), "s"(further) : "memory");
+}
+__device__ __forceinline__ void lds_bring4(RowBuffer buf, uint32_t offset, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(buf) : "memory");
+}
+
+// The interval of positions that a token at position `own` sees, as its lower end and the distance to its upper one; first, last: its own, where given.
+__device__ __forceinline__ void chunk_bounds(const ChunkShape &s, int first, int last, int own, int &lo, uint32_t &span) {
   int low = 0, high = own;
   if (s.window > 0) low = own - s.window + 1;
-  if (s.first) {
-    const int f = s.first[at];
-    low = f > low ? f : low;
-  }
-  if (s.last) high = s.last[at];
+  if (s.first) low = first > low ? first : low;
+  if (s.last) high = last;
   low = low < 0 ? 0 : low;
   high = high >= kNowhere ? kNowhere - 1 : high;
   if (high < low) low = high = kNowhere;
   lo = low;
   span = (uint32_t)high - (uint32_t)low;
 }
+__device__ __forceinline__ void chunk_interval(const ChunkShape &s, size_t at, int own, int &lo, uint32_t &span) {
+  const int first = s.first ? s.first[at] : 0, last = s.last ? s.last[at] : 0;
+  chunk_bounds(s, first, last, own, lo, span);
+}
 
-// Slots of [0, n) whose position is below `target` (positions ascend along the cache): 64 of them looked at a time, by one wave.
-__device__ __forceinline__ int slots_below(const int32_t *pos, int n, int target, int lane) {
-  int lo = 0, hi = n;  // the answer lies in [lo, hi]
+// The token a row belongs to (rows below 2^28).
+__device__ __forceinline__ int chunk_token(int r, uint32_t magic) { return magic ? (int)__umulhi((uint32_t)r, magic) : r; }
+
+// The first slot of [lo, hi) whose position is not below `target`, or hi (positions ascend along the cache): 64 of them looked at a time, by one wave.
+__device__ __forceinline__ int slot_from(const int32_t *pos, int lo, int hi, int target, int lane) {
   while (lo < hi) {
     const int step = (hi - lo + 63) / 64, at = lo + lane * step;
     const int below = __popcll(__ballot(at < hi && pos[at < hi ? at : lo] < target));
@@ -104,6 +132,18 @@ __device__ __forceinline__ int slots_below(const int32_t *pos, int n, int target
     hi = to < hi ? to : hi;
   }
   return lo;
+}
+
+// The slots that rows of tokens [i0, i1] see, as [lo, hi), given the lowest and the highest position that one of them sees (kNowhere and -1: none).
+__device__ __forceinline__ void chunk_range(const ChunkShape &s, const int32_t *pos, int n, int base, int i0, int i1, int first, int last, int lane,
+                                            int &lo, int &hi) {
+  lo = 0;
+  if (s.first || s.window > 0) {
+    // (two slots lie no further apart than their positions: without gaps the first look finds it)
+    const int slot = base + i0, d = pos[slot] - first;
+    lo = d >= 0 ? slot_from(pos, d < slot ? slot - d : 0, slot, first, lane) : slot_from(pos, slot, n, first, lane);
+  }
+  hi = s.last ? slot_from(pos, 0, n, last + 1, lane) : base + i1 + 1;
 }
 
 // cap * tanh(dot * scale / softcap) in log2 units: (1 - u) / (1 + u) with u = 2^(-2 |z| log2 e) is off by 2^-25 of the cap where its argument is small.
@@ -121,18 +161,33 @@ __device__ __forceinline__ void chunk_write(const ChunkAttendParams &p, size_t r
   if (p.lse && d0 == 0) p.lse[row] = sum > 0.f ? (top + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f : -INFINITY;
 }
 
+// ---- many rows: 32 of them a wave, four waves, which share the keys through LDS ----------------------------------------
+template <int D>
+struct ChunkLds {
+  static constexpr int kTileBytes = kChTile * 2 * D;
+  static constexpr int kPlace = 2 * kTileBytes + kChTile * 4;  // K, V and positions of a tile
+  static constexpr int kPlaces = 3;
+};
+// Byte of LDS at which piece `piece` of V's row `row` lies (its operands are read four rows by four pieces; K's as chunk_lds has it).
+template <int D>
+__device__ __forceinline__ int chunk_lds_v(int row, int piece) {
+  return row * (2 * D) + 16 * (piece ^ (D == 128 ? (row & 3) << 2 : ((row >> 1) & 1) << 2));
+}
+
 template <int D, bool SHAPED>
-__global__ __launch_bounds__(kChThreads) void chunk_attend_kernel(const ChunkAttendParams p) {
+__global__ __launch_bounds__(kChThreads, D == 128 ? 3 : 4) void chunk_attend_kernel(const ChunkAttendParams p) {
+  using Lds = ChunkLds<D>;
   const ChunkCache &c = p.c;
-  constexpr int kTileBytes = kChTile * 2 * D;
-  __shared__ __attribute__((aligned(16))) char sm_k[kTileBytes], sm_v[kTileBytes];
-  __shared__ __attribute__((aligned(16))) int sm_pos[kChTile];
-  __shared__ int sm_range[2];
+  // Three tiles' places: one is worked on, one is on its way, one is being asked for.
+  __shared__ __attribute__((aligned(1024))) char sm[Lds::kPlaces * Lds::kPlace];
+  __shared__ int sm_range[2 * kChWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 31, hf = lane >> 5, r16 = lane & 15;
   int unit, blk;
   const int n_blk = (p.T * c.G + kChRows - 1) / kChRows;
-  if (!sb_map(n_blk, c.Nb * c.Hkv, unit, blk)) return;
+  if (!sb_map(n_blk * p.n_split, c.Nb * c.Hkv, unit, blk)) return;
+  const int split = blk / n_blk;
+  blk -= split * n_blk;
   const int b = unit / c.Hkv, h = unit - b * c.Hkv;
   int n;
   const int m = chunk_tokens(c, p.n_new, p.T, b, n);
@@ -143,131 +198,260 @@ __global__ __launch_bounds__(kChThreads) void chunk_attend_kernel(const ChunkAtt
 
   const int row0 = blk * kChRows + wave * 32;
   const int r = row0 + col < R ? row0 + col : R - 1;
-  const int i = r / c.G, g = r - i * c.G;
-  const size_t qrow = ((size_t)b * p.T + i) * c.Hq + (size_t)h * c.G + g;
+  const int tok = chunk_token(r, p.g_magic), g = r - tok * c.G;
   bf16x8 qf[D / 16];
-  load_row_frags<D>(qf, reinterpret_cast<const char *>(p.q + qrow * D), hf);
+  load_row_frags<D>(qf, reinterpret_cast<const char *>(p.q + (((size_t)b * p.T + tok) * c.Hq + (size_t)h * c.G + g) * D), hf);
+  float slope = 0.f;
+  if (SHAPED && p.shape.slope) slope = p.shape.slope[h * c.G + g] * 1.4426950408889634f;
 
-  // what the row sees; in the plain form slots [0, lim], else positions [lo, lo + span]
+  // what the rows see: plain, slots [0, lim]; shaped, positions [lo, lo + span].  all_lo, all_hi: what all of the wave's rows see
   const int32_t *pos = c.pos + (size_t)unit * c.cap;
-  const int lim = base + i;
-  int lo = 0, ref = 0;
+  int lim, ref = 0, t_lo = 0, t_hi, all_lo = 0, all_hi;
   uint32_t span = 0;
-  float at = 0.f, slope = 0.f;
-  int t_lo = 0, t_hi;
+  float at = 0.f;
+  const int r1 = blk * kChRows + kChRows - 1;
+  const int i0 = chunk_token(blk * kChRows, p.g_magic), i1 = chunk_token(r1 < R ? r1 : R - 1, p.g_magic);
   if (SHAPED) {
-    const int own = pos[base + i];
-    chunk_interval(p.shape, (size_t)b * p.T + i, own, lo, span);
     ref = __builtin_amdgcn_readfirstlane(pos[base]);
+    const int own = pos[base + tok];
+    chunk_interval(p.shape, (size_t)b * p.T + tok, own, lim, span);
     at = (float)(own - ref);
-    if (p.shape.slope) slope = p.shape.slope[h * c.G + g] * 1.4426950408889634f;
-    // the slots that some row of the workgroup sees
-    if (tid == 0) {
-      sm_range[0] = kNowhere;
-      sm_range[1] = -1;
+    int first = lim, last = lim == kNowhere ? -1 : (int)(lim + span);
+    all_lo = first;
+    all_hi = last;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+      const int f = __shfl_xor(first, d), l = __shfl_xor(last, d), al = __shfl_xor(all_lo, d), ah = __shfl_xor(all_hi, d);
+      first = f < first ? f : first;
+      last = l > last ? l : last;
+      all_lo = al > all_lo ? al : all_lo;
+      all_hi = ah < all_hi ? ah : all_hi;
+    }
+    if (lane == 0) {
+      sm_range[wave] = first;
+      sm_range[kChWaves + wave] = last;
     }
     __syncthreads();
-    if (lo != kNowhere) {
-      atomicMin(&sm_range[0], lo);
-      atomicMax(&sm_range[1], (int)(lo + span));
+#pragma unroll
+    for (int w = 0; w < kChWaves; ++w) {
+      first = sm_range[w] < first ? sm_range[w] : first;
+      last = sm_range[kChWaves + w] > last ? sm_range[kChWaves + w] : last;
     }
-    __syncthreads();
-    t_lo = slots_below(pos, n, sm_range[0], lane) / kChTile * kChTile;
-    t_hi = slots_below(pos, n, sm_range[1] + 1, lane);
+    chunk_range(p.shape, pos, n, base, i0, i1, __builtin_amdgcn_readfirstlane(first), __builtin_amdgcn_readfirstlane(last), lane, t_lo, t_hi);
+    t_lo = t_lo / kChTile * kChTile;
+    all_lo = __builtin_amdgcn_readfirstlane(all_lo);
   } else {
-    int last = blk * kChRows + kChRows - 1;
-    last = last < R ? last : R - 1;
-    t_hi = base + last / c.G + 1;
+    lim = base + tok;
+    t_hi = base + i1 + 1;
+    all_hi = base + chunk_token(row0 < R ? row0 : R - 1, p.g_magic);
   }
-  t_lo = __builtin_amdgcn_readfirstlane(t_lo);
-  t_hi = __builtin_amdgcn_readfirstlane(t_hi);
+  all_hi = __builtin_amdgcn_readfirstlane(all_hi);
+  const int tiles = t_hi > t_lo ? (t_hi - t_lo + kChTile - 1) / kChTile : 0;
+  const int from = (int)((long long)tiles * split / p.n_split), to = (int)((long long)tiles * (split + 1) / p.n_split);
+  const int t0 = __builtin_amdgcn_readfirstlane(t_lo + from * kChTile), t1 = __builtin_amdgcn_readfirstlane(t_lo + to * kChTile);
 
   f32x16 acc[D / 32];
+  float nm = 1e30f, l = 0.f;  // the exponents' addend (minus the shift, a whole number of log2 units); the lane's share of the sum of weights
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc[dt][e] = 0.f;
-  float m_run = -INFINITY, l_run = 0.f;
 
-  constexpr int PPR = D / 8, PIECES = kChTile * PPR / kChThreads;
-  for (int t = t_lo; t < t_hi; t += kChTile) {
-    const size_t from = chunk_tile<D>(c, unit, t);
+  // Staging, past the registers: a wave brings kInstr parts of 1 KB of either operand.  A lane's piece of a part is the one that belongs at byte
+  // 16 * lane of it; its place in the row is the same for all of a lane's parts.  Rows past the cache's end repeat the last one.
+  constexpr int PPR = D / 8, kInstr = Lds::kTileBytes / 1024 / kChWaves, kRowsPart = 1024 / (2 * D);
+  const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)sm;
+  const int my_row = wave * kRowsPart + lane / PPR;
+  const uint32_t k_off = chunk_lds<D>(my_row, lane % PPR), v_off = chunk_lds_v<D>(my_row, lane % PPR);
+  auto bring = [&](int t, uint32_t place) {
+    if (t >= t1) return;
     const int rows = n - t < kChTile ? n - t : kChTile;
-    const RowBuffer kb = row_buffer<D>(c.K + from, rows), vb = row_buffer<D>(c.V + from, rows);
-    __syncthreads();
+    const size_t at = chunk_tile<D>(c, unit, t);
+    const RowBuffer kb = row_buffer<D>(c.K + at, rows), vb = row_buffer<D>(c.V + at, rows);
 #pragma unroll
-    for (int k = 0; k < PIECES; ++k) {
-      const int at_piece = tid + kChThreads * k, dst = chunk_lds<D>(at_piece / PPR, at_piece % PPR);
-      *reinterpret_cast<u32x4 *>(sm_k + dst) = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(kb, 16 * at_piece, 0, 0));
-      *reinterpret_cast<u32x4 *>(sm_v + dst) = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(vb, 16 * at_piece, 0, 0));
+    for (int i = 0; i < kInstr; ++i) {
+      constexpr int kNext = kRowsPart * kChWaves;  // rows from a lane's part to its next one
+      const uint32_t to = place + 1024 * (wave + i * kChWaves);
+      if (rows == kChTile) {
+        lds_bring16(kb, k_off, i * kNext * 2 * D, to);
+        lds_bring16(vb, v_off, i * kNext * 2 * D, to + Lds::kTileBytes);
+      } else {
+        const int over = my_row + i * kNext - (rows - 1), back = (over > 0 ? over : 0) * (2 * D);
+        lds_bring16(kb, k_off + i * kNext * 2 * D - back, 0, to);
+        lds_bring16(vb, v_off + i * kNext * 2 * D - back, 0, to + Lds::kTileBytes);
+      }
     }
-    if (SHAPED && tid < kChTile) sm_pos[tid] = tid < rows ? pos[t + tid] : -1;
-    __syncthreads();
+    if (SHAPED && wave == 0 && lane < kChTile) {
+      const RowBuffer pb = row_buffer<2>(reinterpret_cast<const uint16_t *>(pos + t), rows);
+      lds_bring4(pb, 4 * (lane < rows ? lane : rows - 1), place + 2 * Lds::kTileBytes);
+    }
+  };
+
+  // this lane's operands in a place: K's row `col`, piece 2 ks + hf; V's rows r16 / 4 + 4 hf + .., columns 4 (r16 % 4) .. +3 of 16 (of which it then gets
+  // column r16, of four rows)
+  uint32_t k_at[D / 16], v_at[D / 32];
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      f32x16 s;
+  for (int ks = 0; ks < D / 16; ++ks) k_at[ks] = lds + chunk_lds<D>(col, 2 * ks + hf);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) s[e] = 0.f;
+  for (int dt = 0; dt < D / 32; ++dt)
+    v_at[dt] = lds + Lds::kTileBytes + chunk_lds_v<D>(4 * hf + (r16 >> 2), 4 * dt + 2 * ((lane >> 4) & 1) + ((r16 >> 1) & 1)) + 8 * (r16 & 1);
+
+  // raw products of the tile in a place
+  auto products = [&](f32x16 &s, uint32_t place) {
 #pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks) {
-        const bf16x8 kf = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(sm_k + chunk_lds<D>(32 * half + col, 2 * ks + hf)));
-        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], s, 0, 0, 0);
+    for (int e = 0; e < 16; ++e) s[e] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) {
+      const bf16x8 kf = lds_piece(k_at[ks] + place);
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], s, 0, 0, 0);
+    }
+  };
+  // Logits of tile t from its products: shaped, and hidden keys' at -inf.  `scale` is still to be multiplied with them, 1 if they are log2 units already.
+  const bool capped = SHAPED && p.shape.cap > 0.f, biased = SHAPED && p.shape.slope != nullptr;
+  const float scale = capped || biased ? 1.f : p.scale_log2;
+  auto shape = [&](f32x16 &s, int t, uint32_t place) {
+    if (SHAPED) {
+      const int *tp = reinterpret_cast<const int *>(sm + place + 2 * Lds::kTileBytes);
+      const int first = __builtin_amdgcn_readfirstlane(tp[0]), last = __builtin_amdgcn_readfirstlane(tp[kChTile - 1]);
+      const bool all = first >= all_lo && last <= all_hi && t + kChTile <= n;
+      if (capped) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[e] = soft_cap(s[e], p.shape);
+      } else if (biased) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[e] *= p.scale_log2;
       }
-      float mx = -INFINITY;
+      if (biased) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int key = 32 * half + 8 * (e >> 2) + 4 * hf + (e & 3);
-        if (SHAPED) {
-          float x = p.shape.cap > 0.f ? soft_cap(s[e], p.shape) : s[e] * p.scale_log2;
-          const int kp = sm_pos[key];
-          x -= slope * fabsf(at - (float)(kp - ref));
-          s[e] = (uint32_t)(kp - lo) <= span ? x : -INFINITY;
-        } else {
-          s[e] = t + key <= lim ? s[e] * p.scale_log2 : -INFINITY;
+        for (int e = 0; e < 16; ++e) {
+          const float f = (float)(tp[8 * (e >> 2) + 4 * hf + (e & 3)] - ref);
+          s[e] = fmaf(-slope, fabsf(at - f), s[e]);
         }
-        mx = fmaxf(mx, s[e]);
       }
-      mx = fmaxf(mx, __shfl_xor(mx, 32));
-      const float m_next = fmaxf(m_run, mx), m_use = m_next == -INFINITY ? 0.f : m_next;
-      const float corr = fast_exp2(m_run - m_use);
-      m_run = m_next;
-      float sum = 0.f;
-      bf16x8 pf[2];  // (the weights are rounded to bf16 for the product with V: half a step of 2^-8 relative each, as the output is)
+      if (!all) {
+        asm volatile("; some keys are hidden");  // (a branch: the compiler would compare every key of every tile)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const float w = fast_exp2(s[e] - m_use);
-        sum += w;
-        pf[e >> 3][e & 7] = (__bf16)w;
+        for (int e = 0; e < 16; ++e) {
+          const int key = 8 * (e >> 2) + 4 * hf + (e & 3), kp = t + key < n ? tp[key] : -1;
+          if ((uint32_t)(kp - lim) > span) s[e] = -INFINITY;
+        }
       }
-      l_run = l_run * corr + sum;
+    } else if (t + kChTile - 1 > all_hi) {
+      asm volatile("; some keys are hidden");
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (t + 8 * (e >> 2) + 4 * hf + (e & 3) > lim) s[e] = -INFINITY;
+    }
+  };
+  // weights of a tile from its logits, with the shift at hand, and their sum
+  auto fold = [&](const f32x16 &s, bf16x8 (&pf)[2]) {
+    float q[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      float w[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        w[e] = fast_exp2(fmaf(s[4 * k + e], scale, nm));
+        pf[k >> 1][4 * (k & 1) + e] = (__bf16)w[e];  // (half a step of 2^-8, as the output's rounding)
+      }
+      q[k] = (w[0] + w[1]) + (w[2] + w[3]);
+    }
+    return (q[0] + q[1]) + (q[2] + q[3]);
+  };
+  // the shift raised to the tile's largest logit, where that lies above it
+  auto raise = [&](const f32x16 &s, float &sum, bf16x8 (&pf)[2]) {
+    float mx = s[0];
+#pragma unroll
+    for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[e]);
+    mx = fmaxf(mx, __shfl_xor(mx, 32));
+    const float next = fminf(floorf(-mx * scale), nm), f = fast_exp2(next - nm);
+    l *= f;
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt) acc[dt] *= f;
+    nm = next;
+    sum = fold(s, pf);
+  };
+  auto add_values = [&](const bf16x8 (&pf)[2], uint32_t place) {
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
       for (int dt = 0; dt < D / 32; ++dt) {
-        acc[dt] *= corr;
-#pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-          // lane (r16 of its 16, ...) points at row r16 / 4 and columns 4 (r16 % 4) .. +3, and gets column r16 of the four rows
-          const int vrow = 32 * half + 16 * ks + 4 * hf + (r16 >> 2), piece = 4 * dt + 2 * ((lane >> 4) & 1) + ((r16 >> 1) & 1);
-          const i16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4 *)(sm_v + chunk_lds<D>(vrow, piece) + 8 * (r16 & 1)));
-          const i16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4 *)(sm_v + chunk_lds<D>(vrow + 8, piece) + 8 * (r16 & 1)));
-          acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7)), pf[ks],
-                                                            acc[dt], 0, 0, 0);
-        }
+        const bf16x8 vt = lds_columns(v_at[dt] + place + 16 * ks * (2 * D), 8 * (2 * D));
+        acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vt, pf[ks], acc[dt], 0, 0, 0);
       }
-    }
+  };
+
+  // One tile out of its place, while the tile after the next goes to the place that the last one has left.  Before the barrier a wave waits for
+  // its own parts of the tile alone, those of the next one stay on their way (a __syncthreads would wait for all).
+  constexpr int kWait = 0x0070;  // s_waitcnt of lgkmcnt(0) and vmcnt(0)
+  auto tile = [&](int t, auto PLACE, auto FREE) {
+    constexpr uint32_t place = decltype(PLACE)::value * Lds::kPlace, free = decltype(FREE)::value * Lds::kPlace;
+    if (t + kChTile >= t1) __builtin_amdgcn_s_waitcnt(kWait);
+    else if (SHAPED && wave == 0) __builtin_amdgcn_s_waitcnt(kWait + 2 * kInstr + 1);
+    else __builtin_amdgcn_s_waitcnt(kWait + 2 * kInstr);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    bring(t + 2 * kChTile, lds + free);
+    f32x16 s;
+    products(s, place);
+    shape(s, t, place);
+    bf16x8 pf[2];
+    float sum = fold(s, pf);
+    if (__any(!(sum < kChLimit))) raise(s, sum, pf);
+    l += sum;
+    add_values(pf, place);
+  };
+  bring(t0, lds);
+  bring(t0 + kChTile, lds + Lds::kPlace);
+  // (the queries are waited for here: in the loop, every third tile would wait for all loads)
+#pragma unroll
+  for (int ks = 0; ks < D / 16; ++ks) asm volatile("" : "+v"(qf[ks]));
+  constexpr std::integral_constant<int, 0> kA{};
+  constexpr std::integral_constant<int, 1> kB{};
+  constexpr std::integral_constant<int, 2> kC{};
+  for (int t = t0; t < t1; t += 3 * kChTile) {
+    tile(t, kA, kC);
+    if (t + kChTile < t1) tile(t + kChTile, kB, kA);
+    if (t + 2 * kChTile < t1) tile(t + 2 * kChTile, kC, kB);
   }
 
-  const float l = l_run + __shfl_xor(l_run, 32);
-  if (row0 + col >= R) return;
-  const float inv = l > 0.f ? 1.f / l : 0.f;  // (a row that sees nothing: zeros, and -inf)
-  uint16_t *out = p.out + qrow * D;
+  // sums of the two halves' keys; outputs row by row through LDS
+  __syncthreads();
+  const float sum = l + __shfl_xor(l, 32);
+  if (p.n_split > 1) {
+    if (row0 + col >= R) return;
+    const size_t prow = ((size_t)unit * p.n_split + split) * p.Rpad + row0 + col;
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4)
+        *reinterpret_cast<f32x4 *>(p.part_o + prow * D + 32 * dt + 2 * e + 4 * hf) =
+            f32x4{acc[dt][e], acc[dt][e + 1], acc[dt][e + 2], acc[dt][e + 3]};
+    if (hf == 0) *reinterpret_cast<float2 *>(p.part_ml + 2 * prow) = float2{-nm, sum};
+    return;
+  }
+  const float inv = sum > 0.f ? 1.f / sum : 0.f;  // (a row that sees nothing: zeros, and -inf)
+  char *const turn = sm + wave * (32 * 2 * D);
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
-    for (int e = 0; e < 16; e += 4) {
-      const uint2 w = {bf16_pack(acc[dt][e] * inv, acc[dt][e + 1] * inv), bf16_pack(acc[dt][e + 2] * inv, acc[dt][e + 3] * inv)};
-      *reinterpret_cast<uint2 *>(out + 32 * dt + 2 * e + 4 * hf) = w;
+    for (int e = 0; e < 16; e += 4)
+      *reinterpret_cast<uint2 *>(turn + chunk_lds<D>(col, 4 * dt + (e >> 2)) + 8 * hf) =
+          uint2{bf16_pack(acc[dt][e] * inv, acc[dt][e + 1] * inv), bf16_pack(acc[dt][e + 2] * inv, acc[dt][e + 3] * inv)};
+  const float lse = sum > 0.f ? (__builtin_amdgcn_logf(sum) - nm) * 0.6931471805599453f : -INFINITY;
+  wave_lds_fence();
+#pragma unroll
+  for (int k = 0; k < 32 * PPR / 64; ++k) {
+    const int at_piece = lane + 64 * k, row = at_piece / PPR, piece = at_piece % PPR, rr = row0 + row;
+    const float row_lse = __shfl(lse, row);
+    if (rr < R) {
+      const int ri = chunk_token(rr, p.g_magic);
+      const size_t orow = ((size_t)b * p.T + ri) * c.Hq + (size_t)h * c.G + (rr - ri * c.G);
+      store_u32x4(p.out + orow * D + 8 * piece, *reinterpret_cast<const u32x4 *>(turn + chunk_lds<D>(row, piece)));
+      if (p.lse && piece == 0) p.lse[orow] = row_lse;
     }
-  if (p.lse && hf == 0) p.lse[qrow] = l > 0.f ? (m_run + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : -INFINITY;
+  }
 }
 
 // ---- few rows: 32 of them a workgroup, its eight waves share out the keys --------------------------------------------------
@@ -303,7 +487,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void chunk_attend_few_kernel(const 
   const int base = n - m;
 
   const int r = row0 + col < R ? row0 + col : R - 1;
-  const int i = r / c.G, g = r - i * c.G;
+  const int i = chunk_token(r, p.g_magic), g = r - i * c.G;
   const size_t qrow = ((size_t)b * p.T + i) * c.Hq + (size_t)h * c.G + g;
   bf16x8 qf[D / 16];
   load_row_frags<D>(qf, reinterpret_cast<const char *>(p.q + qrow * D), hf);
@@ -314,6 +498,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void chunk_attend_few_kernel(const 
   uint32_t span = 0;
   float at = 0.f, slope = 0.f;
   int t_lo = 0, t_hi;
+  const int i0 = chunk_token(row0, p.g_magic), i1 = chunk_token(row0 + kFewRows - 1 < R ? row0 + kFewRows - 1 : R - 1, p.g_magic);
   if (SHAPED) {
     const int own = pos[base + i];
     chunk_interval(p.shape, (size_t)b * p.T + i, own, lo, span);
@@ -328,11 +513,10 @@ __global__ __launch_bounds__(kFewThreads, 2) void chunk_attend_few_kernel(const 
       first = f < first ? f : first;
       last = l > last ? l : last;
     }
-    t_lo = slots_below(pos, n, first, lane) / kFewTile * kFewTile;
-    t_hi = slots_below(pos, n, last + 1, lane);
+    chunk_range(p.shape, pos, n, base, i0, i1, __builtin_amdgcn_readfirstlane(first), __builtin_amdgcn_readfirstlane(last), lane, t_lo, t_hi);
+    t_lo = t_lo / kFewTile * kFewTile;
   } else {
-    const int last = row0 + kFewRows - 1 < R ? row0 + kFewRows - 1 : R - 1;
-    t_hi = base + last / c.G + 1;
+    t_hi = base + i1 + 1;
   }
   // this share's tiles, every kFewWaves'th of them this wave's
   const int tiles = t_hi > t_lo ? (t_hi - t_lo + kFewTile - 1) / kFewTile : 0;
@@ -455,7 +639,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void chunk_attend_few_kernel(const 
   }
   const int rr = row0 + row;
   if (p.n_split == 1) {
-    const int ri = rr / c.G;
+    const int ri = chunk_token(rr, p.g_magic);
     const size_t orow = ((size_t)b * p.T + ri) * c.Hq + (size_t)h * c.G + (rr - ri * c.G);
     chunk_write<D>(p, orow, d0, o, use, sum);
   } else {
@@ -501,7 +685,7 @@ __global__ __launch_bounds__(kMergeThreads) void chunk_merge_kernel(const ChunkA
       }
     }
   }
-  const int i = r / c.G;
+  const int i = chunk_token(r, p.g_magic);
   chunk_write<D>(p, ((size_t)b * p.T + i) * c.Hq + (size_t)h * c.G + (r - i * c.G), d0, o, top, sum);
 }
 

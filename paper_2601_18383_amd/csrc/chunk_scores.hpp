@@ -3,7 +3,9 @@
 // log-sum-exp L_r.
 //
 // Keys are the stationary operand (B: 64 slots a wave), query rows stream through LDS 32 at a time (A), so that a lane holds 16
-// rows of one slot, adds them up by itself, and joins the other half once, at the end: no atomics, one order.
+// rows of one slot, adds them up by itself, and joins the other half once, at the end: no atomics, one order.  What a row sees, and its L, are
+// looked up a group of 256 rows ahead, one row a thread.  Chunks of rows that all see all of a wave's keys skip the comparisons,
+// those that see none skip the products.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -23,24 +25,31 @@ struct ChunkScoreParams {
   int skip_question;     // slots below n_prompt are left alone
   int accumulate;
   float scale_log2;
+  uint32_t g_magic;      // as in ChunkAttendParams
 };
 
 constexpr int kCsKeys = kSbRowsPerWg;  // slots a workgroup
+constexpr int kCsGroup = kSbLRows, kCsPer = kCsGroup / kSbChunk;  // rows looked up at a time; chunks of them
+
+// of a group's rows: minus their L, and what they see: the last slot, or shaped the lowest position, the distance to the highest, their own, their slope
+template <bool SHAPED>
+struct ChunkRows {
+  float minus_l[kCsGroup];
+  int lo[kCsGroup];
+  uint32_t span[SHAPED ? kCsGroup : 1];
+  float at[SHAPED ? kCsGroup : 1], slope[SHAPED ? kCsGroup : 1];
+  // by chunk, shaped: what all of its rows see, what any does
+  int all_lo[kCsPer], all_hi[kCsPer], any_lo[kCsPer], any_hi[kCsPer];
+};
 
 // 1-D grid of ceil(cap / 256) * round_up(units, 8) workgroups, 256 threads.
 template <int D, bool SHAPED>
-__global__ __launch_bounds__(kSbWaves * 64) void chunk_scores_kernel(const ChunkScoreParams p) {
+__global__ __launch_bounds__(kSbWaves * 64, D == 128 ? 3 : 4) void chunk_scores_kernel(const ChunkScoreParams p) {
   using St = SbStage<D>;
   const ChunkCache &c = p.c;
-  __shared__ __attribute__((aligned(16))) char sm_q[St::kBufBytes];
-  struct Row {
-    float L;      // log2 of the denominator, +inf: the row does not count
-    int lo;       // plain: the last slot it sees; shaped: the lowest position
-    uint32_t span;
-    float at, slope;
-  };
-  __shared__ Row sm_row[kSbChunk];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, hf = lane >> 5;
+  __shared__ __attribute__((aligned(16))) char sm_q[2][St::kBufBytes];
+  __shared__ __attribute__((aligned(16))) ChunkRows<SHAPED> sm_rows[2];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, hf = lane >> 5;
   int unit, blk;
   if (!sb_map((c.cap + kCsKeys - 1) / kCsKeys, c.Nb * c.Hkv, unit, blk)) return;
   const int b = unit / c.Hkv, h = unit - b * c.Hkv;
@@ -56,7 +65,7 @@ __global__ __launch_bounds__(kSbWaves * 64) void chunk_scores_kernel(const Chunk
   const int ref = SHAPED ? __builtin_amdgcn_readfirstlane(pos[base]) : 0;
 
   bf16x8 kf[kSbTiles][D / 16];
-  int kpos[kSbTiles];
+  int kpos[kSbTiles];  // of the lane's keys: slot, or shaped position
   float kat[kSbTiles], sum[kSbTiles];
 #pragma unroll
   for (int kt = 0; kt < kSbTiles; ++kt) {
@@ -69,55 +78,158 @@ __global__ __launch_bounds__(kSbWaves * 64) void chunk_scores_kernel(const Chunk
     kat[kt] = SHAPED ? (float)(kpos[kt] - ref) : 0.f;
     sum[kt] = 0.f;
   }
-  // (plain: rows whose own slot lies before all of these keys see none of them)
-  const int i0 = SHAPED ? 0 : (blk * kCsKeys > base ? blk * kCsKeys - base : 0);
-  for (int ch = i0 * c.G / kSbChunk; ch * kSbChunk < R; ++ch) {
-    __syncthreads();
-    {
-      const int at = tid >> 3, r = ch * kSbChunk + at < R ? ch * kSbChunk + at : R - 1, i = r / c.G, g = r - i * c.G;
-      const size_t qrow = ((size_t)b * p.T + i) * c.Hq + (size_t)h * c.G + g;
-      const char *src = reinterpret_cast<const char *>(p.q + qrow * D) + 16 * (tid & 7);
+  const bool has_keys = key0 < n && key0 + kSbRowsPerWave > skip;  // else: staging and barriers only
+  const int k_first = __builtin_amdgcn_readfirstlane(kpos[0]), k_last = __shfl(kpos[kSbTiles - 1], 31);
+
+  // staging: eight threads a row, 128 bytes apart
+  const int st_row = tid >> 3;
+  const uint32_t st_piece = 16u * (uint32_t)(tid & 7);
+  char *const park = sm_q[0] + st_row * St::LROW + st_piece;
+  u32x4 stage[St::NL];
+  auto row_of = [&](int r) {
+    r = r < R ? r : R - 1;
+    const int i = chunk_token(r, p.g_magic);
+    return ((size_t)b * p.T + i) * c.Hq + (size_t)h * c.G + (r - i * c.G);
+  };
+  auto fetch = [&](int ch) {
+    const char *src = reinterpret_cast<const char *>(p.q + row_of(ch * kSbChunk + st_row) * D) + st_piece;
 #pragma unroll
-      for (int k = 0; k < St::NL; ++k)
-        *reinterpret_cast<u32x4 *>(sm_q + at * St::LROW + 16 * (tid & 7) + 128 * k) = *reinterpret_cast<const u32x4 *>(src + 128 * k);
-      if ((tid & 7) == 0) {
-        Row row;
-        const float l = p.lse[qrow];
-        row.L = ch * kSbChunk + at < R && l != -INFINITY ? l * 1.4426950408889634f : INFINITY;
-        row.lo = base + i;
-        row.span = 0;
-        row.at = row.slope = 0.f;
-        if (SHAPED) {
-          const int own = pos[base + i];
-          chunk_interval(p.shape, (size_t)b * p.T + i, own, row.lo, row.span);
-          row.at = (float)(own - ref);
-          if (p.shape.slope) row.slope = p.shape.slope[h * c.G + g] * 1.4426950408889634f;
-        }
-        sm_row[at] = row;
-      }
+    for (int k = 0; k < St::NL; ++k) stage[k] = *reinterpret_cast<const u32x4 *>(src + 128 * k);
+  };
+  auto put = [&](int buf) {
+#pragma unroll
+    for (int k = 0; k < St::NL; ++k) *reinterpret_cast<u32x4 *>(park + buf * St::kBufBytes + 128 * k) = stage[k];
+  };
+  // one row a thread, of the group that begins with row r0
+  float row_l = 0.f;
+  int row_own = 0, row_first = 0, row_last = 0, row_r = 0;
+  auto fetch_rows = [&](int r0) {
+    row_r = r0 + tid;
+    row_l = p.lse[row_of(row_r)];
+    if (SHAPED) {
+      const int i = chunk_token(row_r < R ? row_r : R - 1, p.g_magic);
+      const size_t at = (size_t)b * p.T + i;
+      row_own = pos[base + i];
+      if (p.shape.first) row_first = p.shape.first[at];
+      if (p.shape.last) row_last = p.shape.last[at];
     }
-    __syncthreads();
-    f32x16 acc[kSbTiles];
-    sb_multiply<D>(acc, sm_q, kf, col, hf);
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const Row row = sm_row[8 * (e >> 2) + 4 * hf + (e & 3)];
-#pragma unroll
-      for (int kt = 0; kt < kSbTiles; ++kt) {
-        float x;
-        bool seen;
-        if (SHAPED) {
-          x = p.shape.cap > 0.f ? soft_cap(acc[kt][e], p.shape) : acc[kt][e] * p.scale_log2;
-          x -= row.slope * fabsf(row.at - kat[kt]);
-          seen = (uint32_t)(kpos[kt] - row.lo) <= row.span;
-        } else {
-          x = acc[kt][e] * p.scale_log2;
-          seen = kpos[kt] <= row.lo;
-        }
-        sum[kt] += seen ? fast_exp2(x - row.L) : 0.f;
+  };
+  auto put_rows = [&](int buf) {
+    ChunkRows<SHAPED> &rows = sm_rows[buf];
+    const bool real = row_r < R;
+    const int r = real ? row_r : R - 1, i = chunk_token(r, p.g_magic);
+    // (a row without a key it sees has no weights: its comparisons say so.  Rows behind the last see nothing)
+    rows.minus_l[tid] = row_l == -INFINITY ? 0.f : row_l * -1.4426950408889634f;
+    if (SHAPED) {
+      int lo;
+      uint32_t span;
+      chunk_bounds(p.shape, row_first, row_last, row_own, lo, span);
+      if (!real) {
+        lo = kNowhere;
+        span = 0;
       }
+      rows.lo[tid] = lo;
+      rows.span[tid] = span;
+      rows.at[tid] = (float)(row_own - ref);
+      rows.slope[tid] = p.shape.slope ? p.shape.slope[h * c.G + (r - i * c.G)] * 1.4426950408889634f : 0.f;
+      const int hi = lo == kNowhere ? -1 : (int)(lo + span);
+      int all_lo = lo, all_hi = hi, any_lo = lo, any_hi = hi;
+#pragma unroll
+      for (int d = 1; d < 32; d *= 2) {
+        const int al = __shfl_xor(all_lo, d), ah = __shfl_xor(all_hi, d), nl = __shfl_xor(any_lo, d), nh = __shfl_xor(any_hi, d);
+        all_lo = al > all_lo ? al : all_lo;
+        all_hi = ah < all_hi ? ah : all_hi;
+        any_lo = nl < any_lo ? nl : any_lo;
+        any_hi = nh > any_hi ? nh : any_hi;
+      }
+      if (col == 0) {
+        rows.all_lo[tid >> 5] = all_lo;
+        rows.all_hi[tid >> 5] = all_hi;
+        rows.any_lo[tid >> 5] = any_lo;
+        rows.any_hi[tid >> 5] = any_hi;
+      }
+    } else {
+      rows.lo[tid] = real ? base + i : -1;
     }
+  };
+
+  // (plain, and shaped without `last`: rows whose own slot lies before all of these keys see none of them)
+  const int i0 = (SHAPED && p.shape.last) || blk * kCsKeys <= base ? 0 : blk * kCsKeys - base;
+  const int first = i0 * c.G / kCsGroup * kCsPer, chunks = (R + kSbChunk - 1) / kSbChunk;  // (from a whole group on)
+  if (first < chunks) {
+    fetch_rows(first * kSbChunk);
+    fetch(first);
+    put(0);
+    put_rows(0);
+    if (first + 1 < chunks) fetch(first + 1);
   }
+  int buf = 0;
+  for (int ch = first; ch < chunks; ++ch) {
+    __syncthreads();
+    if (ch + 1 < chunks) put(buf ^ 1);
+    if (ch + 2 < chunks) fetch(ch + 2);
+    const int in_group = (ch - first) % kCsPer, group = (ch - first) / kCsPer;
+    if (in_group == 0 && ch + kCsPer < chunks) fetch_rows((ch + kCsPer) * kSbChunk);
+    if (in_group == kCsPer - 1 && ch + 1 < chunks) put_rows((group + 1) & 1);
+    const ChunkRows<SHAPED> &rows = sm_rows[group & 1];
+    const int r0 = in_group * kSbChunk;
+    bool any = has_keys, all;
+    if (SHAPED) {
+      any = any && __builtin_amdgcn_readfirstlane(rows.any_lo[in_group]) <= k_last && __builtin_amdgcn_readfirstlane(rows.any_hi[in_group]) >= k_first;
+      all = __builtin_amdgcn_readfirstlane(rows.all_lo[in_group]) <= k_first && __builtin_amdgcn_readfirstlane(rows.all_hi[in_group]) >= k_last;
+    } else {
+      const int last = (ch + 1) * kSbChunk - 1;
+      any = any && base + chunk_token(last < R ? last : R - 1, p.g_magic) >= k_first;
+      all = last < R && base + chunk_token(ch * kSbChunk, p.g_magic) >= k_last;
+    }
+    if (__builtin_amdgcn_readfirstlane((int)any)) {
+      f32x16 acc[kSbTiles];
+      sb_multiply<D>(acc, sm_q[buf], kf, col, hf);
+      f32x4 ml[4];  // of the rows 8 j + 4 hf .. +3 that this lane's products belong to
+#pragma unroll
+      for (int j = 0; j < 4; ++j) ml[j] = *reinterpret_cast<const f32x4 *>(&rows.minus_l[r0 + 8 * j + 4 * hf]);
+      float scale = p.scale_log2;
+      if (SHAPED && (p.shape.cap > 0.f || p.shape.slope)) {
+        scale = 1.f;
+        if (p.shape.cap > 0.f) {
+#pragma unroll
+          for (int kt = 0; kt < kSbTiles; ++kt)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[kt][e] = soft_cap(acc[kt][e], p.shape);
+        } else {
+#pragma unroll
+          for (int kt = 0; kt < kSbTiles; ++kt)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[kt][e] *= p.scale_log2;
+        }
+        if (p.shape.slope) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int r = r0 + 8 * (e >> 2) + 4 * hf + (e & 3);
+            const float at = rows.at[r], slope = rows.slope[r];
+#pragma unroll
+            for (int kt = 0; kt < kSbTiles; ++kt) acc[kt][e] = fmaf(-slope, fabsf(at - kat[kt]), acc[kt][e]);
+          }
+        }
+      }
+      if (!__builtin_amdgcn_readfirstlane((int)all)) {
+        asm volatile("; some keys are hidden");  // (a branch: the compiler would compare every key of every chunk)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int r = r0 + 8 * (e >> 2) + 4 * hf + (e & 3), lo = rows.lo[r];
+#pragma unroll
+          for (int kt = 0; kt < kSbTiles; ++kt) {
+            const bool seen = SHAPED ? (uint32_t)(kpos[kt] - lo) <= rows.span[SHAPED ? r : 0] : kpos[kt] <= lo;
+            if (!seen) acc[kt][e] = -INFINITY;
+          }
+        }
+      }
+#pragma unroll
+      for (int kt = 0; kt < kSbTiles; ++kt) sum[kt] += sb_exp_sum(acc[kt], scale, [&](int e) { return ml[e >> 2][e & 3]; });
+    }
+    buf ^= 1;
+  }
+  if (!has_keys) return;
   float tot[kSbTiles];
 #pragma unroll
   for (int kt = 0; kt < kSbTiles; ++kt) tot[kt] = sum[kt] + __shfl_xor(sum[kt], 32);
