@@ -30,6 +30,7 @@ struct ChunkScoreParams {
 
 constexpr int kCsKeys = kSbRowsPerWg;  // slots a workgroup
 constexpr int kCsGroup = kSbLRows, kCsPer = kCsGroup / kSbChunk;  // rows looked up at a time; chunks of them
+constexpr int kCsStage = 2;              // chunks staged at a time, one barrier for all
 
 // of a group's rows: minus their L, and what they see: the last slot, or shaped the lowest position, the distance to the highest, their own, their slope
 template <bool SHAPED>
@@ -47,7 +48,7 @@ template <int D, bool SHAPED>
 __global__ __launch_bounds__(kSbWaves * 64, D == 128 ? 3 : 4) void chunk_scores_kernel(const ChunkScoreParams p) {
   using St = SbStage<D>;
   const ChunkCache &c = p.c;
-  __shared__ __attribute__((aligned(16))) char sm_q[2][St::kBufBytes];
+  __shared__ __attribute__((aligned(16))) char sm_q[2][kCsStage * St::kBufBytes];
   __shared__ __attribute__((aligned(16))) ChunkRows<SHAPED> sm_rows[2];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, hf = lane >> 5;
   int unit, blk;
@@ -85,20 +86,25 @@ __global__ __launch_bounds__(kSbWaves * 64, D == 128 ? 3 : 4) void chunk_scores_
   const int st_row = tid >> 3;
   const uint32_t st_piece = 16u * (uint32_t)(tid & 7);
   char *const park = sm_q[0] + st_row * St::LROW + st_piece;
-  u32x4 stage[St::NL];
+  u32x4 stage[kCsStage][St::NL];
   auto row_of = [&](int r) {
     r = r < R ? r : R - 1;
     const int i = chunk_token(r, p.g_magic);
     return ((size_t)b * p.T + i) * c.Hq + (size_t)h * c.G + (r - i * c.G);
   };
   auto fetch = [&](int ch) {
-    const char *src = reinterpret_cast<const char *>(p.q + row_of(ch * kSbChunk + st_row) * D) + st_piece;
 #pragma unroll
-    for (int k = 0; k < St::NL; ++k) stage[k] = *reinterpret_cast<const u32x4 *>(src + 128 * k);
+    for (int x = 0; x < kCsStage; ++x) {
+      const char *src = reinterpret_cast<const char *>(p.q + row_of((ch + x) * kSbChunk + st_row) * D) + st_piece;
+#pragma unroll
+      for (int k = 0; k < St::NL; ++k) stage[x][k] = *reinterpret_cast<const u32x4 *>(src + 128 * k);
+    }
   };
   auto put = [&](int buf) {
 #pragma unroll
-    for (int k = 0; k < St::NL; ++k) *reinterpret_cast<u32x4 *>(park + buf * St::kBufBytes + 128 * k) = stage[k];
+    for (int x = 0; x < kCsStage; ++x)
+#pragma unroll
+      for (int k = 0; k < St::NL; ++k) *reinterpret_cast<u32x4 *>(park + (buf * kCsStage + x) * St::kBufBytes + 128 * k) = stage[x][k];
   };
   // one row a thread, of the group that begins with row r0
   float row_l = 0.f;
@@ -161,17 +167,11 @@ __global__ __launch_bounds__(kSbWaves * 64, D == 128 ? 3 : 4) void chunk_scores_
     fetch(first);
     put(0);
     put_rows(0);
-    if (first + 1 < chunks) fetch(first + 1);
+    if (first + kCsStage < chunks) fetch(first + kCsStage);
   }
-  int buf = 0;
-  for (int ch = first; ch < chunks; ++ch) {
-    __syncthreads();
-    if (ch + 1 < chunks) put(buf ^ 1);
-    if (ch + 2 < chunks) fetch(ch + 2);
-    const int in_group = (ch - first) % kCsPer, group = (ch - first) / kCsPer;
-    if (in_group == 0 && ch + kCsPer < chunks) fetch_rows((ch + kCsPer) * kSbChunk);
-    if (in_group == kCsPer - 1 && ch + 1 < chunks) put_rows((group + 1) & 1);
-    const ChunkRows<SHAPED> &rows = sm_rows[group & 1];
+  // a chunk whose rows are in `q`, and what is known of them from row r0 of `rows` on
+  auto chunk = [&](int ch, const char *q, const ChunkRows<SHAPED> &rows) {
+    const int in_group = (ch - first) % kCsPer;
     const int r0 = in_group * kSbChunk;
     bool any = has_keys, all;
     if (SHAPED) {
@@ -184,7 +184,7 @@ __global__ __launch_bounds__(kSbWaves * 64, D == 128 ? 3 : 4) void chunk_scores_
     }
     if (__builtin_amdgcn_readfirstlane((int)any)) {
       f32x16 acc[kSbTiles];
-      sb_multiply<D>(acc, sm_q[buf], kf, col, hf);
+      sb_multiply<D>(acc, q, kf, col, hf);
       f32x4 ml[4];  // of the rows 8 j + 4 hf .. +3 that this lane's products belong to
 #pragma unroll
       for (int j = 0; j < 4; ++j) ml[j] = *reinterpret_cast<const f32x4 *>(&rows.minus_l[r0 + 8 * j + 4 * hf]);
@@ -227,6 +227,18 @@ __global__ __launch_bounds__(kSbWaves * 64, D == 128 ? 3 : 4) void chunk_scores_
 #pragma unroll
       for (int kt = 0; kt < kSbTiles; ++kt) sum[kt] += sb_exp_sum(acc[kt], scale, [&](int e) { return ml[e >> 2][e & 3]; });
     }
+  };
+  int buf = 0;
+  for (int ch = first; ch < chunks; ch += kCsStage) {
+    __syncthreads();
+    if (ch + kCsStage < chunks) put(buf ^ 1);
+    if (ch + 2 * kCsStage < chunks) fetch(ch + 2 * kCsStage);
+    const int in_group = (ch - first) % kCsPer, group = (ch - first) / kCsPer;
+    if (in_group == 0 && ch + kCsPer < chunks) fetch_rows((ch + kCsPer) * kSbChunk);
+    if (in_group == kCsPer - kCsStage && ch + kCsStage < chunks) put_rows((group + 1) & 1);
+#pragma unroll
+    for (int x = 0; x < kCsStage; ++x)
+      if (ch + x < chunks) chunk(ch + x, sm_q[buf] + x * St::kBufBytes, sm_rows[group & 1]);
     buf ^= 1;
   }
   if (!has_keys) return;
