@@ -24,31 +24,59 @@ int launch_status() { return hipGetLastError() == hipSuccess ? DYNTS_OK : DYNTS_
 // scratch of a chunk's calls
 struct ChunkPlan {
   bool few;          // chunk_attend_few_kernel
-  int blocks, n_split, Rpad;
-  size_t off_lse = 0, off_ml = 0, off_o = 0, bytes = 0;
+  int rows, blocks;  // query rows of a workgroup, row blocks of a unit
+  int n_split, Rpad;
+  size_t off_lse = 0, off_n = 0, off_ml = 0, off_o = 0, bytes = 0;
 };
 
-// At most this many workgroups take a share of a row block's keys.
-constexpr int kMostShares = 512;
+// Rows of partials that the shares of one call may leave.
+constexpr long long kMostPartials = 65536;
 
-ChunkPlan chunk_plan(const dynts_config &c, int n_tokens) {
+// Which kernel, and into how many shares the keys of a row block are cut at most.  slots: how many a token can see.
+//
+// Few rows, F row blocks of 32, one workgroup a compute unit (two with head_dim 64): a row block is done in 5 + 5.8 us per 1000 slots; many rows, W
+// of 128, three or four a compute unit: 4.5 + 23 us per 1000 slots, 21 where all of them are busy.  us, few / many, each with its best shares:
+//   head_dim 128, 8 units: 1000 slots R = 4 10.3 / 10.2, R = 256 12.8 / 16.7, R = 1024 15.6 / 25.5; 4500 slots R = 64 14.9 / 18.6, R = 512 27.3 / 30.9,
+//     R = 1024 41.5 / 39.2; 16000 slots R = 128 27.0 / 31.2, R = 256 39.8 / 38.4, R = 512 69.5 / 52.3
+//   32 units: 200 slots R = 256 8.8 / 12.0, R = 512 16.4 / 13.8; 4500 slots R = 128 27.9 / 28.3, R = 256 40.8 / 37.6; 16000 slots R = 64 49.0 / 52.3, R = 128
+//     71.0 / 60.7
+//   128 units: R = 64 200 slots 8.5 / 10.3, 4500 52.9 / 59.7, 16000 189 / 199; R = 128 200 slots 15.0 / 11.8, 4500 91.3 / 72.4
+//   512 units: R = 16 300 slots 18.8 / 17.6, 2600 119.7 / 129.6; R = 64 300 slots 32.9 / 20.0, 2600 144.6 / 130.1
+//   head_dim 64: 2 units of 6000 slots R = 1024 30.5 / 27.6, R = 2048 53.5 / 41.8; 10 of 400 R = 308 7.9 / 11.0; 128 of 400 R = 77 9.1 / 12.0, R = 128 9.6 / 11.3, R =
+//     256 18.6 / 15.8
+// Shares, at least 512 slots each, until the chip is full.  us by their number:
+//   few rows, head_dim 128: 8 units of 1000 slots 1 / 2 / 4: 10.6 / 10.5 / 10.6, of 4500 1 / 4 / 8 / 16: 31.0 / 14.0 / 11.5 / 11.0, of 16000 8 / 16 / 32: 21.1 /
+//     19.3 / 22.1; 128 units of 1000 1 / 2: 14.4 / 15.7, of 4500 51.6 / 48.1; head_dim 64, 128 units of 6000 1 / 2: 30.5 / 33.2, 10 of 1500 9.4 / 10.5
+//   many rows, W = 64, 4500 slots 1 / 4 / 8 / 16: 114 / 44.6 / 39.2 / 50.1; W = 128 of 1000 1 / 2 / 4: 30.7 / 27.1 / 30.1; W = 256 of 4500 1 / 2 / 4: 123 /
+//     106 / 119, of 1000 34.6 / 37.4 / 49.0; W = 16 of 16000 8 / 16 / 32: 58.3 / 39.5 / 38.4
+ChunkPlan chunk_plan(const dynts_config &c, int n_tokens, int slots) {
   ChunkPlan pl;
   const long long R = (long long)n_tokens * (c.n_q_heads / c.n_kv_heads), units = (long long)c.batch * c.n_kv_heads;
-  pl.few = R <= 64;
-  const int rows = pl.few ? dynts::kFewRows : dynts::kChRows;
-  pl.blocks = (int)((R + rows - 1) / rows);
-  pl.Rpad = pl.blocks * rows;
-  pl.n_split = 1;
+  const long long F = units * ((R + dynts::kFewRows - 1) / dynts::kFewRows), W = units * ((R + dynts::kChRows - 1) / dynts::kChRows);
+  const bool wide_head = c.head_dim == 128;
+  pl.few = R <= dynts::kFewRows || (F <= (wide_head ? 256 : 512) && (R <= 2 * dynts::kFewRows || F * slots <= (wide_head ? 1 << 20 : 1 << 19)));
+  pl.rows = pl.few ? dynts::kFewRows : dynts::kChRows;
+  pl.blocks = (int)((R + pl.rows - 1) / pl.rows);
+  pl.Rpad = pl.blocks * pl.rows;
+  long long shares = slots / (32 * dynts::kShareTiles);
   if (pl.few) {
-    const long long want = 256 / (units * pl.blocks), most = (c.capacity + 255) / 256;
-    pl.n_split = (int)(want < most ? want : most);
-    pl.n_split = pl.n_split < 1 ? 1 : pl.n_split;
+    if (slots < 1536 || (!wide_head && F > 64)) shares = 1;
+    shares = shares < 16 ? shares : 16;
+    shares = shares < 256 / F ? shares : 256 / F;
+  } else {
+    shares = shares < 32 ? shares : 32;
+    shares = shares < 512 / W ? shares : 512 / W;
   }
+  while (shares > 1 && units * pl.Rpad * shares > kMostPartials) --shares;
+  pl.n_split = shares < 1 ? 1 : (int)shares;
   size_t off = align_up((size_t)c.batch * sizeof(int32_t));
   pl.off_lse = off;
   off += align_up((size_t)c.batch * n_tokens * c.n_q_heads * sizeof(float));
-  // (room for the shares of any shorter chunk, too)
-  const long long most = (long long)kMostShares * dynts::kFewRows;
+  // room for the shares of this and of every shorter chunk: of rows padded to either kernel's, in as many shares as the slots allow
+  const long long padded = (R + dynts::kChRows - 1) / dynts::kChRows * dynts::kChRows, all = units * padded * (c.capacity / (32 * dynts::kShareTiles));
+  const long long most = all < kMostPartials ? all : kMostPartials;
+  pl.off_n = off;
+  off += align_up((size_t)(most / dynts::kFewRows + 1) * sizeof(int32_t));
   pl.off_ml = off;
   off += align_up((size_t)most * 2 * sizeof(float));
   pl.off_o = off;
@@ -57,10 +85,12 @@ ChunkPlan chunk_plan(const dynts_config &c, int n_tokens) {
   return pl;
 }
 
-ChunkPlan chunk_plan(const ChunkCache &c, int n_tokens) {
+ChunkPlan chunk_plan(const ChunkCache &c, int n_tokens, const dynts_shaping *shaping = nullptr) {
   dynts_config cfg{};
   cfg.batch = c.Nb; cfg.n_q_heads = c.Hq; cfg.n_kv_heads = c.Hkv; cfg.head_dim = c.D; cfg.capacity = c.cap;
-  return chunk_plan(cfg, n_tokens);
+  // (slots of a window: no more than its positions, those of the chunk's other tokens beside them)
+  const long long seen = shaping && shaping->window > 0 ? (long long)shaping->window + n_tokens : c.cap;
+  return chunk_plan(cfg, n_tokens, (int)(seen < c.cap ? seen : c.cap));
 }
 
 int check_shaping(const dynts_shaping *s) {
@@ -135,16 +165,18 @@ void launch_attend_d(const dynts::ChunkAttendParams &p, const ChunkPlan &pl, uns
   else hipLaunchKernelGGL((dynts::chunk_attend_kernel<D, SHAPED>), dim3(grid), dim3(dynts::kChThreads), 0, st, p);
   if (p.n_split > 1) {
     constexpr int rows = dynts::kMergeThreads / (D / 8);
-    hipLaunchKernelGGL(dynts::chunk_merge_kernel<D>, dim3((p.T * p.c.G + rows - 1) / rows, p.c.Nb * p.c.Hkv), dim3(dynts::kMergeThreads), 0, st, p);
+    hipLaunchKernelGGL(dynts::chunk_merge_kernel<D>, dim3((p.T * p.c.G + rows - 1) / rows, p.c.Nb * p.c.Hkv), dim3(dynts::kMergeThreads), 0, st, p,
+                       pl.rows);
   }
 }
 
 int launch_attend(const ChunkCache &c, const uint16_t *q, int n_tokens, const int32_t *n_new, const dynts_shaping *shaping, uint16_t *out,
                   float *lse, void *scratch, hipStream_t st) {
-  const ChunkPlan pl = chunk_plan(c, n_tokens);
+  const ChunkPlan pl = chunk_plan(c, n_tokens, shaping);
   char *const base = static_cast<char *>(scratch);
   const dynts::ChunkAttendParams p{c, q, n_new, out, lse, chunk_shape(shaping, c.scale), n_tokens, c.scale * kLog2E, group_magic(c.G), pl.n_split, pl.Rpad,
-                                   reinterpret_cast<float *>(base + pl.off_o), reinterpret_cast<float *>(base + pl.off_ml)};
+                                   reinterpret_cast<float *>(base + pl.off_o), reinterpret_cast<float *>(base + pl.off_ml),
+                                   reinterpret_cast<int32_t *>(base + pl.off_n)};
   const unsigned grid = attend_grid(c, pl);
   if (!grid) return DYNTS_EINVAL;
   if (c.D == 128) {
@@ -182,7 +214,7 @@ extern "C" {
 
 size_t dynts_chunk_scratch_bytes(const dynts_config *cfg, int32_t n_tokens) {
   if (dynts::chunk_check_config(cfg) != DYNTS_OK || check_tokens(n_tokens) != DYNTS_OK) return 0;
-  return chunk_plan(*cfg, n_tokens).bytes;
+  return chunk_plan(*cfg, n_tokens, cfg->capacity).bytes;
 }
 
 int dynts_chunk_append(dynts_ctx *ctx, int32_t layer, const uint16_t *k_new, const uint16_t *v_new, const float *s_new, int32_t n_tokens,
@@ -233,7 +265,7 @@ int dynts_chunk_step(dynts_ctx *ctx, int32_t layer, const uint16_t *q, const uin
   if (rc != DYNTS_OK) return rc;
   if (!q || !out) return DYNTS_ENULL;
   if (misaligned(q, 16) || misaligned(out, 16)) return DYNTS_EINVAL;
-  const ChunkPlan pl = chunk_plan(c, n_tokens);
+  const ChunkPlan pl = chunk_plan(c, n_tokens, shaping);
   rc = check_scratch(scratch, scratch_bytes, pl.bytes);
   if (rc != DYNTS_OK) return rc;
   hipStream_t st = static_cast<hipStream_t>(stream);

@@ -43,11 +43,26 @@ struct ChunkAttendParams {
   int T;
   float scale_log2;
   uint32_t g_magic;       // ceil(2^32 / G), 0 for G = 1
-  // Keys of a row block cut into n_split shares, a workgroup each: unnormalised outputs and (shift, sum) of unit u, share s and row r in row
-  // (u * n_split + s) * Rpad + r
+  // Keys of a row block cut into shares, a workgroup each, as many as there are kShareTiles tiles for, n_split at most: unnormalised outputs
+  // and (shift, sum) of unit u, share s and row r in row (u * n_split + s) * Rpad + r; how many shares there are, in part_n[u * blocks + block].
+  // (The host does not know the lengths: a short cache has one share, and its output is written straight away.)
   int n_split, Rpad;
   float *part_o, *part_ml;  // [..][D], [..][2]
+  int32_t *part_n;
 };
+
+constexpr int kShareTiles = 16;  // least tiles of 32 slots in a share
+
+// This workgroup's share of the tiles of its rows, as [from, to); false: it has none.
+__device__ __forceinline__ bool chunk_share(const ChunkAttendParams &p, int tiles, int split, int place, int &shares, int &from, int &to) {
+  shares = tiles / kShareTiles;
+  shares = shares < 1 ? 1 : (shares < p.n_split ? shares : p.n_split);
+  if (p.n_split > 1 && split == 0 && threadIdx.x == 0) p.part_n[place] = shares;
+  if (split >= shares) return false;
+  from = (int)((long long)tiles * split / shares);
+  to = (int)((long long)tiles * (split + 1) / shares);
+  return true;
+}
 
 constexpr int kChWaves = 4, kChThreads = kChWaves * 64;
 constexpr int kChRows = 32 * kChWaves;  // query rows a workgroup
@@ -247,7 +262,8 @@ __global__ __launch_bounds__(kChThreads, D == 128 ? 3 : 4) void chunk_attend_ker
   }
   all_hi = __builtin_amdgcn_readfirstlane(all_hi);
   const int tiles = t_hi > t_lo ? (t_hi - t_lo + kChTile - 1) / kChTile : 0;
-  const int from = (int)((long long)tiles * split / p.n_split), to = (int)((long long)tiles * (split + 1) / p.n_split);
+  int shares, from, to;
+  if (!chunk_share(p, tiles, split, unit * n_blk + blk, shares, from, to)) return;
   const int t0 = __builtin_amdgcn_readfirstlane(t_lo + from * kChTile), t1 = __builtin_amdgcn_readfirstlane(t_lo + to * kChTile);
 
   f32x16 acc[D / 32];
@@ -419,7 +435,7 @@ __global__ __launch_bounds__(kChThreads, D == 128 ? 3 : 4) void chunk_attend_ker
   // sums of the two halves' keys; outputs row by row through LDS
   __syncthreads();
   const float sum = l + __shfl_xor(l, 32);
-  if (p.n_split > 1) {
+  if (shares > 1) {
     if (row0 + col >= R) return;
     const size_t prow = ((size_t)unit * p.n_split + split) * p.Rpad + row0 + col;
 #pragma unroll
@@ -520,7 +536,8 @@ __global__ __launch_bounds__(kFewThreads, 2) void chunk_attend_few_kernel(const 
   }
   // this share's tiles, every kFewWaves'th of them this wave's
   const int tiles = t_hi > t_lo ? (t_hi - t_lo + kFewTile - 1) / kFewTile : 0;
-  const int from = (int)((long long)tiles * split / p.n_split), to = (int)((long long)tiles * (split + 1) / p.n_split);
+  int shares, from, to;
+  if (!chunk_share(p, tiles, split, unit * n_blk + blk, shares, from, to)) return;
   const int t_end = __builtin_amdgcn_readfirstlane(t_lo + to * kFewTile);
   int t = __builtin_amdgcn_readfirstlane(t_lo + (from + wave) * kFewTile);
 
@@ -638,7 +655,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void chunk_attend_few_kernel(const 
     for (int j = 0; j < 8; ++j) o[j] += f * part[(j & 3) * 65 + 32 * (j >> 2)];
   }
   const int rr = row0 + row;
-  if (p.n_split == 1) {
+  if (shares == 1) {
     const int ri = chunk_token(rr, p.g_magic);
     const size_t orow = ((size_t)b * p.T + ri) * c.Hq + (size_t)h * c.G + (rr - ri * c.G);
     chunk_write<D>(p, orow, d0, o, use, sum);
@@ -653,28 +670,30 @@ __global__ __launch_bounds__(kFewThreads, 2) void chunk_attend_few_kernel(const 
 // The shares of a row together.  grid (ceil(T * G / kMergeRows), units), D / 8 threads a row.
 constexpr int kMergeThreads = 256;
 template <int D>
-__global__ __launch_bounds__(kMergeThreads) void chunk_merge_kernel(const ChunkAttendParams p) {
+__global__ __launch_bounds__(kMergeThreads) void chunk_merge_kernel(const ChunkAttendParams p, int block_rows) {
   const ChunkCache &c = p.c;
   const int unit = blockIdx.y, b = unit / c.Hkv, h = unit - b * c.Hkv;
   int n;
   const int m = chunk_tokens(c, p.n_new, p.T, b, n);
   const int r = blockIdx.x * (kMergeThreads / (D / 8)) + threadIdx.x / (D / 8), d0 = 8 * (threadIdx.x % (D / 8));
   if (r >= m * c.G) return;
+  const int shares = p.part_n[unit * (p.Rpad / block_rows) + r / block_rows];
+  if (shares == 1) return;
   const size_t first = (size_t)unit * p.n_split * p.Rpad + r;
   float top = -INFINITY, sum = 0.f, o[8] = {};
-  for (int s0 = 0; s0 < p.n_split; s0 += 4) {  // four shares' loads at a time
+  for (int s0 = 0; s0 < shares; s0 += 4) {  // four shares' loads at a time
     float2 ml[4];
     f32x4 a[4], z[4];
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
-      const size_t prow = first + (size_t)(s0 + s < p.n_split ? s0 + s : s0) * p.Rpad;
+      const size_t prow = first + (size_t)(s0 + s < shares ? s0 + s : s0) * p.Rpad;
       ml[s] = *reinterpret_cast<const float2 *>(p.part_ml + 2 * prow);
       a[s] = *reinterpret_cast<const f32x4 *>(p.part_o + prow * D + d0);
       z[s] = *reinterpret_cast<const f32x4 *>(p.part_o + prow * D + d0 + 4);
     }
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
-      if (s0 + s >= p.n_split || !(ml[s].y > 0.f)) continue;  // (a share without a key that the row sees)
+      if (s0 + s >= shares || !(ml[s].y > 0.f)) continue;  // (a share without a key that the row sees)
       const float next = fmaxf(top, ml[s].x), f = fast_exp2(top - next), w = fast_exp2(ml[s].x - next);
       top = next;
       sum = sum * f + ml[s].y * w;

@@ -98,6 +98,8 @@ SHAPES = [  # Hq, Hkv, d, n_old, n_new
     (32, 8, 128, [1000], [16]),
     (4, 2, 64, [10, 700], [300, 129]),                                  # several row blocks
     (8, 2, 128, [2500, 1], [5, 2]),
+    (8, 1, 128, [3000, 10], [200, 64]),                                 # many rows, keys in shares; a short cache beside it
+    (4, 1, 64, [4000, 900], [300, 1]),
 ]
 
 
@@ -158,7 +160,7 @@ def _shapings(c, gen, kind):
 @pytest.mark.parametrize("layout", ["dense", "paged"])
 @pytest.mark.parametrize("kind", ["cap", "cap_tight", "slope", "window", "window_one", "documents", "prefix", "empty", "future",
                                   "cap_slope_window_documents_prefix", "slope_prefix_empty"])
-@pytest.mark.parametrize("Hq,Hkv,d,n_old,n_new", [SHAPES[0], SHAPES[1], SHAPES[3], SHAPES[6]])
+@pytest.mark.parametrize("Hq,Hkv,d,n_old,n_new", [SHAPES[0], SHAPES[1], SHAPES[3], SHAPES[6], SHAPES[7], SHAPES[9]])
 def test_shaped(B, layout, kind, Hq, Hkv, d, n_old, n_new):
     c = Case(B, layout, Hq, Hkv, d, n_old, n_new, gaps=90, seed=11, qscale=2.0).fill(True)
     s = _shapings(c, c.gen, kind)
