@@ -162,7 +162,8 @@ unsigned scores_grid(const ChunkCache &c) { return chunk_grid(c, (c.cap + dynts:
 template <int D, bool SHAPED>
 void launch_attend_d(const dynts::ChunkAttendParams &p, const ChunkPlan &pl, unsigned grid, hipStream_t st) {
   if (pl.few) hipLaunchKernelGGL((dynts::chunk_attend_few_kernel<D, SHAPED>), dim3(grid), dim3(dynts::kFewThreads), 0, st, p);
-  else hipLaunchKernelGGL((dynts::chunk_attend_kernel<D, SHAPED>), dim3(grid), dim3(dynts::kChThreads), 0, st, p);
+  else if (SHAPED && p.shape.slope) hipLaunchKernelGGL((dynts::chunk_attend_kernel<D, SHAPED, SHAPED>), dim3(grid), dim3(dynts::kChThreads), 0, st, p);
+  else hipLaunchKernelGGL((dynts::chunk_attend_kernel<D, SHAPED, false>), dim3(grid), dim3(dynts::kChThreads), 0, st, p);
   if (p.n_split > 1) {
     constexpr int rows = dynts::kMergeThreads / (D / 8);
     hipLaunchKernelGGL(dynts::chunk_merge_kernel<D>, dim3((p.T * p.c.G + rows - 1) / rows, p.c.Nb * p.c.Hkv), dim3(dynts::kMergeThreads), 0, st, p,

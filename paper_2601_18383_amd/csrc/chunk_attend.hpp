@@ -189,7 +189,8 @@ __device__ __forceinline__ int chunk_lds_v(int row, int piece) {
   return row * (2 * D) + 16 * (piece ^ (D == 128 ? (row & 3) << 2 : ((row >> 1) & 1) << 2));
 }
 
-template <int D, bool SHAPED>
+// SHAPED: positions count, not slots.  BIASED: with a bias by distance.
+template <int D, bool SHAPED, bool BIASED>
 __global__ __launch_bounds__(kChThreads, D == 128 ? 3 : 4) void chunk_attend_kernel(const ChunkAttendParams p) {
   using Lds = ChunkLds<D>;
   const ChunkCache &c = p.c;
@@ -217,20 +218,17 @@ __global__ __launch_bounds__(kChThreads, D == 128 ? 3 : 4) void chunk_attend_ker
   bf16x8 qf[D / 16];
   load_row_frags<D>(qf, reinterpret_cast<const char *>(p.q + (((size_t)b * p.T + tok) * c.Hq + (size_t)h * c.G + g) * D), hf);
   float slope = 0.f;
-  if (SHAPED && p.shape.slope) slope = p.shape.slope[h * c.G + g] * 1.4426950408889634f;
+  if (BIASED) slope = p.shape.slope[h * c.G + g] * 1.4426950408889634f;
 
   // what the rows see: plain, slots [0, lim]; shaped, positions [lo, lo + span].  all_lo, all_hi: what all of the wave's rows see
   const int32_t *pos = c.pos + (size_t)unit * c.cap;
-  int lim, ref = 0, t_lo = 0, t_hi, all_lo = 0, all_hi;
+  int lim, own = 0, t_lo = 0, t_hi, all_lo = 0, all_hi;
   uint32_t span = 0;
-  float at = 0.f;
   const int r1 = blk * kChRows + kChRows - 1;
   const int i0 = chunk_token(blk * kChRows, p.g_magic), i1 = chunk_token(r1 < R ? r1 : R - 1, p.g_magic);
   if (SHAPED) {
-    ref = __builtin_amdgcn_readfirstlane(pos[base]);
-    const int own = pos[base + tok];
+    own = pos[base + tok];
     chunk_interval(p.shape, (size_t)b * p.T + tok, own, lim, span);
-    at = (float)(own - ref);
     int first = lim, last = lim == kNowhere ? -1 : (int)(lim + span);
     all_lo = first;
     all_hi = last;
@@ -323,28 +321,21 @@ __global__ __launch_bounds__(kChThreads, D == 128 ? 3 : 4) void chunk_attend_ker
     }
   };
   // Logits of tile t from its products: shaped, and hidden keys' at -inf.  `scale` is still to be multiplied with them, 1 if they are log2 units already.
-  const bool capped = SHAPED && p.shape.cap > 0.f, biased = SHAPED && p.shape.slope != nullptr;
-  const float scale = capped || biased ? 1.f : p.scale_log2;
-  auto shape = [&](f32x16 &s, int t, uint32_t place) {
+  const bool capped = SHAPED && p.shape.cap > 0.f;
+  const float scale = capped || BIASED ? 1.f : p.scale_log2;
+  auto shape = [&](f32x16 &s, int t, const int *tp) {
     if (SHAPED) {
-      const int *tp = reinterpret_cast<const int *>(sm + place + 2 * Lds::kTileBytes);
-      const int first = __builtin_amdgcn_readfirstlane(tp[0]), last = __builtin_amdgcn_readfirstlane(tp[kChTile - 1]);
-      const bool all = first >= all_lo && last <= all_hi && t + kChTile <= n;
       if (capped) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[e] = soft_cap(s[e], p.shape);
-      } else if (biased) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) s[e] *= p.scale_log2;
       }
-      if (biased) {
+      if (BIASED) {
+        const float c = capped ? 1.f : p.scale_log2;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const float f = (float)(tp[8 * (e >> 2) + 4 * hf + (e & 3)] - ref);
-          s[e] = fmaf(-slope, fabsf(at - f), s[e]);
-        }
+        for (int e = 0; e < 16; ++e) s[e] = fmaf(-slope, fabsf((float)(own - tp[8 * (e >> 2) + 4 * hf + (e & 3)])), s[e] * c);
       }
-      if (!all) {
+      const int first = __builtin_amdgcn_readfirstlane(tp[0]), last = __builtin_amdgcn_readfirstlane(tp[kChTile - 1]);
+      if (first < all_lo || last > all_hi || t + kChTile > n) {
         asm volatile("; some keys are hidden");  // (a branch: the compiler would compare every key of every tile)
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
@@ -374,18 +365,22 @@ __global__ __launch_bounds__(kChThreads, D == 128 ? 3 : 4) void chunk_attend_ker
     }
     return (q[0] + q[1]) + (q[2] + q[3]);
   };
-  // the shift raised to the tile's largest logit, where that lies above it
-  auto raise = [&](const f32x16 &s, float &sum, bf16x8 (&pf)[2]) {
-    float mx = s[0];
+  // the same, the shift raised to the tile's largest logit where that lies far above it
+  auto weigh = [&](const f32x16 &s, bf16x8 (&pf)[2]) {
+    float sum = fold(s, pf);
+    if (__any(!(sum < kChLimit))) {
+      float mx = s[0];
 #pragma unroll
-    for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[e]);
-    mx = fmaxf(mx, __shfl_xor(mx, 32));
-    const float next = fminf(floorf(-mx * scale), nm), f = fast_exp2(next - nm);
-    l *= f;
+      for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[e]);
+      mx = fmaxf(mx, __shfl_xor(mx, 32));
+      const float next = fminf(floorf(-mx * scale), nm), f = fast_exp2(next - nm);
+      l *= f;
 #pragma unroll
-    for (int dt = 0; dt < D / 32; ++dt) acc[dt] *= f;
-    nm = next;
-    sum = fold(s, pf);
+      for (int dt = 0; dt < D / 32; ++dt) acc[dt] *= f;
+      nm = next;
+      sum = fold(s, pf);
+    }
+    l += sum;
   };
   auto add_values = [&](const bf16x8 (&pf)[2], uint32_t place) {
 #pragma unroll
@@ -411,11 +406,10 @@ __global__ __launch_bounds__(kChThreads, D == 128 ? 3 : 4) void chunk_attend_ker
     bring(t + 2 * kChTile, lds + free);
     f32x16 s;
     products(s, place);
-    shape(s, t, place);
+    const int *tp = reinterpret_cast<const int *>(sm + place + 2 * Lds::kTileBytes);
+    shape(s, t, tp);
     bf16x8 pf[2];
-    float sum = fold(s, pf);
-    if (__any(!(sum < kChLimit))) raise(s, sum, pf);
-    l += sum;
+    weigh(s, pf);
     add_values(pf, place);
   };
   bring(t0, lds);
