@@ -136,8 +136,14 @@ def _ptr(t, dtype=None):
     return t.data_ptr()
 
 
+# The current stream's handle without the Stream object around it, which takes longer to make (2.8 us) than a launch.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream):
     if stream is None:
+        if _raw_stream is not None:
+            return _raw_stream(torch.cuda.current_device())
         return torch.cuda.current_stream().cuda_stream
     if isinstance(stream, int):
         return stream
@@ -459,6 +465,7 @@ class Shaping:
         self.t = (slope, first, last)
         self.s = dynts_shaping(softcap, window, _ptr(slope, torch.float32), _ptr(first, torch.int32),
                                _ptr(last, torch.int32))
+        self.ref = C.byref(self.s)
 
 
 def dynts_chunk_scratch_bytes(cfg, n_tokens):
@@ -466,7 +473,7 @@ def dynts_chunk_scratch_bytes(cfg, n_tokens):
 
 
 def _shaping(shaping):
-    return None if shaping is None else C.byref(shaping.s)
+    return None if shaping is None else shaping.ref
 
 
 def dynts_chunk_append(ctx, layer, k_new, v_new, scratch, n_new=None, s_new=None, question=False, stream=None):
@@ -510,20 +517,22 @@ class Rotary:
     def __init__(self, head_dim, freq, axis=None, n_axes=1, pairing=DYNTS_PAIR_HALVES):
         assert axis is None or axis.shape == freq.shape
         self.t = (freq, axis)
+        self.head_dim, self.n_axes = head_dim, n_axes
         self.r = dynts_rotary(head_dim, freq.numel(), pairing, n_axes, _ptr(freq, torch.float32), _ptr(axis, torch.uint8))
+        self.ref = C.byref(self.r)
 
 
 def dynts_rotate(rotary, q, k, positions, q_out, k_out, inverse=False, stream=None):
     """q bf16 [...][q_heads][d], k bf16 [...][k_heads][d] or None, positions int32 [n_axes][...]; q_out may be q, k_out k."""
-    d = rotary.r.head_dim
-    n = positions.numel() // rotary.r.n_axes
-    assert q.shape[-1] == d and q.numel() == n * q.shape[-2] * d and q_out.shape == q.shape, "one position a token"
+    d, n, hk = rotary.head_dim, positions.numel() // rotary.n_axes, 0
+    hq, size = q.shape[-2], q.numel()
+    assert size == n * hq * d and q_out.numel() == size, "one position a token, head_dim elements a head"
     if k is not None:
-        assert k.shape[-1] == d and k.numel() == n * k.shape[-2] * d and k_out.shape == k.shape, "one position a token"
-    _check(lib.dynts_rotate(C.byref(rotary.r), _ptr(q, torch.bfloat16), q.shape[-2], _ptr(k, torch.bfloat16),
-                            k.shape[-2] if k is not None else 0, _ptr(positions, torch.int32), n, 1 if inverse else 0,
-                            _ptr(q_out, torch.bfloat16), _ptr(k_out, torch.bfloat16) if k is not None else None,
-                            _stream(stream)), "dynts_rotate")
+        hk, size = k.shape[-2], k.numel()
+        assert size == n * hk * d and k_out.numel() == size, "one position a token, head_dim elements a head"
+    _check(lib.dynts_rotate(rotary.ref, _ptr(q, torch.bfloat16), hq, _ptr(k, torch.bfloat16), hk,
+                            _ptr(positions, torch.int32), n, 1 if inverse else 0, _ptr(q_out, torch.bfloat16),
+                            _ptr(k_out, torch.bfloat16) if k is not None else None, _stream(stream)), "dynts_rotate")
 
 
 class Cache:

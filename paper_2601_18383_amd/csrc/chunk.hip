@@ -130,12 +130,13 @@ int check_append(const ChunkCache &c, const uint16_t *k_new, const uint16_t *v_n
   return DYNTS_OK;
 }
 
+// copy: false leaves the rows to chunk_attend_kernel
 int launch_append(const ChunkCache &c, const uint16_t *k_new, const uint16_t *v_new, const float *s_new, int n_tokens,
-                  const int32_t *n_new, int question, int32_t *taken, hipStream_t st) {
-  const dynts::ChunkAppendParams p{c, k_new, v_new, c.score_mode == DYNTS_SCORE_EXTERNAL ? s_new : nullptr, n_new, taken, n_tokens, question ? 1 : 0};
+                  const int32_t *n_new, int question, int32_t *taken, bool copy, hipStream_t st) {
+  const dynts::ChunkAppendParams p{c, k_new, v_new, s_new, n_new, taken, n_tokens, question};
   const long long pieces = (long long)n_tokens * c.Hkv * (c.D / 8);
   const dim3 block(dynts::kAppendThreads);
-  if (pieces <= dynts::kAppendSmall) {
+  if (copy && pieces <= dynts::kAppendSmall) {
     if (c.D == 128) hipLaunchKernelGGL((dynts::chunk_reserve_kernel<128, true>), dim3(c.Nb), block, 0, st, p);
     else hipLaunchKernelGGL((dynts::chunk_reserve_kernel<64, true>), dim3(c.Nb), block, 0, st, p);
     return launch_status();
@@ -143,10 +144,10 @@ int launch_append(const ChunkCache &c, const uint16_t *k_new, const uint16_t *v_
   const dim3 grid((unsigned)((pieces + dynts::kAppendThreads - 1) / dynts::kAppendThreads), c.Nb);
   if (c.D == 128) {
     hipLaunchKernelGGL((dynts::chunk_reserve_kernel<128, false>), dim3(c.Nb), block, 0, st, p);
-    hipLaunchKernelGGL((dynts::chunk_copy_kernel<128>), grid, block, 0, st, p);
+    if (copy) hipLaunchKernelGGL((dynts::chunk_copy_kernel<128>), grid, block, 0, st, p);
   } else {
     hipLaunchKernelGGL((dynts::chunk_reserve_kernel<64, false>), dim3(c.Nb), block, 0, st, p);
-    hipLaunchKernelGGL((dynts::chunk_copy_kernel<64>), grid, block, 0, st, p);
+    if (copy) hipLaunchKernelGGL((dynts::chunk_copy_kernel<64>), grid, block, 0, st, p);
   }
   return launch_status();
 }
@@ -162,8 +163,9 @@ unsigned scores_grid(const ChunkCache &c) { return chunk_grid(c, (c.cap + dynts:
 template <int D, bool SHAPED>
 void launch_attend_d(const dynts::ChunkAttendParams &p, const ChunkPlan &pl, unsigned grid, hipStream_t st) {
   if (pl.few) hipLaunchKernelGGL((dynts::chunk_attend_few_kernel<D, SHAPED>), dim3(grid), dim3(dynts::kFewThreads), 0, st, p);
-  else if (SHAPED && p.shape.slope) hipLaunchKernelGGL((dynts::chunk_attend_kernel<D, SHAPED, SHAPED>), dim3(grid), dim3(dynts::kChThreads), 0, st, p);
-  else hipLaunchKernelGGL((dynts::chunk_attend_kernel<D, SHAPED, false>), dim3(grid), dim3(dynts::kChThreads), 0, st, p);
+  else if (SHAPED && p.shape.slope) hipLaunchKernelGGL((dynts::chunk_attend_kernel<D, SHAPED, SHAPED, false>), dim3(grid), dim3(dynts::kChThreads), 0, st, p);
+  else if (!SHAPED && p.k_new) hipLaunchKernelGGL((dynts::chunk_attend_kernel<D, false, false, !SHAPED>), dim3(grid), dim3(dynts::kChThreads), 0, st, p);
+  else hipLaunchKernelGGL((dynts::chunk_attend_kernel<D, SHAPED, false, false>), dim3(grid), dim3(dynts::kChThreads), 0, st, p);
   if (p.n_split > 1) {
     constexpr int rows = dynts::kMergeThreads / (D / 8);
     hipLaunchKernelGGL(dynts::chunk_merge_kernel<D>, dim3((p.T * p.c.G + rows - 1) / rows, p.c.Nb * p.c.Hkv), dim3(dynts::kMergeThreads), 0, st, p,
@@ -171,13 +173,20 @@ void launch_attend_d(const dynts::ChunkAttendParams &p, const ChunkPlan &pl, uns
   }
 }
 
+// rows to append on the way, or none
+struct Fresh {
+  const uint16_t *k_new = nullptr, *v_new = nullptr;
+  const float *s_new = nullptr;
+  int question = 0;
+};
+
 int launch_attend(const ChunkCache &c, const uint16_t *q, int n_tokens, const int32_t *n_new, const dynts_shaping *shaping, uint16_t *out,
-                  float *lse, void *scratch, hipStream_t st) {
+                  float *lse, void *scratch, const Fresh &fresh, hipStream_t st) {
   const ChunkPlan pl = chunk_plan(c, n_tokens, shaping);
   char *const base = static_cast<char *>(scratch);
   const dynts::ChunkAttendParams p{c, q, n_new, out, lse, chunk_shape(shaping, c.scale), n_tokens, c.scale * kLog2E, group_magic(c.G), pl.n_split, pl.Rpad,
                                    reinterpret_cast<float *>(base + pl.off_o), reinterpret_cast<float *>(base + pl.off_ml),
-                                   reinterpret_cast<int32_t *>(base + pl.off_n)};
+                                   reinterpret_cast<int32_t *>(base + pl.off_n), fresh.k_new, fresh.v_new, fresh.s_new, fresh.question};
   const unsigned grid = attend_grid(c, pl);
   if (!grid) return DYNTS_EINVAL;
   if (c.D == 128) {
@@ -226,7 +235,8 @@ int dynts_chunk_append(dynts_ctx *ctx, int32_t layer, const uint16_t *k_new, con
   if (rc == DYNTS_OK) rc = check_append(c, k_new, v_new, s_new, question);
   if (rc == DYNTS_OK) rc = check_scratch(scratch, scratch_bytes, chunk_plan(c, n_tokens).bytes);
   if (rc != DYNTS_OK) return rc;
-  return launch_append(c, k_new, v_new, s_new, n_tokens, n_new, question, static_cast<int32_t *>(scratch), static_cast<hipStream_t>(stream));
+  if (c.score_mode != DYNTS_SCORE_EXTERNAL) s_new = nullptr;
+  return launch_append(c, k_new, v_new, s_new, n_tokens, n_new, question ? 1 : 0, static_cast<int32_t *>(scratch), true, static_cast<hipStream_t>(stream));
 }
 
 int dynts_chunk_attend(dynts_ctx *ctx, int32_t layer, const uint16_t *q, int32_t n_tokens, const int32_t *n_new, const dynts_shaping *shaping,
@@ -240,7 +250,7 @@ int dynts_chunk_attend(dynts_ctx *ctx, int32_t layer, const uint16_t *q, int32_t
   if (misaligned(q, 16) || misaligned(out, 16)) return DYNTS_EINVAL;
   rc = check_scratch(scratch, scratch_bytes, chunk_plan(c, n_tokens).bytes);
   if (rc != DYNTS_OK) return rc;
-  return launch_attend(c, q, n_tokens, n_new, shaping, out, lse, scratch, static_cast<hipStream_t>(stream));
+  return launch_attend(c, q, n_tokens, n_new, shaping, out, lse, scratch, Fresh{}, static_cast<hipStream_t>(stream));
 }
 
 int dynts_chunk_scores(dynts_ctx *ctx, int32_t layer, const uint16_t *q, int32_t n_tokens, const int32_t *n_new, const dynts_shaping *shaping,
@@ -274,8 +284,12 @@ int dynts_chunk_step(dynts_ctx *ctx, int32_t layer, const uint16_t *q, const uin
   const bool scores = c.score_mode == DYNTS_SCORE_ACCUMULATE && !question;
   if (!attend_grid(c, pl) || (scores && !scores_grid(c))) return DYNTS_EINVAL;  // (before the append)
   if (scores && !lse) lse = reinterpret_cast<float *>(static_cast<char *>(scratch) + pl.off_lse);
-  rc = launch_append(c, k_new, v_new, s_new, n_tokens, n_new, question, taken, st);
-  if (rc == DYNTS_OK) rc = launch_attend(c, q, n_tokens, taken, shaping, out, lse, scratch, st);
+  if (c.score_mode != DYNTS_SCORE_EXTERNAL) s_new = nullptr;
+  question = question ? 1 : 0;
+  const bool on_the_way = !pl.few && !shaped(shaping);
+  rc = launch_append(c, k_new, v_new, s_new, n_tokens, n_new, question, taken, !on_the_way, st);
+  if (rc == DYNTS_OK)
+    rc = launch_attend(c, q, n_tokens, taken, shaping, out, lse, scratch, on_the_way ? Fresh{k_new, v_new, s_new, question} : Fresh{}, st);
   if (rc == DYNTS_OK && scores) rc = launch_scores(c, q, n_tokens, taken, shaping, lse, nullptr, 1, st);
   return rc;
 }

@@ -45,6 +45,28 @@ __device__ __forceinline__ void chunk_copy(const ChunkAppendParams &p, int b, in
   }
 }
 
+// The same for tokens [i0, i1) of one head, by `threads` threads.
+template <int D>
+__device__ __forceinline__ void chunk_copy_head(const ChunkCache &c, const uint16_t *k_new, const uint16_t *v_new, const float *s_new, int T, int question,
+                                                int b, int h, int n, int i0, int i1, int pos0, int tid, int threads) {
+  constexpr int LPR = D / 8;
+  const size_t unit = (size_t)b * c.Hkv + h;
+  for (int at = i0 * LPR + tid; at < i1 * LPR; at += threads) {
+    const int piece = at % LPR, i = at / LPR, slot = n + i;
+    const size_t row = ((size_t)b * T + i) * c.Hkv + h, src = row * D + 8 * piece;
+    size_t dst;
+    if (c.block_table) dst = paged_row<D>(c.block_table + unit * c.max_pages, slot, c.max_pages, c.n_pages) + 8 * piece;
+    else dst = (unit * (size_t)c.cap + slot) * D + 8 * piece;
+    store_u32x4(c.K + dst, load_u32x4(k_new + src));
+    store_u32x4(c.V + dst, load_u32x4(v_new + src));
+    if (piece == 0) {
+      const size_t e = unit * (size_t)c.cap + slot;
+      c.S[e] = question ? INFINITY : s_new ? s_new[row] : 0.f;
+      c.pos[e] = pos0 + i;
+    }
+  }
+}
+
 // grid (Nb).  A chunk that does not fit leaves its sequence alone: status bit 0 (no room), 2 (no pages), 3 (a question behind thinking tokens).
 template <int D, bool COPY>
 __global__ __launch_bounds__(kAppendThreads) void chunk_reserve_kernel(const ChunkAppendParams p) {

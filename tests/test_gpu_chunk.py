@@ -98,9 +98,15 @@ SHAPES = [  # Hq, Hkv, d, n_old, n_new
     (32, 8, 128, [1000], [16]),
     (4, 2, 64, [10, 700], [300, 129]),                                  # several row blocks
     (8, 2, 128, [2500, 1], [5, 2]),
-    (8, 1, 128, [3000, 10], [200, 64]),                                 # many rows, keys in shares; a short cache beside it
+    (8, 1, 128, [3000, 10], [200, 64]),                                 # keys in shares; a short cache beside it
     (4, 1, 64, [4000, 900], [300, 1]),
+    (28, 4, 128, [0, 31, 32, 33, 100, 257, 64, 1, 5, 0, 90, 128], [60, 60, 1, 59, 0, 33, 60, 37, 32, 31, 64, 7]),  # many rows of many units
+    (16, 8, 64, [0, 1, 63, 64, 65, 200, 31, 0] * 2, [150, 149, 64, 1, 0, 128, 65, 150] * 2),
+    (8, 2, 128, [8000], [600]),                                         # many rows of few units: keys in shares
+    (8, 2, 64, [3500], [600]),
+    (16, 1, 128, [50, 0, 7] * 4, [70, 65, 8] * 4),                      # the largest group, many rows
 ]
+MANY = SHAPES[10:]
 
 
 @pytest.mark.parametrize("layout", ["dense", "paged"])
@@ -160,7 +166,7 @@ def _shapings(c, gen, kind):
 @pytest.mark.parametrize("layout", ["dense", "paged"])
 @pytest.mark.parametrize("kind", ["cap", "cap_tight", "slope", "window", "window_one", "documents", "prefix", "empty", "future",
                                   "cap_slope_window_documents_prefix", "slope_prefix_empty"])
-@pytest.mark.parametrize("Hq,Hkv,d,n_old,n_new", [SHAPES[0], SHAPES[1], SHAPES[3], SHAPES[6], SHAPES[7], SHAPES[9]])
+@pytest.mark.parametrize("Hq,Hkv,d,n_old,n_new", [SHAPES[0], SHAPES[1], SHAPES[3], SHAPES[6], SHAPES[7], SHAPES[9]] + MANY)
 def test_shaped(B, layout, kind, Hq, Hkv, d, n_old, n_new):
     c = Case(B, layout, Hq, Hkv, d, n_old, n_new, gaps=90, seed=11, qscale=2.0).fill(True)
     s = _shapings(c, c.gen, kind)
@@ -211,7 +217,7 @@ def test_late_and_large_maxima(B):
 # ---- the cache's state -------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("layout", ["dense", "paged"])
-@pytest.mark.parametrize("Hq,Hkv,d,n_old,n_new", [SHAPES[0], SHAPES[1], SHAPES[4], SHAPES[6]])
+@pytest.mark.parametrize("Hq,Hkv,d,n_old,n_new", [SHAPES[0], SHAPES[1], SHAPES[4], SHAPES[6]] + MANY)
 def test_step_is_append_attend_scores(B, layout, Hq, Hkv, d, n_old, n_new):
     """One chunk: rows, positions, lengths and scores in the cache, outputs as the definition has them."""
     c = Case(B, layout, Hq, Hkv, d, n_old, n_new, gaps=20, seed=2).fill(False)
