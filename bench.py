@@ -547,6 +547,73 @@ def run_score_block(args, wl):
                 first_timed_step=0, active_min=wl.batch, active_max=wl.batch)
 
 
+def run_chunk(args, wl):
+    """A chunk of T new tokens of every sequence on a generator-made steady-state cache of layer 0: rotary positions of its
+    queries and keys, then append, attention and score accumulation.  A step is one such chunk; lengths are set back in
+    between."""
+    import torch
+    from paper_2601_18383_amd import binding as B, synth
+
+    dev = torch.device("cuda:0")
+    gen = synth.Synth(wl, dev)
+    T, n0, Nb, d = args.chunk, wl.steady_len + wl.evict_every // 2, wl.batch, wl.head_dim
+    cache = B.Cache(1, Nb, wl.n_q_heads, wl.n_kv_heads, d, max(n0 + T, wl.capacity), wl.budget, wl.window, wl.evict_every,
+                    device=dev)
+    st = gen.steady_state(0, n0)
+    cache.K[0, :, :, :n0] = st["K"]
+    cache.V[0, :, :, :n0] = st["V"]
+    cache.S[0, :, :, :n0] = st["S"]
+    cache.pos[0, :, :, :n0] = torch.arange(n0, device=dev, dtype=torch.int32)
+    cache.n_prompt.fill_(wl.prompt)
+    steps = torch.arange(70000, 70000 + T)
+    q = gen.q(0, steps).permute(1, 0, 2, 3).contiguous()
+    k, v = (x.permute(1, 0, 2, 3).contiguous() for x in gen.kv(0, steps))
+    qr, kr, out = torch.empty_like(q), torch.empty_like(k), torch.zeros_like(q)
+    rotary = B.Rotary(d, (10000.0 ** (-torch.arange(d // 2, device=dev, dtype=torch.float64) / (d // 2))).to(torch.float32))
+    positions = (n0 + torch.arange(T, device=dev, dtype=torch.int32)).expand(1, Nb, T).contiguous()
+    scratch = torch.empty(B.dynts_chunk_scratch_bytes(cache.cfg, T), dtype=torch.uint8, device=dev)
+    parts = [torch.cuda.Event(enable_timing=True) for _ in range(3)]
+
+    def step():
+        cache.seq_len.fill_(n0)
+        cache.next_pos.fill_(n0)
+        B.dynts_rotate(rotary, q, k, positions, qr, kr)
+        B.dynts_chunk_step(cache.ctx, 0, qr, kr, v, out, scratch)
+
+    for _ in range(args.warmup):
+        step()
+    torch.cuda.synchronize()
+    t0 = time.perf_counter()
+    for _ in range(args.steps):
+        step()
+    torch.cuda.synchronize()
+    dt = time.perf_counter() - t0
+    parts[0].record()
+    for _ in range(20):
+        B.dynts_rotate(rotary, q, k, positions, qr, kr)
+    parts[1].record()
+    for _ in range(20):
+        cache.seq_len.fill_(n0)
+        B.dynts_chunk_step(cache.ctx, 0, qr, kr, v, out, scratch)
+    parts[2].record()
+    torch.cuda.synchronize()
+    assert int(cache.status.item()) == 0
+    ms = dt / args.steps * 1e3
+    pairs = Nb * wl.n_q_heads * (T * n0 + T * (T + 1) / 2.0)
+    flops = 6.0 * d * pairs   # logits and outputs, and the logits once more for the scores
+    nbytes = Nb * (wl.n_kv_heads * (4.0 * d * n0 + 12.0 * d * T + 8.0 * (n0 + T)) + 8.0 * wl.n_q_heads * d * T)
+    mfma, hbm = flops / (ms * 1e-3) / 1e12, nbytes / (ms * 1e-3) / 1e9
+    bound = ("mfma", mfma, 2500.0, "TFLOP/s") if mfma / 2500.0 > hbm / 8000.0 else ("hbm", hbm, 8000.0, "GB/s")
+    roofline = {"bound": bound[0], "kernel": "rotate_kernel + chunk_attend_kernel or chunk_attend_few_kernel + chunk_scores_kernel",
+                "achieved": round(bound[1], 1), "peak": bound[2], "unit": bound[3], "frac": round(bound[1] / bound[2], 4),
+                "traffic": None, "algorithmic_flops_per_call": flops, "algorithmic_bytes_per_call": nbytes,
+                "rotate_us": round(parts[0].elapsed_time(parts[1]) / 20 * 1e3, 1),
+                "chunk_step_us": round(parts[1].elapsed_time(parts[2]) / 20 * 1e3, 1)}
+    return dict(value=args.steps / dt, ms_per_step=ms, roofline=roofline, whole_step_gbs=hbm,
+                seq_steps_per_s=args.steps * Nb / dt, evictions_timed=0, first_timed_step=0, active_min=Nb, active_max=Nb,
+                mode="chunks of %d new tokens a sequence on a steady-state cache" % T)
+
+
 def run_predictor(args, wl):
     """The Importance Predictor head with synthetic weights at the size of the workload's model shape
     (28 query heads: 3584 -> 7168 -> 1792 -> 1, else 4096 -> 8192 -> 2048 -> 1), one score per sequence
@@ -654,9 +721,10 @@ def result_line(args, wl, r, cpu):
     """The one JSON object bench.py prints."""
     line = {
         "metric": "predictor calls/sec, 1 MI355X" if getattr(args, "predictor", False) else
+                  "chunk steps/sec (rotate+append+attn+score), 1 MI355X" if getattr(args, "chunk", 0) else
                   "block-scoring calls/sec, 1 MI355X" if getattr(args, "score_block", 0) else
                   "decode steps/sec (attn+score+evict), 1 MI355X", "value": round(r["value"], 2),
-        "unit": "calls/s" if getattr(args, "score_block", 0) or getattr(args, "predictor", False) else "decode steps/s", "n_gpus": 1, "steps": args.steps, "warmup": args.warmup,
+        "unit": "calls/s" if getattr(args, "score_block", 0) or getattr(args, "predictor", False) or getattr(args, "chunk", 0) else "decode steps/s", "n_gpus": 1, "steps": args.steps, "warmup": args.warmup,
         "ms_per_step": round(r["ms_per_step"], 5), "higher_is_better": True, "scaling": "weak",
         "vs_baseline": None, "dtype": "bf16", "data": "synthetic",
         "config": {"workload": "%s: %d layer(s), batch %d, %d q / %d kv heads, head_dim %d, prompt %d, budget %d, "
@@ -698,6 +766,9 @@ def main():
     ap.add_argument("--score-block", type=int, default=0, metavar="T",
                     help="time dynts_score_block for a block of T queries (with their keys) on a steady-state "
                          "cache instead of the decode path")
+    ap.add_argument("--chunk", type=int, default=0, metavar="T",
+                    help="time chunks of T new tokens a sequence (rotary positions, append, attention, scores) on a "
+                         "steady-state cache instead of the decode path")
     ap.add_argument("--paged", action="store_true",
                     help="steady-state run on the paged (block-table) cache layout instead of the dense one")
     ap.add_argument("--predictor", action="store_true",
@@ -734,6 +805,9 @@ def main():
         args.no_cpu_baseline = True
     elif args.score_block:
         r = run_score_block(args, wl)
+        args.no_cpu_baseline = True
+    elif args.chunk:
+        r = run_chunk(args, wl)
         args.no_cpu_baseline = True
     elif args.trajectory:
         r = run_trajectory(args, wl)

@@ -476,9 +476,50 @@ def _shaping(shaping):
     return None if shaping is None else shaping.ref
 
 
+def _on_device(*tensors):
+    """All of them on the current GPU: an address of another one, or of the host, would only be found out by a kernel."""
+    dev = None
+    for t in tensors:
+        if t is None:
+            continue
+        at = t.get_device()
+        if at < 0:
+            raise ValueError("tensors have to be on the GPU")
+        if dev is None:
+            dev = torch.cuda.current_device()
+        if at != dev:
+            raise ValueError("tensors have to be on the current GPU (%d, not %d)" % (dev, at))
+
+
+def _chunk_sizes(q, n_new, shaping, lse=None):
+    """n_new, shaping and lse fit a chunk of queries q [Nb][T][Hq][d]."""
+    Nb, T, Hq, d = q.shape
+    assert n_new is None or n_new.numel() == Nb, "n_new holds one number a sequence"
+    assert lse is None or lse.numel() * d == q.numel(), "lse holds one number a token and query head"
+    if shaping is not None:
+        slope, first, last = shaping.t
+        assert slope is None or slope.numel() == Hq, "slope holds one number a query head"
+        assert first is None or first.numel() == Nb * T, "first holds one position a token"
+        assert last is None or last.numel() == Nb * T, "last holds one position a token"
+        _on_device(q, n_new, lse, slope, first, last)
+    else:
+        _on_device(q, n_new, lse)
+    return T
+
+
+def _chunk_rows(k_new, v_new, s_new):
+    """k_new, v_new [Nb][T][Hkv][d] and s_new [Nb][T][Hkv] are of one chunk."""
+    assert k_new.shape == v_new.shape and k_new.dim() == 4, "k_new and v_new are of one shape"
+    assert s_new is None or s_new.numel() * k_new.shape[3] == k_new.numel(), "s_new holds one number a token and KV head"
+    _on_device(k_new, v_new, s_new)
+
+
 def dynts_chunk_append(ctx, layer, k_new, v_new, scratch, n_new=None, s_new=None, question=False, stream=None):
     """k_new, v_new bf16 [Nb][T][Hkv][d], s_new fp32 [Nb][T][Hkv], n_new int32 [Nb]; scratch: device tensor of at least
     dynts_chunk_scratch_bytes bytes."""
+    _chunk_rows(k_new, v_new, s_new)
+    assert n_new is None or n_new.numel() == k_new.shape[0], "n_new holds one number a sequence"
+    _on_device(n_new, scratch)
     _check(lib.dynts_chunk_append(ctx, layer, _ptr(k_new, torch.bfloat16), _ptr(v_new, torch.bfloat16),
                                   _ptr(s_new, torch.float32), k_new.shape[1], _ptr(n_new, torch.int32),
                                   1 if question else 0, scratch.data_ptr(), scratch.numel() * scratch.element_size(),
@@ -487,7 +528,10 @@ def dynts_chunk_append(ctx, layer, k_new, v_new, scratch, n_new=None, s_new=None
 
 def dynts_chunk_attend(ctx, layer, q, out, scratch, lse=None, n_new=None, shaping=None, stream=None):
     """q, out bf16 [Nb][T][Hq][d], lse fp32 [Nb][T][Hq] or None, shaping: Shaping or None."""
-    _check(lib.dynts_chunk_attend(ctx, layer, _ptr(q, torch.bfloat16), q.shape[1], _ptr(n_new, torch.int32),
+    T = _chunk_sizes(q, n_new, shaping, lse)
+    assert out.numel() == q.numel(), "out has the shape of q"
+    _on_device(out, scratch)
+    _check(lib.dynts_chunk_attend(ctx, layer, _ptr(q, torch.bfloat16), T, _ptr(n_new, torch.int32),
                                   _shaping(shaping), _ptr(out, torch.bfloat16), _ptr(lse, torch.float32),
                                   scratch.data_ptr(), scratch.numel() * scratch.element_size(), _stream(stream)),
            "dynts_chunk_attend")
@@ -495,16 +539,22 @@ def dynts_chunk_attend(ctx, layer, q, out, scratch, lse=None, n_new=None, shapin
 
 def dynts_chunk_scores(ctx, layer, q, lse, dst=None, accumulate=True, n_new=None, shaping=None, stream=None):
     """q and lse as in dynts_chunk_attend; dst fp32 [Nb][Hkv][cap] or None (= the layer's S)."""
-    _check(lib.dynts_chunk_scores(ctx, layer, _ptr(q, torch.bfloat16), q.shape[1], _ptr(n_new, torch.int32),
+    T = _chunk_sizes(q, n_new, shaping, lse)
+    _on_device(dst)
+    _check(lib.dynts_chunk_scores(ctx, layer, _ptr(q, torch.bfloat16), T, _ptr(n_new, torch.int32),
                                   _shaping(shaping), _ptr(lse, torch.float32), _ptr(dst, torch.float32),
                                   1 if accumulate else 0, _stream(stream)), "dynts_chunk_scores")
 
 
 def dynts_chunk_step(ctx, layer, q, k_new, v_new, out, scratch, lse=None, n_new=None, s_new=None, question=False,
                      shaping=None, stream=None):
-    assert q.shape[:2] == k_new.shape[:2] == v_new.shape[:2], "q, k_new and v_new are of one chunk"
+    """dynts_chunk_append, dynts_chunk_attend and dynts_chunk_scores into S in one call; arguments as there."""
+    T = _chunk_sizes(q, n_new, shaping, lse)
+    _chunk_rows(k_new, v_new, s_new)
+    assert q.shape[:2] == k_new.shape[:2] and out.numel() == q.numel(), "q, k_new, v_new and out are of one chunk"
+    _on_device(out, scratch)
     _check(lib.dynts_chunk_step(ctx, layer, _ptr(q, torch.bfloat16), _ptr(k_new, torch.bfloat16),
-                                _ptr(v_new, torch.bfloat16), _ptr(s_new, torch.float32), q.shape[1],
+                                _ptr(v_new, torch.bfloat16), _ptr(s_new, torch.float32), T,
                                 _ptr(n_new, torch.int32), 1 if question else 0, _shaping(shaping),
                                 _ptr(out, torch.bfloat16), _ptr(lse, torch.float32), scratch.data_ptr(),
                                 scratch.numel() * scratch.element_size(), _stream(stream)), "dynts_chunk_step")
@@ -530,6 +580,7 @@ def dynts_rotate(rotary, q, k, positions, q_out, k_out, inverse=False, stream=No
     if k is not None:
         hk, size = k.shape[-2], k.numel()
         assert size == n * hk * d and k_out.numel() == size, "one position a token, head_dim elements a head"
+    _on_device(q, k, positions, q_out, k_out)
     _check(lib.dynts_rotate(rotary.ref, _ptr(q, torch.bfloat16), hq, _ptr(k, torch.bfloat16), hk,
                             _ptr(positions, torch.int32), n, 1 if inverse else 0, _ptr(q_out, torch.bfloat16),
                             _ptr(k_out, torch.bfloat16) if k is not None else None, _stream(stream)), "dynts_rotate")

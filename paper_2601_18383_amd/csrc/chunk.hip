@@ -152,13 +152,15 @@ int launch_append(const ChunkCache &c, const uint16_t *k_new, const uint16_t *v_
   return launch_status();
 }
 
-// workgroups of `blocks` a unit, units rounded up to the 8 XCDs; 0 if a grid cannot hold them (2^32 threads)
-unsigned chunk_grid(const ChunkCache &c, long long blocks) {
+// workgroups of `blocks` a unit, units rounded up to the 8 XCDs; 0 if a grid cannot hold their threads (2^32)
+unsigned chunk_grid(const ChunkCache &c, long long blocks, int threads) {
   const long long wgs = blocks * (((long long)c.Nb * c.Hkv + 7) / 8 * 8);
-  return wgs >= (1LL << 32) / 256 ? 0u : (unsigned)wgs;
+  return wgs >= (1LL << 32) / threads ? 0u : (unsigned)wgs;
 }
-unsigned attend_grid(const ChunkCache &c, const ChunkPlan &pl) { return chunk_grid(c, (long long)pl.blocks * pl.n_split); }
-unsigned scores_grid(const ChunkCache &c) { return chunk_grid(c, (c.cap + dynts::kCsKeys - 1) / dynts::kCsKeys); }
+unsigned attend_grid(const ChunkCache &c, const ChunkPlan &pl) {
+  return chunk_grid(c, (long long)pl.blocks * pl.n_split, pl.few ? dynts::kFewThreads : dynts::kChThreads);
+}
+unsigned scores_grid(const ChunkCache &c) { return chunk_grid(c, (c.cap + dynts::kCsKeys - 1) / dynts::kCsKeys, dynts::kSbWaves * 64); }
 
 template <int D, bool SHAPED>
 void launch_attend_d(const dynts::ChunkAttendParams &p, const ChunkPlan &pl, unsigned grid, hipStream_t st) {

@@ -72,8 +72,9 @@ __device__ __forceinline__ bool chunk_share(const ChunkAttendParams &p, int tile
 constexpr int kChWaves = 4, kChThreads = kChWaves * 64;
 constexpr int kChRows = 32 * kChWaves;  // query rows a workgroup
 constexpr int kChTile = 32;             // slots staged at a time
-constexpr float kChLimit = 1e9f;        // a lane's weights of a tile that sum to this or more raise the shift
+constexpr float kChLimit = 1e18f;       // a lane's weights of a tile that sum to this or more raise the shift
 constexpr int kNowhere = 0x7fffffff;    // a position that no key has
+static_assert(kPageSlots % kChTile == 0, "a tile lies inside a page");
 
 // New tokens of sequence b that are queries, and its length.
 __device__ __forceinline__ int chunk_tokens(const ChunkCache &c, const int32_t *n_new, int T, int b, int &n) {

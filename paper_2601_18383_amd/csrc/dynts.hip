@@ -842,7 +842,7 @@ int chunk_cache(const dynts_ctx *ctx, int32_t layer, ChunkCache *out) {
 
 extern "C" {
 
-int dynts_version(void) { return 100; }
+int dynts_version(void) { return 200; }
 
 const char *dynts_strerror(int code) {
   switch (code) {

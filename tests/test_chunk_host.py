@@ -140,3 +140,32 @@ def test_rotate_refusals(B):
     for kw in (dict(q=odd), dict(qo=odd), dict(k=odd), dict(ko=odd), dict(hq=0), dict(hk=0), dict(hk=-1)):
         assert r(**kw) == B.DYNTS_EINVAL, kw
     assert r(n=0) == B.DYNTS_OK  # nothing to turn: no launch
+
+
+def test_the_binding_refuses_what_does_not_fit(B):
+    """Tensors of the host, sizes that do not belong together: found before the library is called."""
+    import torch
+    ctx = C.c_void_p(0)  # (a call that came through would be answered with an error for it)
+    q = torch.zeros((2, 3, 8, 64), dtype=torch.bfloat16)
+    k = torch.zeros((2, 3, 2, 64), dtype=torch.bfloat16)
+    lse = torch.zeros((2, 3, 8))
+    s = torch.zeros(64, dtype=torch.uint8)
+    n2, n3 = torch.zeros(2, dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
+    pos = torch.zeros((2, 4), dtype=torch.int32)
+    for call in (lambda: B.dynts_chunk_attend(ctx, 0, q, q, s), lambda: B.dynts_chunk_scores(ctx, 0, q, lse),
+                 lambda: B.dynts_chunk_step(ctx, 0, q, k, k, q, s), lambda: B.dynts_chunk_append(ctx, 0, k, k, s),
+                 lambda: B.dynts_rotate(B.Rotary(64, torch.ones(32)), q, k, torch.zeros((1, 2, 3), dtype=torch.int32), q, k)):
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: B.dynts_chunk_attend(ctx, 0, q, q, s, n_new=n3), lambda: B.dynts_chunk_attend(ctx, 0, q, q, s, lse=lse[:1]),
+                 lambda: B.dynts_chunk_attend(ctx, 0, q, q, s, shaping=B.Shaping(first=pos)),
+                 lambda: B.dynts_chunk_attend(ctx, 0, q, q, s, shaping=B.Shaping(last=pos)),
+                 lambda: B.dynts_chunk_scores(ctx, 0, q, lse, shaping=B.Shaping(slope=torch.zeros(7))),
+                 lambda: B.dynts_chunk_append(ctx, 0, k, k[:, :2], s), lambda: B.dynts_chunk_append(ctx, 0, k, q, s),
+                 lambda: B.dynts_rotate(B.Rotary(64, torch.ones(32)), q, k, torch.zeros((1, 2, 4), dtype=torch.int32), q, k),
+                 lambda: B.dynts_rotate(B.Rotary(64, torch.ones(32)), q, k, torch.zeros((1, 2, 3), dtype=torch.int32), q, q),
+                 lambda: B.Rotary(64, torch.ones(32), axis=torch.zeros(31, dtype=torch.uint8)),
+                 lambda: B.Shaping(first=torch.zeros((2, 3))), lambda: B.Shaping(slope=torch.zeros((8, 2))[:, 0])):
+        with pytest.raises(AssertionError):
+            call()
+    assert n2.numel() == 2

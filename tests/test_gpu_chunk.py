@@ -70,6 +70,7 @@ class Case:
     def check(self, what="", lse=None, recv=None, **shape):
         """out (and lse, recv) against the definition; padding untouched."""
         per = {k: shape.pop(k, None) for k in ("first", "last")}
+        scale = shape.pop("scale", 1.0 / math.sqrt(self.d))
         worst = {}
         for b, (a, m) in enumerate(zip(self.n_old, self.n_new)):
             assert torch.all(self.out[b, m:] == 7.0), "padding of sequence %d was written" % b
@@ -78,7 +79,7 @@ class Case:
             if m == 0:
                 continue
             kw = dict(shape, **{k: (v[b] if v is not None else None) for k, v in per.items()})
-            r = plain.attention(self.q[b], self.K[b], self.V[b], self.pos[b], a + m, m, 1.0 / math.sqrt(self.d), **kw)
+            r = plain.attention(self.q[b], self.K[b], self.V[b], self.pos[b], a + m, m, scale, **kw)
             name = "%s[%d]" % (what, b)
             worst["out"] = max(worst.get("out", 0), plain.check(self.out[b, :m], r["out"], r["out_tol"], name + " out"))
             if lse is not None:
@@ -199,6 +200,20 @@ def test_keys_hidden_from_all_may_be_anything(B):
     assert torch.all(dst[:, :, :50] == 0)
     c.K[:, :, :50] = 0
     c.check("hidden", lse=c.lse, recv=dst, first=first)
+
+
+def test_a_scale_of_the_callers(B):
+    c = Case(B, "dense", 8, 2, 64, [100, 3], [20, 40], seed=12)
+    c.cache.close()
+    c.cache = B.Cache(1, 2, 8, 2, 64, c.cap, 0, 0, 1, softmax_scale=0.31)
+    c.fill(True)
+    q = c.q.to(DEV)
+    for shape in (dict(), dict(softcap=4.0), dict(softcap=4.0, window=30)):
+        sh = B.Shaping(**shape) if shape else None
+        dst = torch.zeros((2, 2, c.cap), dtype=torch.float32, device=DEV)
+        B.dynts_chunk_attend(c.cache.ctx, 0, q, c.out, c.scratch, lse=c.lse, n_new=c.n, shaping=sh)
+        B.dynts_chunk_scores(c.cache.ctx, 0, q, c.lse, dst=dst, accumulate=False, n_new=c.n, shaping=sh)
+        c.check("scale", lse=c.lse, recv=dst, scale=0.31, **shape)
 
 
 def test_late_and_large_maxima(B):
@@ -461,3 +476,67 @@ def test_results_do_not_change_from_run_to_run(B):
         got = (c.out.clone(), c.lse.clone(), dst)
         first = first or got
         assert all(torch.equal(x, y) for x, y in zip(first, got))
+
+
+@pytest.mark.parametrize("layout", ["dense", "paged"])
+def test_a_request_from_its_prompt_on(B, layout):
+    """Everything together, as a serving program uses it, over two layers: a prompt in two chunks with rotary positions, single
+    tokens by dynts_decode_step, a trigger, drafted tokens of which some are dropped again by a compaction, a padded chunk with a
+    window and capped logits.  After each chunk its outputs are those of the definition on what the cache then holds."""
+    gen = torch.Generator().manual_seed(21)
+    L, Nb, Hq, Hkv, d = 2, 3, 28, 4, 128
+    budget, window, every = 40, 8, 20
+    cap = 200
+    c = (B.Cache if layout == "dense" else B.PagedCache)(L, Nb, Hq, Hkv, d, cap, budget, window, every)
+    rot = B.Rotary(d, (10000.0 ** (-torch.arange(64, dtype=torch.float64) / 64)).to(torch.float32).to(DEV))
+    scratch = torch.empty(B.dynts_chunk_scratch_bytes(c.cfg, 64), dtype=torch.uint8, device=DEV)
+
+    def fresh(T, layer):
+        q, k, v = (_rand(gen, Nb, T, h, d).to(DEV) for h in (Hq, Hkv, Hkv))
+        at = (c.next_pos[layer][:, None] + torch.arange(T, device=DEV)).to(torch.int32)[None].contiguous()
+        B.dynts_rotate(rot, q, k, at, q, k)
+        return q, k, v
+
+    def chunk(T, layer, n_new=None, question=False, **shape):
+        q, k, v = fresh(T, layer)
+        n0 = c.seq_len[layer].tolist()
+        out = torch.full((Nb, T, Hq, d), 7.0, dtype=torch.bfloat16, device=DEV)
+        lse = torch.full((Nb, T, Hq), 7.0, dtype=torch.float32, device=DEV)
+        n = torch.tensor(n_new, dtype=torch.int32, device=DEV) if n_new else None
+        B.dynts_chunk_step(c.ctx, layer, q, k, v, out, scratch, lse=lse, n_new=n, question=question, shaping=B.Shaping(**shape) if shape else None)
+        K, V, pos = c.K[layer].cpu(), c.V[layer].cpu(), c.pos[layer].cpu()
+        for b in range(Nb):
+            m = n_new[b] if n_new else T
+            end = n0[b] + m
+            assert int(c.seq_len[layer, b]) == end and torch.all(out[b, m:] == 7.0) and torch.all(lse[b, m:] == 7.0)
+            assert torch.equal(K[b, :, n0[b]:end], k[b, :m].transpose(0, 1).cpu()) and torch.equal(V[b, :, n0[b]:end], v[b, :m].transpose(0, 1).cpu())
+            if m:
+                r = plain.attention(q[b].cpu(), K[b], V[b], pos[b], end, m, 1.0 / math.sqrt(d), **shape)
+                plain.check(out[b, :m], r["out"], r["out_tol"], "request out")
+                plain.check(lse[b, :m], r["lse"], r["lse_tol"], "request lse")
+
+    o = torch.zeros((Nb, Hq, d), dtype=torch.float32, device=DEV)
+    for layer in range(L):
+        chunk(33, layer, question=True)
+        chunk(12, layer, n_new=[12, 5, 0], question=True)
+    for _ in range(budget + window + every):
+        for layer in range(L):
+            q, k, v = (x[:, 0].contiguous() for x in fresh(1, layer))
+            B.dynts_decode_step(c.ctx, layer, q, k, v, o)
+    for layer in range(L):
+        B.dynts_select_evict(c.ctx, layer, c.keep_idx, c.new_len)
+        B.dynts_compact(c.ctx, layer, c.keep_idx, c.new_len)
+        chunk(6, layer)                                     # drafted
+        kept = (c.seq_len[layer] - 4).to(torch.int32)       # four of them are not accepted
+        c.keep_idx.copy_(torch.arange(cap, device=DEV, dtype=torch.int32).expand_as(c.keep_idx))
+        B.dynts_compact(c.ctx, layer, c.keep_idx, kept)
+        c.next_pos[layer] -= 4
+        chunk(17, layer, n_new=[0, 17, 9], window=30, softcap=8.0)
+        q, k, v = (x[:, 0].contiguous() for x in fresh(1, layer))
+        B.dynts_decode_step(c.ctx, layer, q, k, v, o)
+        B.dynts_update_scores(c.ctx, layer)
+        assert torch.isfinite(o).all()
+    assert int(c.status.item()) == 0
+    if layout == "paged":
+        used, taken = c.pages_in_use()
+        assert used == taken
