@@ -136,14 +136,16 @@ def _ptr(t, dtype=None):
     return t.data_ptr()
 
 
-# The current stream's handle without the Stream object around it, which takes longer to make (2.8 us) than a launch.
+# The current stream's handle without the Stream object around it, which takes longer to make (2.8 us) than a launch; the current
+# device without a check that there is one (tensors of it have been made).
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _stream(stream):
     if stream is None:
         if _raw_stream is not None:
-            return _raw_stream(torch.cuda.current_device())
+            return _raw_stream(_device())
         return torch.cuda.current_stream().cuda_stream
     if isinstance(stream, int):
         return stream
@@ -462,7 +464,9 @@ class Shaping:
     slope fp32 [Hq]; first, last int32 [Nb][T], the T of the chunk it is used with."""
 
     def __init__(self, softcap=0.0, window=0, slope=None, first=None, last=None):
-        self.t = (slope, first, last)
+        self.t = [t for t in (slope, first, last) if t is not None]
+        self.heads = None if slope is None else slope.numel()
+        self.tokens = {t.numel() for t in (first, last) if t is not None}
         self.s = dynts_shaping(softcap, window, _ptr(slope, torch.float32), _ptr(first, torch.int32),
                                _ptr(last, torch.int32))
         self.ref = C.byref(self.s)
@@ -486,51 +490,49 @@ def _on_device(*tensors):
         if at < 0:
             raise ValueError("tensors have to be on the GPU")
         if dev is None:
-            dev = torch.cuda.current_device()
+            dev = _device()
         if at != dev:
             raise ValueError("tensors have to be on the current GPU (%d, not %d)" % (dev, at))
 
 
-def _chunk_sizes(q, n_new, shaping, lse=None):
-    """n_new, shaping and lse fit a chunk of queries q [Nb][T][Hq][d]."""
+def _chunk_sizes(q, n_new, shaping, lse, *others):
+    """n_new, shaping and lse fit a chunk of queries q [Nb][T][Hq][d], and all lie on the current GPU, `others` too."""
     Nb, T, Hq, d = q.shape
     assert n_new is None or n_new.numel() == Nb, "n_new holds one number a sequence"
-    assert lse is None or lse.numel() * d == q.numel(), "lse holds one number a token and query head"
-    if shaping is not None:
-        slope, first, last = shaping.t
-        assert slope is None or slope.numel() == Hq, "slope holds one number a query head"
-        assert first is None or first.numel() == Nb * T, "first holds one position a token"
-        assert last is None or last.numel() == Nb * T, "last holds one position a token"
-        _on_device(q, n_new, lse, slope, first, last)
+    assert lse is None or lse.numel() == Nb * T * Hq, "lse holds one number a token and query head"
+    if shaping is None:
+        _on_device(q, n_new, lse, *others)
     else:
-        _on_device(q, n_new, lse)
+        assert shaping.heads is None or shaping.heads == Hq, "slope holds one number a query head"
+        assert not shaping.tokens or shaping.tokens == {Nb * T}, "first and last hold one position a token"
+        _on_device(q, n_new, lse, *others, *shaping.t)
     return T
 
 
 def _chunk_rows(k_new, v_new, s_new):
     """k_new, v_new [Nb][T][Hkv][d] and s_new [Nb][T][Hkv] are of one chunk."""
-    assert k_new.shape == v_new.shape and k_new.dim() == 4, "k_new and v_new are of one shape"
-    assert s_new is None or s_new.numel() * k_new.shape[3] == k_new.numel(), "s_new holds one number a token and KV head"
-    _on_device(k_new, v_new, s_new)
+    Nb, T, Hkv, d = k_new.shape
+    assert v_new.numel() == Nb * T * Hkv * d, "k_new and v_new are of one shape"
+    assert s_new is None or s_new.numel() == Nb * T * Hkv, "s_new holds one number a token and KV head"
+    return Nb, T
 
 
 def dynts_chunk_append(ctx, layer, k_new, v_new, scratch, n_new=None, s_new=None, question=False, stream=None):
     """k_new, v_new bf16 [Nb][T][Hkv][d], s_new fp32 [Nb][T][Hkv], n_new int32 [Nb]; scratch: device tensor of at least
     dynts_chunk_scratch_bytes bytes."""
-    _chunk_rows(k_new, v_new, s_new)
-    assert n_new is None or n_new.numel() == k_new.shape[0], "n_new holds one number a sequence"
-    _on_device(n_new, scratch)
+    Nb, T = _chunk_rows(k_new, v_new, s_new)
+    assert n_new is None or n_new.numel() == Nb, "n_new holds one number a sequence"
+    _on_device(k_new, v_new, s_new, n_new, scratch)
     _check(lib.dynts_chunk_append(ctx, layer, _ptr(k_new, torch.bfloat16), _ptr(v_new, torch.bfloat16),
-                                  _ptr(s_new, torch.float32), k_new.shape[1], _ptr(n_new, torch.int32),
+                                  _ptr(s_new, torch.float32), T, _ptr(n_new, torch.int32),
                                   1 if question else 0, scratch.data_ptr(), scratch.numel() * scratch.element_size(),
                                   _stream(stream)), "dynts_chunk_append")
 
 
 def dynts_chunk_attend(ctx, layer, q, out, scratch, lse=None, n_new=None, shaping=None, stream=None):
     """q, out bf16 [Nb][T][Hq][d], lse fp32 [Nb][T][Hq] or None, shaping: Shaping or None."""
-    T = _chunk_sizes(q, n_new, shaping, lse)
+    T = _chunk_sizes(q, n_new, shaping, lse, out, scratch)
     assert out.numel() == q.numel(), "out has the shape of q"
-    _on_device(out, scratch)
     _check(lib.dynts_chunk_attend(ctx, layer, _ptr(q, torch.bfloat16), T, _ptr(n_new, torch.int32),
                                   _shaping(shaping), _ptr(out, torch.bfloat16), _ptr(lse, torch.float32),
                                   scratch.data_ptr(), scratch.numel() * scratch.element_size(), _stream(stream)),
@@ -539,8 +541,7 @@ def dynts_chunk_attend(ctx, layer, q, out, scratch, lse=None, n_new=None, shapin
 
 def dynts_chunk_scores(ctx, layer, q, lse, dst=None, accumulate=True, n_new=None, shaping=None, stream=None):
     """q and lse as in dynts_chunk_attend; dst fp32 [Nb][Hkv][cap] or None (= the layer's S)."""
-    T = _chunk_sizes(q, n_new, shaping, lse)
-    _on_device(dst)
+    T = _chunk_sizes(q, n_new, shaping, lse, dst)
     _check(lib.dynts_chunk_scores(ctx, layer, _ptr(q, torch.bfloat16), T, _ptr(n_new, torch.int32),
                                   _shaping(shaping), _ptr(lse, torch.float32), _ptr(dst, torch.float32),
                                   1 if accumulate else 0, _stream(stream)), "dynts_chunk_scores")
@@ -549,10 +550,8 @@ def dynts_chunk_scores(ctx, layer, q, lse, dst=None, accumulate=True, n_new=None
 def dynts_chunk_step(ctx, layer, q, k_new, v_new, out, scratch, lse=None, n_new=None, s_new=None, question=False,
                      shaping=None, stream=None):
     """dynts_chunk_append, dynts_chunk_attend and dynts_chunk_scores into S in one call; arguments as there."""
-    T = _chunk_sizes(q, n_new, shaping, lse)
-    _chunk_rows(k_new, v_new, s_new)
-    assert q.shape[:2] == k_new.shape[:2] and out.numel() == q.numel(), "q, k_new, v_new and out are of one chunk"
-    _on_device(out, scratch)
+    T = _chunk_sizes(q, n_new, shaping, lse, k_new, v_new, s_new, out, scratch)
+    assert _chunk_rows(k_new, v_new, s_new) == (q.shape[0], T) and out.numel() == q.numel(), "q, k_new, v_new and out are of one chunk"
     _check(lib.dynts_chunk_step(ctx, layer, _ptr(q, torch.bfloat16), _ptr(k_new, torch.bfloat16),
                                 _ptr(v_new, torch.bfloat16), _ptr(s_new, torch.float32), T,
                                 _ptr(n_new, torch.int32), 1 if question else 0, _shaping(shaping),

@@ -46,7 +46,8 @@ constexpr long long kMostPartials = 65536;
 //     256 18.6 / 15.8
 // Shares, at least 512 slots each, until the chip is full.  us by their number:
 //   few rows, head_dim 128: 8 units of 1000 slots 1 / 2 / 4: 10.6 / 10.5 / 10.6, of 4500 1 / 4 / 8 / 16: 31.0 / 14.0 / 11.5 / 11.0, of 16000 8 / 16 / 32: 21.1 /
-//     19.3 / 22.1; 128 units of 1000 1 / 2: 14.4 / 15.7, of 4500 51.6 / 48.1; head_dim 64, 128 units of 6000 1 / 2: 30.5 / 33.2, 10 of 1500 9.4 / 10.5
+//     19.3 / 22.1; 128 units of 1200 1 / 2: 16.8 / 19.0, of 2464 27.0 / 30.2, of 4000 39.9 / 44.6; head_dim 64, 128 units of 6000 1 / 2: 30.5 / 33.2, 10 of 1500
+//     9.4 / 10.5
 //   many rows, W = 64, 4500 slots 1 / 4 / 8 / 16: 114 / 44.6 / 39.2 / 50.1; W = 128 of 1000 1 / 2 / 4: 30.7 / 27.1 / 30.1; W = 256 of 4500 1 / 2 / 4: 123 /
 //     106 / 119, of 1000 34.6 / 37.4 / 49.0; W = 16 of 16000 8 / 16 / 32: 58.3 / 39.5 / 38.4
 ChunkPlan chunk_plan(const dynts_config &c, int n_tokens, int slots) {
@@ -60,9 +61,9 @@ ChunkPlan chunk_plan(const dynts_config &c, int n_tokens, int slots) {
   pl.Rpad = pl.blocks * pl.rows;
   long long shares = slots / (32 * dynts::kShareTiles);
   if (pl.few) {
-    if (slots < 1536 || (!wide_head && F > 64)) shares = 1;
     shares = shares < 16 ? shares : 16;
     shares = shares < 256 / F ? shares : 256 / F;
+    if (slots < 1536 || shares < 3) shares = 1;
   } else {
     shares = shares < 32 ? shares : 32;
     shares = shares < 512 / W ? shares : 512 / W;
@@ -208,12 +209,15 @@ int launch_scores(const ChunkCache &c, const uint16_t *q, int n_tokens, const in
   const unsigned grid = scores_grid(c);
   if (!grid) return DYNTS_EINVAL;
   const dim3 block(dynts::kSbWaves * 64);
+  const bool positions = shaped(shaping), biased = positions && shaping->slope;
   if (c.D == 128) {
-    if (shaped(shaping)) hipLaunchKernelGGL((dynts::chunk_scores_kernel<128, true>), dim3(grid), block, 0, st, p);
-    else hipLaunchKernelGGL((dynts::chunk_scores_kernel<128, false>), dim3(grid), block, 0, st, p);
+    if (biased) hipLaunchKernelGGL((dynts::chunk_scores_kernel<128, true, true>), dim3(grid), block, 0, st, p);
+    else if (positions) hipLaunchKernelGGL((dynts::chunk_scores_kernel<128, true, false>), dim3(grid), block, 0, st, p);
+    else hipLaunchKernelGGL((dynts::chunk_scores_kernel<128, false, false>), dim3(grid), block, 0, st, p);
   } else {
-    if (shaped(shaping)) hipLaunchKernelGGL((dynts::chunk_scores_kernel<64, true>), dim3(grid), block, 0, st, p);
-    else hipLaunchKernelGGL((dynts::chunk_scores_kernel<64, false>), dim3(grid), block, 0, st, p);
+    if (biased) hipLaunchKernelGGL((dynts::chunk_scores_kernel<64, true, true>), dim3(grid), block, 0, st, p);
+    else if (positions) hipLaunchKernelGGL((dynts::chunk_scores_kernel<64, true, false>), dim3(grid), block, 0, st, p);
+    else hipLaunchKernelGGL((dynts::chunk_scores_kernel<64, false, false>), dim3(grid), block, 0, st, p);
   }
   return launch_status();
 }

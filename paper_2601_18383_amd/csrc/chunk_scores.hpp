@@ -33,23 +33,25 @@ constexpr int kCsGroup = kSbLRows, kCsPer = kCsGroup / kSbChunk;  // rows looked
 constexpr int kCsStage = 2;              // chunks staged at a time, one barrier for all
 
 // of a group's rows: minus their L, and what they see: the last slot, or shaped the lowest position, the distance to the highest, their own, their slope
-template <bool SHAPED>
+template <bool SHAPED, bool BIASED>
 struct ChunkRows {
   float minus_l[kCsGroup];
   int lo[kCsGroup];
   uint32_t span[SHAPED ? kCsGroup : 1];
-  float at[SHAPED ? kCsGroup : 1], slope[SHAPED ? kCsGroup : 1];
+  int own[BIASED ? kCsGroup : 1];
+  float slope[BIASED ? kCsGroup : 1];
   // by chunk, shaped: what all of its rows see, what any does
   int all_lo[kCsPer], all_hi[kCsPer], any_lo[kCsPer], any_hi[kCsPer];
 };
 
 // 1-D grid of ceil(cap / 256) * round_up(units, 8) workgroups, 256 threads.
-template <int D, bool SHAPED>
-__global__ __launch_bounds__(kSbWaves * 64, D == 128 ? 3 : 4) void chunk_scores_kernel(const ChunkScoreParams p) {
+// SHAPED, BIASED as in chunk_attend_kernel.
+template <int D, bool SHAPED, bool BIASED>
+__global__ __launch_bounds__(kSbWaves * 64, D == 128 || SHAPED ? 3 : 4) void chunk_scores_kernel(const ChunkScoreParams p) {
   using St = SbStage<D>;
   const ChunkCache &c = p.c;
   __shared__ __attribute__((aligned(16))) char sm_q[2][kCsStage * St::kBufBytes];
-  __shared__ __attribute__((aligned(16))) ChunkRows<SHAPED> sm_rows[2];
+  __shared__ __attribute__((aligned(16))) ChunkRows<SHAPED, BIASED> sm_rows[2];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, hf = lane >> 5;
   int unit, blk;
   if (!sb_map((c.cap + kCsKeys - 1) / kCsKeys, c.Nb * c.Hkv, unit, blk)) return;
@@ -63,11 +65,10 @@ __global__ __launch_bounds__(kSbWaves * 64, D == 128 ? 3 : 4) void chunk_scores_
   const int R = m * c.G, base = n - m;
   const int key0 = blk * kCsKeys + wave * kSbRowsPerWave;
   const int32_t *pos = c.pos + (size_t)unit * c.cap;
-  const int ref = SHAPED ? __builtin_amdgcn_readfirstlane(pos[base]) : 0;
 
   bf16x8 kf[kSbTiles][D / 16];
   int kpos[kSbTiles];  // of the lane's keys: slot, or shaped position
-  float kat[kSbTiles], sum[kSbTiles];
+  float sum[kSbTiles];
 #pragma unroll
   for (int kt = 0; kt < kSbTiles; ++kt) {
     int slot = key0 + 32 * kt + col;
@@ -76,7 +77,6 @@ __global__ __launch_bounds__(kSbWaves * 64, D == 128 ? 3 : 4) void chunk_scores_
                                      : ((size_t)unit * c.cap + slot) * D;
     load_row_frags<D>(kf[kt], reinterpret_cast<const char *>(c.K + row), hf);
     kpos[kt] = SHAPED ? pos[slot] : slot;
-    kat[kt] = SHAPED ? (float)(kpos[kt] - ref) : 0.f;
     sum[kt] = 0.f;
   }
   const bool has_keys = key0 < n && key0 + kSbRowsPerWave > skip;  // else: staging and barriers only
@@ -121,7 +121,7 @@ __global__ __launch_bounds__(kSbWaves * 64, D == 128 ? 3 : 4) void chunk_scores_
     }
   };
   auto put_rows = [&](int buf) {
-    ChunkRows<SHAPED> &rows = sm_rows[buf];
+    ChunkRows<SHAPED, BIASED> &rows = sm_rows[buf];
     const bool real = row_r < R;
     const int r = real ? row_r : R - 1, i = chunk_token(r, p.g_magic);
     // (a row without a key it sees has no weights: its comparisons say so.  Rows behind the last see nothing)
@@ -136,8 +136,10 @@ __global__ __launch_bounds__(kSbWaves * 64, D == 128 ? 3 : 4) void chunk_scores_
       }
       rows.lo[tid] = lo;
       rows.span[tid] = span;
-      rows.at[tid] = (float)(row_own - ref);
-      rows.slope[tid] = p.shape.slope ? p.shape.slope[h * c.G + (r - i * c.G)] * 1.4426950408889634f : 0.f;
+      if (BIASED) {
+        rows.own[tid] = row_own;
+        rows.slope[tid] = p.shape.slope[h * c.G + (r - i * c.G)] * 1.4426950408889634f;
+      }
       const int hi = lo == kNowhere ? -1 : (int)(lo + span);
       int all_lo = lo, all_hi = hi, any_lo = lo, any_hi = hi;
 #pragma unroll
@@ -170,7 +172,7 @@ __global__ __launch_bounds__(kSbWaves * 64, D == 128 ? 3 : 4) void chunk_scores_
     if (first + kCsStage < chunks) fetch(first + kCsStage);
   }
   // a chunk whose rows are in `q`, and what is known of them from row r0 of `rows` on
-  auto chunk = [&](int ch, const char *q, const ChunkRows<SHAPED> &rows) {
+  auto chunk = [&](int ch, const char *q, const ChunkRows<SHAPED, BIASED> &rows) {
     const int in_group = (ch - first) % kCsPer;
     const int r0 = in_group * kSbChunk;
     bool any = has_keys, all;
@@ -189,28 +191,22 @@ __global__ __launch_bounds__(kSbWaves * 64, D == 128 ? 3 : 4) void chunk_scores_
 #pragma unroll
       for (int j = 0; j < 4; ++j) ml[j] = *reinterpret_cast<const f32x4 *>(&rows.minus_l[r0 + 8 * j + 4 * hf]);
       float scale = p.scale_log2;
-      if (SHAPED && (p.shape.cap > 0.f || p.shape.slope)) {
+      if (SHAPED && p.shape.cap > 0.f) {
         scale = 1.f;
-        if (p.shape.cap > 0.f) {
 #pragma unroll
-          for (int kt = 0; kt < kSbTiles; ++kt)
+        for (int kt = 0; kt < kSbTiles; ++kt)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) acc[kt][e] = soft_cap(acc[kt][e], p.shape);
-        } else {
+          for (int e = 0; e < 16; ++e) acc[kt][e] = soft_cap(acc[kt][e], p.shape);
+      }
+      if (BIASED) {
 #pragma unroll
-          for (int kt = 0; kt < kSbTiles; ++kt)
+        for (int e = 0; e < 16; ++e) {
+          const int r = r0 + 8 * (e >> 2) + 4 * hf + (e & 3), own = rows.own[BIASED ? r : 0];
+          const float slope = rows.slope[BIASED ? r : 0];
 #pragma unroll
-            for (int e = 0; e < 16; ++e) acc[kt][e] *= p.scale_log2;
+          for (int kt = 0; kt < kSbTiles; ++kt) acc[kt][e] = fmaf(-slope, fabsf((float)(own - kpos[kt])), acc[kt][e] * scale);
         }
-        if (p.shape.slope) {
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const int r = r0 + 8 * (e >> 2) + 4 * hf + (e & 3);
-            const float at = rows.at[r], slope = rows.slope[r];
-#pragma unroll
-            for (int kt = 0; kt < kSbTiles; ++kt) acc[kt][e] = fmaf(-slope, fabsf(at - kat[kt]), acc[kt][e]);
-          }
-        }
+        scale = 1.f;
       }
       if (!__builtin_amdgcn_readfirstlane((int)all)) {
         asm volatile("; some keys are hidden");  // (a branch: the compiler would compare every key of every chunk)
