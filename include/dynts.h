@@ -323,7 +323,7 @@ int dynts_predict_scores(const dynts_predictor *w, const uint16_t *h, int32_t ba
  *   scratch: >= dynts_chunk_scratch_bytes(cfg, n_tokens) bytes of device memory, 256-byte aligned, contents irrelevant
  *     before and after (what serves a chunk serves every smaller one; it may be shared by calls that are
  *     stream-ordered with respect to each other).
- * Outputs are bf16, as what a projection reads next; the weights are rounded to bf16 for their product with V, sums,
+ * Arrays that are written overlap no other argument.  Outputs are bf16, as what a projection reads next; the weights are rounded to bf16 for their product with V, sums,
  * products and statistics are fp32. */
 
 /* What is done to the logits of a chunk, in this order (s the scaled product of a query at position p and a key at
@@ -387,7 +387,7 @@ int dynts_chunk_step(dynts_ctx *ctx, int32_t layer, const uint16_t *q, const uin
  * taken off in 64 bits, one rounding to bf16 at the end.
  *   q bf16 [n_tokens][q_heads][head_dim], k bf16 [n_tokens][k_heads][head_dim] or NULL; q_out, k_out of the same shapes, the same
  *   arrays or others (that do not overlap).  positions int32 [n_axes][n_tokens].
- * head_dim a multiple of 8, n_pairs a multiple of 8, at most 128 and head_dim / 2.  An axis[p] past the last one counts as that one. */
+ * n_tokens below 2^24, head_dim a multiple of 8, n_pairs a multiple of 8, at most 128 and head_dim / 2.  An axis[p] past the last one counts as that one. */
 #define DYNTS_PAIR_HALVES 0   /* pair p: elements p and n_pairs + p */
 #define DYNTS_PAIR_ADJACENT 1 /* pair p: elements 2 p and 2 p + 1 */
 typedef struct dynts_rotary {

@@ -208,6 +208,7 @@ def dynts_bind_paged(ctx, K_pool, V_pool, block_table, free_stack, free_top, S, 
                                 _ptr(seq_len, torch.int32), _ptr(next_pos, torch.int32), _ptr(n_prompt, torch.int32),
                                 _ptr(workspace), workspace.numel() * workspace.element_size(),
                                 _ptr(status, torch.int32)), "dynts_bind_paged")
+    ctx.gpu = K_pool.get_device()
 
 
 def dynts_prefill(ctx, layer, K0, V0, m, stream=None):
@@ -480,8 +481,9 @@ def _shaping(shaping):
     return None if shaping is None else shaping.ref
 
 
-def _on_device(*tensors):
-    """All of them on the current GPU: an address of another one, or of the host, would only be found out by a kernel."""
+def _on_device(ctx, *tensors):
+    """All of them on the current GPU, and the arrays bound to ctx: an address of another one, or of the host, would only be found out
+    by a kernel."""
     dev = None
     for t in tensors:
         if t is None:
@@ -493,19 +495,22 @@ def _on_device(*tensors):
             dev = _device()
         if at != dev:
             raise ValueError("tensors have to be on the current GPU (%d, not %d)" % (dev, at))
+    bound = getattr(ctx, "gpu", dev)
+    if bound != dev:
+        raise ValueError("the cache lies on GPU %d, the current one is %d" % (bound, dev))
 
 
-def _chunk_sizes(q, n_new, shaping, lse, *others):
+def _chunk_sizes(ctx, q, n_new, shaping, lse, *others):
     """n_new, shaping and lse fit a chunk of queries q [Nb][T][Hq][d], and all lie on the current GPU, `others` too."""
     Nb, T, Hq, d = q.shape
     assert n_new is None or n_new.numel() == Nb, "n_new holds one number a sequence"
     assert lse is None or lse.numel() == Nb * T * Hq, "lse holds one number a token and query head"
     if shaping is None:
-        _on_device(q, n_new, lse, *others)
+        _on_device(ctx, q, n_new, lse, *others)
     else:
         assert shaping.heads is None or shaping.heads == Hq, "slope holds one number a query head"
         assert not shaping.tokens or shaping.tokens == {Nb * T}, "first and last hold one position a token"
-        _on_device(q, n_new, lse, *others, *shaping.t)
+        _on_device(ctx, q, n_new, lse, *others, *shaping.t)
     return T
 
 
@@ -522,7 +527,7 @@ def dynts_chunk_append(ctx, layer, k_new, v_new, scratch, n_new=None, s_new=None
     dynts_chunk_scratch_bytes bytes."""
     Nb, T = _chunk_rows(k_new, v_new, s_new)
     assert n_new is None or n_new.numel() == Nb, "n_new holds one number a sequence"
-    _on_device(k_new, v_new, s_new, n_new, scratch)
+    _on_device(ctx, k_new, v_new, s_new, n_new, scratch)
     _check(lib.dynts_chunk_append(ctx, layer, _ptr(k_new, torch.bfloat16), _ptr(v_new, torch.bfloat16),
                                   _ptr(s_new, torch.float32), T, _ptr(n_new, torch.int32),
                                   1 if question else 0, scratch.data_ptr(), scratch.numel() * scratch.element_size(),
@@ -531,7 +536,7 @@ def dynts_chunk_append(ctx, layer, k_new, v_new, scratch, n_new=None, s_new=None
 
 def dynts_chunk_attend(ctx, layer, q, out, scratch, lse=None, n_new=None, shaping=None, stream=None):
     """q, out bf16 [Nb][T][Hq][d], lse fp32 [Nb][T][Hq] or None, shaping: Shaping or None."""
-    T = _chunk_sizes(q, n_new, shaping, lse, out, scratch)
+    T = _chunk_sizes(ctx, q, n_new, shaping, lse, out, scratch)
     assert out.numel() == q.numel(), "out has the shape of q"
     _check(lib.dynts_chunk_attend(ctx, layer, _ptr(q, torch.bfloat16), T, _ptr(n_new, torch.int32),
                                   _shaping(shaping), _ptr(out, torch.bfloat16), _ptr(lse, torch.float32),
@@ -541,7 +546,7 @@ def dynts_chunk_attend(ctx, layer, q, out, scratch, lse=None, n_new=None, shapin
 
 def dynts_chunk_scores(ctx, layer, q, lse, dst=None, accumulate=True, n_new=None, shaping=None, stream=None):
     """q and lse as in dynts_chunk_attend; dst fp32 [Nb][Hkv][cap] or None (= the layer's S)."""
-    T = _chunk_sizes(q, n_new, shaping, lse, dst)
+    T = _chunk_sizes(ctx, q, n_new, shaping, lse, dst)
     _check(lib.dynts_chunk_scores(ctx, layer, _ptr(q, torch.bfloat16), T, _ptr(n_new, torch.int32),
                                   _shaping(shaping), _ptr(lse, torch.float32), _ptr(dst, torch.float32),
                                   1 if accumulate else 0, _stream(stream)), "dynts_chunk_scores")
@@ -550,7 +555,7 @@ def dynts_chunk_scores(ctx, layer, q, lse, dst=None, accumulate=True, n_new=None
 def dynts_chunk_step(ctx, layer, q, k_new, v_new, out, scratch, lse=None, n_new=None, s_new=None, question=False,
                      shaping=None, stream=None):
     """dynts_chunk_append, dynts_chunk_attend and dynts_chunk_scores into S in one call; arguments as there."""
-    T = _chunk_sizes(q, n_new, shaping, lse, k_new, v_new, s_new, out, scratch)
+    T = _chunk_sizes(ctx, q, n_new, shaping, lse, k_new, v_new, s_new, out, scratch)
     assert _chunk_rows(k_new, v_new, s_new) == (q.shape[0], T) and out.numel() == q.numel(), "q, k_new, v_new and out are of one chunk"
     _check(lib.dynts_chunk_step(ctx, layer, _ptr(q, torch.bfloat16), _ptr(k_new, torch.bfloat16),
                                 _ptr(v_new, torch.bfloat16), _ptr(s_new, torch.float32), T,
@@ -579,7 +584,7 @@ def dynts_rotate(rotary, q, k, positions, q_out, k_out, inverse=False, stream=No
     if k is not None:
         hk, size = k.shape[-2], k.numel()
         assert size == n * hk * d and k_out.numel() == size, "one position a token, head_dim elements a head"
-    _on_device(q, k, positions, q_out, k_out)
+    _on_device(None, q, k, positions, q_out, k_out)
     _check(lib.dynts_rotate(rotary.ref, _ptr(q, torch.bfloat16), hq, _ptr(k, torch.bfloat16), hk,
                             _ptr(positions, torch.int32), n, 1 if inverse else 0, _ptr(q_out, torch.bfloat16),
                             _ptr(k_out, torch.bfloat16) if k is not None else None, _stream(stream)), "dynts_rotate")

@@ -19,6 +19,10 @@ constexpr float kLog2E = 1.4426950408889634f;
 
 size_t align_up(size_t v) { return (v + kAlign - 1) / kAlign * kAlign; }
 bool misaligned(const void *p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to != 0; }
+bool overlap(const void *a, size_t a_bytes, const void *b, size_t b_bytes) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + b_bytes && y < x + a_bytes;
+}
 int launch_status() { return hipGetLastError() == hipSuccess ? DYNTS_OK : DYNTS_EHIP; }
 
 // scratch of a chunk's calls
@@ -256,6 +260,8 @@ int dynts_chunk_attend(dynts_ctx *ctx, int32_t layer, const uint16_t *q, int32_t
   if (misaligned(q, 16) || misaligned(out, 16)) return DYNTS_EINVAL;
   rc = check_scratch(scratch, scratch_bytes, chunk_plan(c, n_tokens).bytes);
   if (rc != DYNTS_OK) return rc;
+  const size_t q_bytes = (size_t)c.Nb * n_tokens * c.Hq * c.D * 2;
+  if (overlap(out, q_bytes, q, q_bytes)) return DYNTS_EINVAL;
   return launch_attend(c, q, n_tokens, n_new, shaping, out, lse, scratch, Fresh{}, static_cast<hipStream_t>(stream));
 }
 
@@ -289,6 +295,8 @@ int dynts_chunk_step(dynts_ctx *ctx, int32_t layer, const uint16_t *q, const uin
   int32_t *taken = static_cast<int32_t *>(scratch);
   const bool scores = c.score_mode == DYNTS_SCORE_ACCUMULATE && !question;
   if (!attend_grid(c, pl) || (scores && !scores_grid(c))) return DYNTS_EINVAL;  // (before the append)
+  const size_t row = (size_t)c.Nb * n_tokens * c.D * 2, q_bytes = row * c.Hq, k_bytes = row * c.Hkv;
+  if (overlap(out, q_bytes, q, q_bytes) || overlap(out, q_bytes, k_new, k_bytes) || overlap(out, q_bytes, v_new, k_bytes)) return DYNTS_EINVAL;
   if (scores && !lse) lse = reinterpret_cast<float *>(static_cast<char *>(scratch) + pl.off_lse);
   if (c.score_mode != DYNTS_SCORE_EXTERNAL) s_new = nullptr;
   question = question ? 1 : 0;
@@ -310,7 +318,7 @@ int dynts_rotate(const dynts_rotary *r, const uint16_t *q, int32_t q_heads, cons
   if (n_tokens == 0) return DYNTS_OK;
   if (!r->freq || !positions || !q || !q_out || (k && !k_out)) return DYNTS_ENULL;
   if (q_heads <= 0 || (k && k_heads <= 0)) return DYNTS_EINVAL;
-  if (((long long)q_heads + (k ? k_heads : 0)) * r->head_dim > (1 << 28)) return DYNTS_ESHAPE;
+  if (((long long)q_heads + (k ? k_heads : 0)) * r->head_dim > (1 << 28) || n_tokens >= dynts::kRotMaxTokens) return DYNTS_ESHAPE;
   if (misaligned(q, 16) || misaligned(q_out, 16) || (k && (misaligned(k, 16) || misaligned(k_out, 16)))) return DYNTS_EINVAL;
   const dynts::RotateParams p{q, k, q_out, k_out, positions, r->freq, r->axis, n_tokens, q_heads, k ? k_heads : 0, r->head_dim, r->n_pairs,
                               r->n_axes, inverse ? -1.f : 1.f};

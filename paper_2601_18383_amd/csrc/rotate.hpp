@@ -24,6 +24,7 @@ struct RotateParams {
 
 constexpr int kRotThreads = 256;
 constexpr int kRotMaxPairs = 128;
+constexpr int kRotMaxTokens = 1 << 24;  // (a grid holds fewer than 2^32 threads)
 
 // grid (tokens), one token a workgroup.
 template <bool ADJACENT>

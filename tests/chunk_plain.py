@@ -11,16 +11,17 @@ import torch
 HALF16, HALF32 = 2.0 ** -8, 2.0 ** -24
 
 
-def attention(q, K, V, pos, n, m, scale, softcap=0.0, window=0, slope=None, first=None, last=None):
+def attention(q, K, V, pos, n, m, scale, softcap=0.0, window=0, slope=None, first=None, last=None, device="cpu"):
     """One sequence: q [T][Hq][d], K, V [Hkv][>= n][d], pos [Hkv][>= n]; its last m tokens are the queries.
     -> dict of out [m][Hq][d], lse [m][Hq], recv [Hkv][n] and bounds out_tol, lse_tol, recv_tol."""
     Hq, d = q.shape[1:]
     Hkv = K.shape[0]
     G = Hq // Hkv
-    q, K, V = q[:m].double().cpu(), K[:, :n].double().cpu(), V[:, :n].double().cpu()
-    pos = pos[:, :n].long().cpu()
+    q, K, V = (x.to(device, torch.float64) for x in (q[:m], K[:, :n], V[:, :n]))
+    pos = pos[:, :n].to(device, torch.int64)
     r = dict(out=torch.zeros(m, Hq, d, dtype=torch.float64), lse=torch.zeros(m, Hq, dtype=torch.float64),
              recv=torch.zeros(Hkv, n, dtype=torch.float64))
+    r = {k: x.to(device) for k, x in r.items()}
     r.update(out_tol=torch.zeros_like(r["out"]), lse_tol=torch.zeros_like(r["lse"]), recv_tol=torch.zeros_like(r["recv"]))
     for hq in range(Hq):
         h = hq // G
@@ -37,15 +38,15 @@ def attention(q, K, V, pos, n, m, scale, softcap=0.0, window=0, slope=None, firs
             off = off + 8 * HALF32 * bias
         shaped = softcap > 0 or window > 0 or slope is not None or first is not None or last is not None
         if shaped:
-            high = own if last is None else last[:m].long().cpu()
+            high = own if last is None else last[:m].to(device, torch.int64)
             low = torch.full_like(own, -1)
             if window > 0:
                 low = own - window + 1
             if first is not None:
-                low = torch.maximum(low, first[:m].long().cpu())
+                low = torch.maximum(low, first[:m].to(device, torch.int64))
             seen = (pos[h][None] >= low[:, None]) & (pos[h][None] <= high[:, None])
         else:
-            seen = torch.arange(n)[None] <= (n - m + torch.arange(m))[:, None]
+            seen = torch.arange(n, device=device)[None] <= (n - m + torch.arange(m, device=device))[:, None]
         x = torch.where(seen, x, -math.inf)
         off = torch.where(seen, off, 0.0)
         lse = torch.logsumexp(x, dim=-1)
@@ -60,7 +61,7 @@ def attention(q, K, V, pos, n, m, scale, softcap=0.0, window=0, slope=None, firs
         r["lse"][:, hq], r["lse_tol"][:, hq] = lse, lse_tol
         r["recv"][h] += w.sum(0)
         r["recv_tol"][h] += (w * (torch.exp(rel) - 1)).sum(0) + (m * G + 8) * HALF32 * w.sum(0) + m * 2.0 ** -126
-    return r
+    return {k: x.cpu() for k, x in r.items()}
 
 
 def check(got, ref, tol, what):

@@ -121,6 +121,20 @@ def test_grids_past_their_limit_are_refused(B):
     B.dynts_destroy(ctx)
 
 
+def test_an_output_over_an_input_is_refused(B):
+    cfg, ctx = _bound(B)
+    T, at = 16, lambda x: C.c_void_p(1 << 30 | x)
+    need, rows, k_rows = B.dynts_chunk_scratch_bytes(cfg, T), 3 * T * 8 * 128 * 2, 3 * T * 2 * 128 * 2
+    far, scratch = at(1 << 28), at(1 << 29)
+    for out in (at(0), at(16), at(rows - 16)):
+        assert B.lib.dynts_chunk_attend(ctx, 0, at(0), T, None, None, out, None, scratch, need, None) == B.DYNTS_EINVAL
+        assert B.lib.dynts_chunk_attend(ctx, 0, out, T, None, None, at(0), None, scratch, need, None) == B.DYNTS_EINVAL
+    for out in (at(0), at(k_rows - 16)):
+        assert B.lib.dynts_chunk_step(ctx, 0, far, at(0), far, None, T, None, 0, None, out, None, scratch, need, None) == B.DYNTS_EINVAL
+        assert B.lib.dynts_chunk_step(ctx, 0, far, far, at(0), None, T, None, 0, None, out, None, scratch, need, None) == B.DYNTS_EINVAL
+    B.dynts_destroy(ctx)
+
+
 def test_rotate_refusals(B):
     L = B.lib
 
@@ -132,7 +146,7 @@ def test_rotate_refusals(B):
     assert r(pairing=2) == B.DYNTS_EINVAL and r(pairing=-1) == B.DYNTS_EINVAL
     assert r(axes=0) == B.DYNTS_EINVAL and r(pairs=0) == B.DYNTS_EINVAL and r(n=-1) == B.DYNTS_EINVAL
     for kw in (dict(d=0), dict(d=-8), dict(d=100), dict(pairs=12), dict(pairs=72), dict(d=512, pairs=136), dict(d=64, pairs=40),
-               dict(hq=1 << 22)):
+               dict(hq=1 << 22), dict(n=1 << 24)):
         assert r(**kw) == B.DYNTS_ESHAPE, kw
     for kw in (dict(freq=None), dict(pos=None), dict(q=None), dict(qo=None), dict(ko=None)):
         assert r(**kw) == B.DYNTS_ENULL, kw
@@ -169,3 +183,21 @@ def test_the_binding_refuses_what_does_not_fit(B):
         with pytest.raises(AssertionError):
             call()
     assert n2.numel() == 2
+
+
+def test_the_binding_refuses_a_cache_of_another_gpu(B, monkeypatch):
+    class OnGpu:
+        def get_device(self):
+            return 0
+
+    monkeypatch.setattr(B, "_device", lambda: 0)
+    ctx = C.c_void_p(0)
+    B._on_device(ctx, OnGpu(), None)
+    ctx.gpu = 0
+    B._on_device(ctx, OnGpu(), None)
+    ctx.gpu = 1
+    with pytest.raises(ValueError):
+        B._on_device(ctx, OnGpu(), None)
+    monkeypatch.setattr(B, "_device", lambda: 1)
+    with pytest.raises(ValueError):
+        B._on_device(ctx, OnGpu(), None)

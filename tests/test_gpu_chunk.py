@@ -427,6 +427,49 @@ def test_lengths_past_the_cache_are_clamped(B):
 
 
 @pytest.mark.parametrize("layout", ["dense", "paged"])
+@pytest.mark.parametrize("T,shape", [(3, {}), (300, {}), (300, dict(window=500))])
+def test_a_cache_past_32_bits(B, layout, T, shape):
+    """The last head of 1.1 million slots times 32 heads: its elements begin past 2^32.  A chunk's step there against the definition; the
+    other sequence is left alone."""
+    Hkv, d, n = 16, 128, 1100000
+    gen = torch.Generator(device=DEV).manual_seed(9)
+    c = (B.Cache if layout == "dense" else B.PagedCache)(1, 2, Hkv, Hkv, d, n + T, 0, 0, 1)
+    if layout == "paged":  # the second sequence in the pool's last pages, a head's side by side, the chunk's on the free stack
+        page = c.n_pages - Hkv * c.max_pages + torch.arange(Hkv * c.max_pages, dtype=torch.int32, device=DEV).view(Hkv, c.max_pages)
+        have = (n + 63) // 64
+        c.block_table[0, 1, :, :have] = page[:, :have]
+        top = Hkv * (c.max_pages - have)
+        c.free_stack[:top] = page[:, have:].reshape(-1).flip(0)
+        c.free_top.fill_(top)
+    pool_K, pool_V = (c.K, c.V) if layout == "dense" else (c.K_pool, c.V_pool)
+    assert pool_K.numel() > 2 ** 32
+    rand = lambda *s: torch.randn(s, generator=gen, device=DEV).to(torch.bfloat16)
+    K, V = rand(n, d), rand(n, d)
+    for pool, x in ((pool_K, K), (pool_V, V)):
+        if layout == "dense":
+            pool[0, 1, -1, :n] = x
+        else:
+            pool.view(-1, d)[-c.max_pages * 64:][:n] = x
+    c.seq_len[0, 1] = n
+    c.next_pos[0, 1] = n
+    c.pos[0, 1, :, :n] = torch.arange(n, dtype=torch.int32, device=DEV)
+    q, k, v = (rand(2, T, Hkv, d) for _ in range(3))
+    q = q * 4  # (few keys carry a row's weight: an output that a wrong place would change)
+    out = torch.full((2, T, Hkv, d), 7.0, dtype=torch.bfloat16, device=DEV)
+    lse = torch.zeros((2, T, Hkv), device=DEV)
+    scratch = torch.empty(B.dynts_chunk_scratch_bytes(c.cfg, T), dtype=torch.uint8, device=DEV)
+    n_new = torch.tensor([0, T], dtype=torch.int32, device=DEV)
+    B.dynts_chunk_step(c.ctx, 0, q, k, v, out, scratch, lse=lse, n_new=n_new, shaping=B.Shaping(**shape) if shape else None)
+    assert int(c.status.item()) == 0 and c.seq_len.tolist() == [[0, n + T]]
+    assert torch.all(out[0] == 7.0) and torch.all(c.S[0, 0] == 0)
+    r = plain.attention(q[1, :, -1:], torch.cat((K, k[1, :, -1]))[None], torch.cat((V, v[1, :, -1]))[None], torch.arange(n + T)[None], n + T, T,
+                        1.0 / math.sqrt(d), device=DEV, **shape)
+    plain.check(out[1, :, -1:], r["out"], r["out_tol"], "out")
+    plain.check(lse[1, :, -1:], r["lse"], r["lse_tol"], "lse")
+    plain.check(c.S[0, 1, -1:, :n + T], r["recv"], r["recv_tol"], "received")
+
+
+@pytest.mark.parametrize("layout", ["dense", "paged"])
 def test_captured_steps(B, layout):
     """A rotation and a chunk's step recorded into a graph and replayed, with eager work between the replays: the same as eager."""
     gen = torch.Generator().manual_seed(6)
@@ -463,6 +506,46 @@ def test_captured_steps(B, layout):
         assert torch.equal(a.S, b.S) and torch.equal(a.seq_len, b.seq_len)
         n = int(a.seq_len.max().item())
         assert torch.equal(a.K[:, :, :, :n], b.K[:, :, :, :n])
+
+
+def test_graphs_that_share_scratch_and_streams_that_do_not(B):
+    """Two graphs with one scratch, replayed in turn on one stream; two streams at once, each with a scratch of its own."""
+    cases = [Case(B, "dense", 8, 1, 128, [2900, 10], [200, 64], seed=1).fill(True), Case(B, "paged", 28, 4, 128, [900, 333], [40, 77], seed=2).fill(True)]
+    qs = [c.q.to(DEV) for c in cases]
+    want = []
+    for c, q in zip(cases, qs):
+        B.dynts_chunk_attend(c.cache.ctx, 0, q, c.out, c.scratch, lse=c.lse, n_new=c.n)
+        want.append((c.out.clone(), c.lse.clone()))
+    shared = torch.empty(max(c.scratch.numel() for c in cases), dtype=torch.uint8, device=DEV)
+    graphs = []
+    for c, q in zip(cases, qs):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            B.dynts_chunk_attend(c.cache.ctx, 0, q, c.out, shared, lse=c.lse, n_new=c.n)
+
+    def same():
+        torch.cuda.synchronize()
+        for c, (out, lse) in zip(cases, want):
+            assert torch.equal(c.out, out) and torch.equal(c.lse, lse)
+            c.out.fill_(7.0)
+            c.lse.fill_(7.0)
+        torch.cuda.synchronize()
+
+    same()
+    for turn in range(4):
+        shared.fill_(turn)
+        for graph in graphs:
+            graph.replay()
+        same()
+    streams = [torch.cuda.Stream() for _ in cases]
+    for turn in range(4):
+        for c, q, stream in zip(cases, qs, streams):
+            with torch.cuda.stream(stream):
+                B.dynts_chunk_attend(c.cache.ctx, 0, q, c.out, c.scratch, lse=c.lse, n_new=c.n)
+        same()
+        for c, q, stream in zip(cases, qs, streams):
+            B.dynts_chunk_attend(c.cache.ctx, 0, q, c.out, c.scratch, lse=c.lse, n_new=c.n, stream=stream.cuda_stream)
+        same()
 
 
 def test_results_do_not_change_from_run_to_run(B):
