@@ -85,15 +85,17 @@ __device__ __forceinline__ int chunk_tokens(const ChunkCache &c, const int32_t *
   return m < n ? m : n;
 }
 
-// Where slot t (the same in every lane) of a unit begins, in elements.  The page number comes by the scalar cache: by the vector caches it would be
+// The page that the table has for slot t (the same in every lane) of a unit.  The number comes by the scalar cache: by the vector caches it would be
 // waited for behind every load in flight.
-template <int D>
-__device__ __forceinline__ size_t chunk_tile(const ChunkCache &c, size_t unit, int t) {
-  if (!c.block_table) return (unit * (size_t)c.cap + t) * D;
+__device__ __forceinline__ int chunk_page(const ChunkCache &c, size_t unit, int t) {
   int pi = t / kPageSlots;
   pi = pi < c.max_pages ? pi : c.max_pages - 1;
-  const int pg = *(const __attribute__((address_space(4))) int32_t *)(uintptr_t)(c.block_table + unit * c.max_pages + pi);
-  return ((size_t)safe_page(pg, c.n_pages) * kPageSlots + t % kPageSlots) * D;
+  return *(const __attribute__((address_space(4))) int32_t *)(uintptr_t)(c.block_table + unit * c.max_pages + pi);
+}
+// Where slot t begins, in elements; page: chunk_page's, if there are pages.
+template <int D>
+__device__ __forceinline__ size_t chunk_tile(const ChunkCache &c, size_t unit, int t, int page) {
+  return c.block_table ? ((size_t)safe_page(page, c.n_pages) * kPageSlots + t % kPageSlots) * D : (unit * (size_t)c.cap + t) * D;
 }
 
 // Byte of LDS at which 16-byte piece `piece` of row `row` of a tile lies.  The pieces of a row are permuted so that what is read together lies in
@@ -155,16 +157,23 @@ __device__ __forceinline__ int slot_from(const int32_t *pos, int lo, int hi, int
   return lo;
 }
 
-// The slots that rows of tokens [i0, i1] see, as [lo, hi), given the lowest and the highest position that one of them sees (kNowhere and -1: none).
-__device__ __forceinline__ void chunk_range(const ChunkShape &s, const int32_t *pos, int n, int base, int i0, int i1, int first, int last, int lane,
-                                            int &lo, int &hi) {
+// The slots that rows of tokens [i0, i1] see, as [lo, hi), given the lowest and the highest position that one of them sees (kNowhere and -1: none) and
+// the positions of slots 0 and n - 1.
+__device__ __forceinline__ void chunk_range(const ChunkShape &s, const int32_t *pos, int n, int base, int i0, int i1, int first, int last, int head, int tail,
+                                            int lane, int &lo, int &hi) {
   lo = 0;
+  hi = base + i1 + 1;
+  if (tail - head == n - 1) {  // (no gaps: nothing to look up)
+    if (s.first || s.window > 0) lo = first <= head ? 0 : ((uint32_t)first - (uint32_t)head < (uint32_t)n ? first - head : n);
+    if (s.last) hi = last < head ? 0 : ((uint32_t)last - (uint32_t)head < (uint32_t)n ? last - head + 1 : n);
+    return;
+  }
   if (s.first || s.window > 0) {
-    // (two slots lie no further apart than their positions: without gaps the first look finds it)
+    // (two slots lie no further apart than their positions)
     const int slot = base + i0, d = pos[slot] - first;
     lo = d >= 0 ? slot_from(pos, d < slot ? slot - d : 0, slot, first, lane) : slot_from(pos, slot, n, first, lane);
   }
-  hi = s.last ? slot_from(pos, 0, n, last + 1, lane) : base + i1 + 1;
+  if (s.last) hi = slot_from(pos, 0, n, last + 1, lane);
 }
 
 // cap * tanh(dot * scale / softcap) in log2 units: (1 - u) / (1 + u) with u = 2^(-2 |z| log2 e) is off by 2^-25 of the cap where its argument is small.
@@ -230,12 +239,13 @@ __global__ __launch_bounds__(kChThreads, D == 128 ? 3 : 4) void chunk_attend_ker
 
   // what the rows see: plain, slots [0, lim]; shaped, positions [lo, lo + span].  all_lo, all_hi: what all of the wave's rows see
   const int32_t *pos = c.pos + (size_t)unit * c.cap;
-  int lim, own = 0, t_lo = 0, t_hi, all_lo = 0, all_hi;
+  int lim, own = 0, t_lo = 0, t_hi, all_lo = 0, all_hi, own_lo = 0;  // (own_lo: of the wave's first row)
   uint32_t span = 0;
   const int r1 = blk * kChRows + kChRows - 1;
   const int i0 = chunk_token(blk * kChRows, p.g_magic), i1 = chunk_token(r1 < R ? r1 : R - 1, p.g_magic);
   if (SHAPED) {
     own = pos[base + tok];
+    const int head = pos[0], tail = pos[n - 1];
     chunk_interval(p.shape, (size_t)b * p.T + tok, own, lim, span);
     int first = lim, last = lim == kNowhere ? -1 : (int)(lim + span);
     all_lo = first;
@@ -258,9 +268,11 @@ __global__ __launch_bounds__(kChThreads, D == 128 ? 3 : 4) void chunk_attend_ker
       first = sm_range[w] < first ? sm_range[w] : first;
       last = sm_range[kChWaves + w] > last ? sm_range[kChWaves + w] : last;
     }
-    chunk_range(p.shape, pos, n, base, i0, i1, __builtin_amdgcn_readfirstlane(first), __builtin_amdgcn_readfirstlane(last), lane, t_lo, t_hi);
+    chunk_range(p.shape, pos, n, base, i0, i1, __builtin_amdgcn_readfirstlane(first), __builtin_amdgcn_readfirstlane(last), __builtin_amdgcn_readfirstlane(head),
+                __builtin_amdgcn_readfirstlane(tail), lane, t_lo, t_hi);
     t_lo = t_lo / kChTile * kChTile;
     all_lo = __builtin_amdgcn_readfirstlane(all_lo);
+    if (BIASED) own_lo = __builtin_amdgcn_readlane(own, 0);
   } else {
     lim = base + tok;
     t_hi = base + i1 + 1;
@@ -302,8 +314,11 @@ __global__ __launch_bounds__(kChThreads, D == 128 ? 3 : 4) void chunk_attend_ker
       lds_bring16(vb, off + v_off, 0, to + Lds::kTileBytes);
     }
   };
+  // (the page of the next tile to bring: looked up a tile ahead)
+  int page = c.block_table ? chunk_page(c, unit, t0) : 0;
   auto bring = [&](int t, uint32_t place) {
     if (t >= t1) return;
+    const int this_page = page;
     int rows = n - t < kChTile ? n - t : kChTile, cached = kChTile;
     if (APPEND) {
       cached = base - t;
@@ -311,7 +326,8 @@ __global__ __launch_bounds__(kChThreads, D == 128 ? 3 : 4) void chunk_attend_ker
       if (cached <= 0) return;
       rows = cached < rows ? cached : rows;
     }
-    const size_t at = chunk_tile<D>(c, unit, t);
+    const size_t at = chunk_tile<D>(c, unit, t, this_page);
+    if (c.block_table) page = chunk_page(c, unit, t + kChTile);
     const RowBuffer kb = row_buffer<D>(c.K + at, rows), vb = row_buffer<D>(c.V + at, rows);
 #pragma unroll
     for (int i = 0; i < kInstr; ++i) {
@@ -361,12 +377,18 @@ __global__ __launch_bounds__(kChThreads, D == 128 ? 3 : 4) void chunk_attend_ker
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[e] = soft_cap(s[e], p.shape);
       }
+      const int first = __builtin_amdgcn_readfirstlane(tp[0]), last = __builtin_amdgcn_readfirstlane(tp[kChTile - 1]);
       if (BIASED) {
         const float c = capped ? 1.f : p.scale_log2;
+        if (last - first == kChTile - 1 && last <= own_lo) {  // positions without gaps, none behind a row's own
+          const float bias = -slope * (float)(own - first - 4 * hf);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) s[e] = fmaf(-slope, fabsf((float)(own - tp[8 * (e >> 2) + 4 * hf + (e & 3)])), s[e] * c);
+          for (int e = 0; e < 16; ++e) s[e] = fmaf(s[e], c, fmaf(slope, (float)(8 * (e >> 2) + (e & 3)), bias));
+        } else {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) s[e] = fmaf(-slope, fabsf((float)(own - tp[8 * (e >> 2) + 4 * hf + (e & 3)])), s[e] * c);
+        }
       }
-      const int first = __builtin_amdgcn_readfirstlane(tp[0]), last = __builtin_amdgcn_readfirstlane(tp[kChTile - 1]);
       if (first < all_lo || last > all_hi || t + kChTile > n) {
         asm volatile("; some keys are hidden");  // (a branch: the compiler would compare every key of every tile)
 #pragma unroll
@@ -547,7 +569,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void chunk_attend_few_kernel(const 
   int t_lo = 0, t_hi;
   const int i0 = chunk_token(row0, p.g_magic), i1 = chunk_token(row0 + kFewRows - 1 < R ? row0 + kFewRows - 1 : R - 1, p.g_magic);
   if (SHAPED) {
-    const int own = pos[base + i];
+    const int own = pos[base + i], head = pos[0], tail = pos[n - 1];
     chunk_interval(p.shape, (size_t)b * p.T + i, own, lo, span);
     ref = __builtin_amdgcn_readfirstlane(pos[base]);
     at = (float)(own - ref);
@@ -560,7 +582,8 @@ __global__ __launch_bounds__(kFewThreads, 2) void chunk_attend_few_kernel(const 
       first = f < first ? f : first;
       last = l > last ? l : last;
     }
-    chunk_range(p.shape, pos, n, base, i0, i1, __builtin_amdgcn_readfirstlane(first), __builtin_amdgcn_readfirstlane(last), lane, t_lo, t_hi);
+    chunk_range(p.shape, pos, n, base, i0, i1, __builtin_amdgcn_readfirstlane(first), __builtin_amdgcn_readfirstlane(last), __builtin_amdgcn_readfirstlane(head),
+                __builtin_amdgcn_readfirstlane(tail), lane, t_lo, t_hi);
     t_lo = t_lo / kFewTile * kFewTile;
   } else {
     t_hi = base + i1 + 1;
@@ -586,7 +609,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void chunk_attend_few_kernel(const 
   auto fetch = [&](int tile, u32x4 (&x)[PIECES], const uint16_t *pool) {
     // (past the share's end: a buffer of no rows, nothing is fetched)
     const int rows = tile < t_end ? (n - tile < kFewTile ? n - tile : kFewTile) : 0;
-    const RowBuffer buf = row_buffer<D>(pool + (rows > 0 ? chunk_tile<D>(c, unit, tile) : 0), rows);
+    const RowBuffer buf = row_buffer<D>(pool + (rows > 0 ? chunk_tile<D>(c, unit, tile, c.block_table ? chunk_page(c, unit, tile) : 0) : 0), rows);
 #pragma unroll
     for (int k = 0; k < PIECES; ++k) x[k] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(buf, 16 * (lane + 64 * k), 0, 0));
   };

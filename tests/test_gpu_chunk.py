@@ -184,6 +184,22 @@ def test_shaped(B, layout, kind, Hq, Hkv, d, n_old, n_new):
     assert int(c.cache.status.item()) == 0
 
 
+@pytest.mark.parametrize("kind", ["slope", "window", "documents", "prefix", "empty", "future", "cap_slope_window_documents_prefix", "slope_prefix_empty"])
+@pytest.mark.parametrize("Hq,Hkv,d,n_old,n_new", [SHAPES[1], SHAPES[7], SHAPES[9], (8, 2, 128, [300, 0, 1], [500, 400, 31]), (8, 2, 64, [0, 70], [600, 450])])
+def test_shaped_without_gaps(B, kind, Hq, Hkv, d, n_old, n_new):
+    """Positions that go up by one, from 17 on: slots are found without a search, and the bias of a tile is linear."""
+    c = Case(B, "dense", Hq, Hkv, d, n_old, n_new, seed=13, qscale=2.0)
+    c.pos, c.next = [p + 17 for p in c.pos], [p + 17 for p in c.next]
+    c.fill(True)
+    s = _shapings(c, c.gen, kind)
+    sh = B.Shaping(**{k: (v.to(DEV) if torch.is_tensor(v) else v) for k, v in s.items()})
+    dst = torch.full((len(n_old), Hkv, c.cap), 7.0, dtype=torch.float32, device=DEV)
+    q = c.q.to(DEV)
+    B.dynts_chunk_attend(c.cache.ctx, 0, q, c.out, c.scratch, lse=c.lse, n_new=c.n, shaping=sh)
+    B.dynts_chunk_scores(c.cache.ctx, 0, q, c.lse, dst=dst, accumulate=False, n_new=c.n, shaping=sh)
+    c.check(kind, lse=c.lse, recv=dst, **s)
+
+
 def test_keys_hidden_from_all_may_be_anything(B):
     """K rows of another document that hold NaN and infinities, and what lies behind the length in the cache."""
     c = Case(B, "dense", 8, 2, 64, [100], [70], seed=3).fill(True)
