@@ -102,17 +102,29 @@ struct SbStage {
 template <int D>
 __device__ __forceinline__ void sb_multiply(f32x16 (&acc)[kSbTiles], const char *buf, const bf16x8 (&st)[kSbTiles][D / 16],
                                             int c, int hf) {
-  bf16x8 a[D / 16];
-  load_row_frags<D>(a, buf + c * SbStage<D>::LROW, hf);
+  const char *const row = buf + c * SbStage<D>::LROW + 16 * hf;
+  auto piece = [&](int ks) { return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(row + 32 * ks)); };
+  // (read four pieces ahead, in this order: the scores of a chunk with a window in 199 us instead of 210, both passes here as before)
+  constexpr int kAhead = 4;
+  bf16x8 a[kAhead];
+#pragma unroll
+  for (int ks = 0; ks < kAhead; ++ks) a[ks] = piece(ks);
 #pragma unroll
   for (int t = 0; t < kSbTiles; ++t)
 #pragma unroll
     for (int i = 0; i < 16; ++i) acc[t][i] = 0.f;
+  __builtin_amdgcn_sched_barrier(0);
   __builtin_amdgcn_s_setprio(1);  // (a wave's products first: 1 % of both passes)
 #pragma unroll
-  for (int ks = 0; ks < D / 16; ++ks)
+  for (int ks = 0; ks < D / 16; ++ks) {
 #pragma unroll
-    for (int t = 0; t < kSbTiles; ++t) acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[ks], st[t][ks], acc[t], 0, 0, 0);
+    for (int t = 0; t < kSbTiles; ++t) acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[ks % kAhead], st[t][ks], acc[t], 0, 0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    if (ks + kAhead < D / 16) {
+      a[ks % kAhead] = piece(ks + kAhead < D / 16 ? ks + kAhead : 0);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
   __builtin_amdgcn_s_setprio(0);
 }
 
