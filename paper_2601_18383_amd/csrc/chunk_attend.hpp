@@ -60,12 +60,16 @@ constexpr int kShareTiles = 16;  // least tiles of 32 slots in a share
 
 // This workgroup's share of the tiles of its rows, as [from, to); false: it has none.
 __device__ __forceinline__ bool chunk_share(const ChunkAttendParams &p, int tiles, int split, int place, int &shares, int &from, int &to) {
+  shares = 1;
+  from = 0;
+  to = tiles;
+  if (p.n_split == 1) return true;
   shares = tiles / kShareTiles;
   shares = shares < 1 ? 1 : (shares < p.n_split ? shares : p.n_split);
-  if (p.n_split > 1 && split == 0 && threadIdx.x == 0) p.part_n[place] = shares;
+  if (split == 0 && threadIdx.x == 0) p.part_n[place] = shares;
   if (split >= shares) return false;
-  from = (int)((long long)tiles * split / shares);
-  to = (int)((long long)tiles * (split + 1) / shares);
+  from = tiles * split / shares;  // (tiles below 2^18, shares 32 at most)
+  to = tiles * (split + 1) / shares;
   return true;
 }
 
@@ -176,10 +180,11 @@ __device__ __forceinline__ void chunk_range(const ChunkShape &s, const int32_t *
   if (s.last) hi = slot_from(pos, 0, n, last + 1, lane);
 }
 
-// cap * tanh(dot * scale / softcap) in log2 units: (1 - u) / (1 + u) with u = 2^(-2 |z| log2 e) is off by 2^-25 of the cap where its argument is small.
+// cap * tanh(z), z = dot * scale / softcap, in log2 units, as cap - 2 cap / (1 + e^(2 z)): five operations, off by 6 half steps of the cap at most, wherever it lies
+// (cap (1 - u) / (1 + u) with u = e^(-2 |z|): seven, off by 3; attention of 2048 tokens of 8 sequences, 32 heads on 8, 372 us and so 346, scores of 512
+// tokens of 16 on 2464 slots, 28 on 4, 346 and so 307).
 __device__ __forceinline__ float soft_cap(float dot, const ChunkShape &s) {
-  const float u = fast_exp2(-fabsf(dot * s.cap_in));
-  return copysignf(s.cap * (1.f - u) * __builtin_amdgcn_rcpf(1.f + u), dot);
+  return fmaf(-2.f * s.cap, __builtin_amdgcn_rcpf(1.f + fast_exp2(dot * s.cap_in)), s.cap);
 }
 
 // Eight neighbouring elements of an output row, and its lse, from their unnormalised values, shift and sum.
@@ -204,9 +209,16 @@ __device__ __forceinline__ int chunk_lds_v(int row, int piece) {
   return row * (2 * D) + 16 * (piece ^ (D == 128 ? (row & 3) << 2 : ((row >> 1) & 1) << 2));
 }
 
-// SHAPED: positions count, not slots.  BIASED: with a bias by distance.  APPEND (plain form): the chunk's own rows are not in the cache yet; they are read
-// where the caller has them, and every workgroup copies those of its tokens at its end.  (Copied by a launch of their own before, 512 tokens of 64
-// sequences, 32 heads on 8: 260 us a step instead of 217.)
+// Bound by instruction issue and by the clock that the matrix cores leave: 2048 queries on 16384 slots, 32 heads on 8 of 128, 584 GFLOP in 517 us, 1.13
+// PFLOP/s (a product of 8192 x 8192 x 8192 reaches 1.27); the matrix cores are busy 57 % of the cycles, at 1.8 GHz.  Short prompts by HBM: 512
+// tokens of 64 sequences into an empty cache move 0.8 GB in 235 us.
+//   Three workgroups a compute unit (168 registers): with two and twice the rows a wave 640 us, with the next tile's products among a tile's weights 551.
+//   Tiles by loads straight to LDS: through registers there is no room for three workgroups (1610 us, spilled).
+//
+// SHAPED: positions count, not slots.  BIASED: with a bias by distance (a form of its own: its operations cost the others registers).  APPEND (plain
+// form): the chunk's own rows are not in the cache yet; they are read where the caller has them, and every workgroup copies those of its tokens at its
+// end.  (Copied by a launch of their own before, 512 tokens of 64 sequences, 32 heads on 8: 244 us a step instead of 236, heads of 64 134 instead of
+// 123, 28 on 4 of 32 sequences, 600 tokens, 122 instead of 123.)
 template <int D, bool SHAPED, bool BIASED, bool APPEND>
 __global__ __launch_bounds__(kChThreads, D == 128 ? 3 : 4) void chunk_attend_kernel(const ChunkAttendParams p) {
   using Lds = ChunkLds<D>;
@@ -559,7 +571,8 @@ __global__ __launch_bounds__(kChThreads, D == 128 ? 3 : 4) void chunk_attend_ker
 
 // ---- few rows: 32 of them a workgroup, its eight waves share out the keys --------------------------------------------------
 // Bound by HBM (or the memory-side cache): every wave streams 32 slots at a time through registers and a part of LDS of its own, the next
-// tile's loads in flight while it works on one, no barrier before the end.  There the waves' outputs are joined through LDS.
+// tile's loads in flight while it works on one, no barrier before the end.  There the waves' outputs are joined through LDS.  Four tokens of 32
+// sequences on 2464 slots, 28 heads on 4 of 128: 161 MB in 35 us from HBM, 28 from the memory-side cache.
 constexpr int kFewWaves = 8, kFewThreads = kFewWaves * 64, kFewRows = 32, kFewTile = 32;
 template <int D>
 struct FewLds {
