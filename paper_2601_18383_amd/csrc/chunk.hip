@@ -108,6 +108,7 @@ int check_shaping(const dynts_shaping *s) {
 uint32_t group_magic(int G) { return G == 1 ? 0u : (uint32_t)(((1ull << 32) + G - 1) / G); }
 
 bool shaped(const dynts_shaping *s) { return s && (s->softcap > 0.f || s->window > 0 || s->slope || s->first || s->last); }
+bool shaped(const dynts::ChunkShape &s) { return s.cap > 0.f || s.window > 0 || s.slope || s.first || s.last; }
 
 dynts::ChunkShape chunk_shape(const dynts_shaping *s, float scale) {
   dynts::ChunkShape out{};
@@ -165,7 +166,20 @@ unsigned chunk_grid(const ChunkCache &c, long long blocks, int threads) {
 unsigned attend_grid(const ChunkCache &c, const ChunkPlan &pl) {
   return chunk_grid(c, (long long)pl.blocks * pl.n_split, pl.few ? dynts::kFewThreads : dynts::kChThreads);
 }
-unsigned scores_grid(const ChunkCache &c) { return chunk_grid(c, (c.cap + dynts::kCsKeys - 1) / dynts::kCsKeys, dynts::kSbWaves * 64); }
+// Which kernel of chunk_scores.hpp.  C: chunks of 32 rows of a unit, W: workgroups of 64 slots, one a compute unit.  Few slots: 7 + C / 4 us a round of 256 of
+// them; many: 4 + 0.8 C us while its W / 4 workgroups have a compute unit each.  us, few / many:
+//   head_dim 128: C = 66, W = 168 21.9 / 60.4, W = 672 60.9 / 61.5; C = 219, W = 152 57.0 / 170, W = 512 97.6 / 184; C = 389, W = 432 100 / 304; C = 112,
+//     W = 752 93.1 / 92.2, W = 1504 183 / 122; C = 14, W = 640 26.3 / 16.8; C = 2, W = 568 14.5 / 5.9
+//   head_dim 64: C = 164, W = 78 23.1 / 128; C = 10, W = 64 6.0 / 10.9; C = 38, W = 288 15.7 / 29.8, W = 1152 38.2 / 40.2
+bool scores_few(const ChunkCache &c, int n_tokens) {
+  const long long W = (long long)c.Nb * c.Hkv * ((c.cap + dynts::kCfKeys - 1) / dynts::kCfKeys);
+  const long long C = ((long long)n_tokens * c.G + dynts::kSbChunk - 1) / dynts::kSbChunk;
+  return W <= 256 ? C >= 8 : W <= 512 && C >= 32;
+}
+unsigned scores_grid(const ChunkCache &c, bool few) {
+  return few ? chunk_grid(c, (c.cap + dynts::kCfKeys - 1) / dynts::kCfKeys, dynts::kCfWaves * 64)
+             : chunk_grid(c, (c.cap + dynts::kCsKeys - 1) / dynts::kCsKeys, dynts::kSbWaves * 64);
+}
 
 template <int D, bool SHAPED>
 void launch_attend_d(const dynts::ChunkAttendParams &p, const ChunkPlan &pl, unsigned grid, hipStream_t st) {
@@ -206,23 +220,27 @@ int launch_attend(const ChunkCache &c, const uint16_t *q, int n_tokens, const in
   return launch_status();
 }
 
+template <int D, bool SHAPED, bool BIASED>
+void launch_scores_form(const dynts::ChunkScoreParams &p, bool few, unsigned grid, hipStream_t st) {
+  if (few) hipLaunchKernelGGL((dynts::chunk_scores_few_kernel<D, SHAPED, BIASED>), dim3(grid), dim3(dynts::kCfWaves * 64), 0, st, p);
+  else hipLaunchKernelGGL((dynts::chunk_scores_kernel<D, SHAPED, BIASED>), dim3(grid), dim3(dynts::kSbWaves * 64), 0, st, p);
+}
+template <int D>
+void launch_scores_d(const dynts::ChunkScoreParams &p, bool few, unsigned grid, hipStream_t st) {
+  if (shaped(p.shape) && p.shape.slope) launch_scores_form<D, true, true>(p, few, grid, st);
+  else if (shaped(p.shape)) launch_scores_form<D, true, false>(p, few, grid, st);
+  else launch_scores_form<D, false, false>(p, few, grid, st);
+}
+
 int launch_scores(const ChunkCache &c, const uint16_t *q, int n_tokens, const int32_t *n_new, const dynts_shaping *shaping, const float *lse,
                   float *dst, int accumulate, hipStream_t st) {
   const dynts::ChunkScoreParams p{c, q, n_new, lse, dst ? dst : c.S, chunk_shape(shaping, c.scale), n_tokens, dst ? 0 : 1, accumulate ? 1 : 0,
                                   c.scale * kLog2E, group_magic(c.G)};
-  const unsigned grid = scores_grid(c);
+  const bool few = scores_few(c, n_tokens);
+  const unsigned grid = scores_grid(c, few);
   if (!grid) return DYNTS_EINVAL;
-  const dim3 block(dynts::kSbWaves * 64);
-  const bool positions = shaped(shaping), biased = positions && shaping->slope;
-  if (c.D == 128) {
-    if (biased) hipLaunchKernelGGL((dynts::chunk_scores_kernel<128, true, true>), dim3(grid), block, 0, st, p);
-    else if (positions) hipLaunchKernelGGL((dynts::chunk_scores_kernel<128, true, false>), dim3(grid), block, 0, st, p);
-    else hipLaunchKernelGGL((dynts::chunk_scores_kernel<128, false, false>), dim3(grid), block, 0, st, p);
-  } else {
-    if (biased) hipLaunchKernelGGL((dynts::chunk_scores_kernel<64, true, true>), dim3(grid), block, 0, st, p);
-    else if (positions) hipLaunchKernelGGL((dynts::chunk_scores_kernel<64, true, false>), dim3(grid), block, 0, st, p);
-    else hipLaunchKernelGGL((dynts::chunk_scores_kernel<64, false, false>), dim3(grid), block, 0, st, p);
-  }
+  if (c.D == 128) launch_scores_d<128>(p, few, grid, st);
+  else launch_scores_d<64>(p, few, grid, st);
   return launch_status();
 }
 
@@ -294,7 +312,7 @@ int dynts_chunk_step(dynts_ctx *ctx, int32_t layer, const uint16_t *q, const uin
   hipStream_t st = static_cast<hipStream_t>(stream);
   int32_t *taken = static_cast<int32_t *>(scratch);
   const bool scores = c.score_mode == DYNTS_SCORE_ACCUMULATE && !question;
-  if (!attend_grid(c, pl) || (scores && !scores_grid(c))) return DYNTS_EINVAL;  // (before the append)
+  if (!attend_grid(c, pl) || (scores && !scores_grid(c, scores_few(c, n_tokens)))) return DYNTS_EINVAL;  // (before the append)
   const size_t row = (size_t)c.Nb * n_tokens * c.D * 2, q_bytes = row * c.Hq, k_bytes = row * c.Hkv;
   if (overlap(out, q_bytes, q, q_bytes) || overlap(out, q_bytes, k_new, k_bytes) || overlap(out, q_bytes, v_new, k_bytes)) return DYNTS_EINVAL;
   if (scores && !lse) lse = reinterpret_cast<float *>(static_cast<char *>(scratch) + pl.off_lse);

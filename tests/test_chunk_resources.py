@@ -59,3 +59,8 @@ def test_scores_keep_three_workgroups_a_compute_unit(kernels):
         assert k["vgpr_count"] <= 168 and 3 * k["group_segment_fixed_size"] <= 160 * 1024, name
     for name, k in _named(kernels, r"chunk_scores_kernelILi(64|128)ELb0ELb0EE", 2).items():
         assert k["vgpr_spill_count"] == 0, name
+
+
+def test_scores_of_few_slots_do_not_spill(kernels):
+    for name, k in _named(kernels, r"chunk_scores_few_kernelILi(64|128)E", 6).items():
+        assert k["vgpr_count"] <= 256 and k["vgpr_spill_count"] == 0, name

@@ -106,6 +106,7 @@ SHAPES = [  # Hq, Hkv, d, n_old, n_new
     (8, 2, 128, [8000], [600]),                                         # many rows of few units: keys in shares
     (8, 2, 64, [3500], [600]),
     (16, 1, 128, [50, 0, 7] * 4, [70, 65, 8] * 4),                      # the largest group, many rows
+    (32, 8, 128, [700, 0, 300, 64, 10, 650], [100, 99, 64, 130, 1, 33]),  # many slots of many units, several groups of rows
 ]
 MANY = SHAPES[10:]
 
