@@ -174,6 +174,7 @@ def make_config(n_layers, batch, n_q_heads, n_kv_heads, head_dim, capacity, budg
 def dynts_create(cfg):
     ctx = C.c_void_p()
     _check(lib.dynts_create(C.byref(cfg), C.byref(ctx)), "dynts_create")
+    ctx.dims = (cfg.batch, cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim, cfg.capacity)
     return ctx
 
 
@@ -481,9 +482,9 @@ def _shaping(shaping):
     return None if shaping is None else shaping.ref
 
 
-def _on_device(ctx, *tensors):
-    """All of them on the current GPU, and the arrays bound to ctx: an address of another one, or of the host, would only be found out
-    by a kernel."""
+def _on_device(owner, *tensors):
+    """All of them on the current GPU, and what is bound to the context (or are the rotary tables): an address of another one, or of
+    the host, would only be found out by a kernel."""
     dev = None
     for t in tensors:
         if t is None:
@@ -495,14 +496,16 @@ def _on_device(ctx, *tensors):
             dev = _device()
         if at != dev:
             raise ValueError("tensors have to be on the current GPU (%d, not %d)" % (dev, at))
-    bound = getattr(ctx, "gpu", dev)
+    bound = getattr(owner, "gpu", dev)
     if bound != dev:
-        raise ValueError("the cache lies on GPU %d, the current one is %d" % (bound, dev))
+        raise ValueError("the cache's arrays or the tables are not on the current GPU (%d, not %d)" % (dev, bound))
 
 
 def _chunk_sizes(ctx, q, n_new, shaping, lse, *others):
     """n_new, shaping and lse fit a chunk of queries q [Nb][T][Hq][d], and all lie on the current GPU, `others` too."""
     Nb, T, Hq, d = q.shape
+    dims = getattr(ctx, "dims", None)
+    assert dims is None or (Nb, Hq, d) == (dims[0], dims[1], dims[3]), "the context's batch, query heads and head_dim"
     assert n_new is None or n_new.numel() == Nb, "n_new holds one number a sequence"
     assert lse is None or lse.numel() == Nb * T * Hq, "lse holds one number a token and query head"
     if shaping is None:
@@ -514,9 +517,11 @@ def _chunk_sizes(ctx, q, n_new, shaping, lse, *others):
     return T
 
 
-def _chunk_rows(k_new, v_new, s_new):
+def _chunk_rows(ctx, k_new, v_new, s_new):
     """k_new, v_new [Nb][T][Hkv][d] and s_new [Nb][T][Hkv] are of one chunk."""
     Nb, T, Hkv, d = k_new.shape
+    dims = getattr(ctx, "dims", None)
+    assert dims is None or (Nb, Hkv, d) == (dims[0], dims[2], dims[3]), "the context's batch, KV heads and head_dim"
     assert v_new.numel() == Nb * T * Hkv * d, "k_new and v_new are of one shape"
     assert s_new is None or s_new.numel() == Nb * T * Hkv, "s_new holds one number a token and KV head"
     return Nb, T
@@ -525,7 +530,7 @@ def _chunk_rows(k_new, v_new, s_new):
 def dynts_chunk_append(ctx, layer, k_new, v_new, scratch, n_new=None, s_new=None, question=False, stream=None):
     """k_new, v_new bf16 [Nb][T][Hkv][d], s_new fp32 [Nb][T][Hkv], n_new int32 [Nb]; scratch: device tensor of at least
     dynts_chunk_scratch_bytes bytes."""
-    Nb, T = _chunk_rows(k_new, v_new, s_new)
+    Nb, T = _chunk_rows(ctx, k_new, v_new, s_new)
     assert n_new is None or n_new.numel() == Nb, "n_new holds one number a sequence"
     _on_device(ctx, k_new, v_new, s_new, n_new, scratch)
     _check(lib.dynts_chunk_append(ctx, layer, _ptr(k_new, torch.bfloat16), _ptr(v_new, torch.bfloat16),
@@ -546,6 +551,8 @@ def dynts_chunk_attend(ctx, layer, q, out, scratch, lse=None, n_new=None, shapin
 
 def dynts_chunk_scores(ctx, layer, q, lse, dst=None, accumulate=True, n_new=None, shaping=None, stream=None):
     """q and lse as in dynts_chunk_attend; dst fp32 [Nb][Hkv][cap] or None (= the layer's S)."""
+    dims = getattr(ctx, "dims", None)
+    assert dst is None or dims is None or dst.numel() == dims[0] * dims[2] * dims[4], "dst holds one number a slot"
     T = _chunk_sizes(ctx, q, n_new, shaping, lse, dst)
     _check(lib.dynts_chunk_scores(ctx, layer, _ptr(q, torch.bfloat16), T, _ptr(n_new, torch.int32),
                                   _shaping(shaping), _ptr(lse, torch.float32), _ptr(dst, torch.float32),
@@ -556,7 +563,7 @@ def dynts_chunk_step(ctx, layer, q, k_new, v_new, out, scratch, lse=None, n_new=
                      shaping=None, stream=None):
     """dynts_chunk_append, dynts_chunk_attend and dynts_chunk_scores into S in one call; arguments as there."""
     T = _chunk_sizes(ctx, q, n_new, shaping, lse, k_new, v_new, s_new, out, scratch)
-    assert _chunk_rows(k_new, v_new, s_new) == (q.shape[0], T) and out.numel() == q.numel(), "q, k_new, v_new and out are of one chunk"
+    assert _chunk_rows(ctx, k_new, v_new, s_new) == (q.shape[0], T) and out.numel() == q.numel(), "q, k_new, v_new and out are of one chunk"
     _check(lib.dynts_chunk_step(ctx, layer, _ptr(q, torch.bfloat16), _ptr(k_new, torch.bfloat16),
                                 _ptr(v_new, torch.bfloat16), _ptr(s_new, torch.float32), T,
                                 _ptr(n_new, torch.int32), 1 if question else 0, _shaping(shaping),
@@ -569,8 +576,8 @@ class Rotary:
     axis uint8 [n_pairs] or None."""
 
     def __init__(self, head_dim, freq, axis=None, n_axes=1, pairing=DYNTS_PAIR_HALVES):
-        assert axis is None or axis.shape == freq.shape
-        self.t = (freq, axis)
+        assert axis is None or (axis.shape == freq.shape and axis.device == freq.device)
+        self.t, self.gpu = (freq, axis), freq.get_device()
         self.head_dim, self.n_axes = head_dim, n_axes
         self.r = dynts_rotary(head_dim, freq.numel(), pairing, n_axes, _ptr(freq, torch.float32), _ptr(axis, torch.uint8))
         self.ref = C.byref(self.r)
@@ -584,7 +591,7 @@ def dynts_rotate(rotary, q, k, positions, q_out, k_out, inverse=False, stream=No
     if k is not None:
         hk, size = k.shape[-2], k.numel()
         assert size == n * hk * d and k_out.numel() == size, "one position a token, head_dim elements a head"
-    _on_device(None, q, k, positions, q_out, k_out)
+    _on_device(rotary, q, k, positions, q_out, k_out)
     _check(lib.dynts_rotate(rotary.ref, _ptr(q, torch.bfloat16), hq, _ptr(k, torch.bfloat16), hk,
                             _ptr(positions, torch.int32), n, 1 if inverse else 0, _ptr(q_out, torch.bfloat16),
                             _ptr(k_out, torch.bfloat16) if k is not None else None, _stream(stream)), "dynts_rotate")

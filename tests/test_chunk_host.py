@@ -201,3 +201,27 @@ def test_the_binding_refuses_a_cache_of_another_gpu(B, monkeypatch):
     monkeypatch.setattr(B, "_device", lambda: 1)
     with pytest.raises(ValueError):
         B._on_device(ctx, OnGpu(), None)
+
+
+def test_the_binding_refuses_chunks_of_another_context(B):
+    """Batch, heads and head_dim of the context, and the size of dst: a smaller tensor would be read or written past its end."""
+    import torch
+    cfg, ctx = _bound(B)  # 3 sequences, 8 heads on 2 of 128, 400 slots
+    z = lambda *s: torch.zeros(s, dtype=torch.bfloat16)
+    q, k, s = z(3, 5, 8, 128), z(3, 5, 2, 128), torch.zeros(64, dtype=torch.uint8)
+    lse = torch.zeros((3, 5, 8))
+    for bad in (z(2, 5, 8, 128), z(3, 5, 4, 128), z(3, 5, 8, 64)):
+        with pytest.raises(AssertionError):
+            B.dynts_chunk_attend(ctx, 0, bad, bad, s)
+        with pytest.raises(AssertionError):
+            B.dynts_chunk_step(ctx, 0, bad, k, k, bad, s)
+    for bad in (z(2, 5, 2, 128), z(3, 5, 1, 128), z(3, 5, 2, 64)):
+        with pytest.raises(AssertionError):
+            B.dynts_chunk_append(ctx, 0, bad, bad, s)
+    with pytest.raises(AssertionError):
+        B.dynts_chunk_scores(ctx, 0, q, lse, dst=torch.zeros((3, 2, 399)))
+    with pytest.raises(ValueError):  # (these sizes fit: it is the host's tensors that are refused)
+        B.dynts_chunk_scores(ctx, 0, q, lse, dst=torch.zeros((3, 2, 400)))
+    rot = B.Rotary(128, torch.ones(64))
+    assert rot.gpu < 0  # tables of the host are refused wherever the queries are
+    B.dynts_destroy(ctx)
