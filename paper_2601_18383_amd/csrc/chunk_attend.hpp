@@ -58,6 +58,21 @@ struct ChunkAttendParams {
 
 constexpr int kShareTiles = 16;  // least tiles of 32 slots in a share
 
+// Workgroup to unit and block: a unit's blocks on one XCD, as sb_map has them, but block by block through `group` units at a time, so that those that have least
+// to do (the first rows, the last slots) come last and fill what the others leave.  Attention, 4 units: 1024 tokens of 8 sequences, 32 heads on 8, 73 us
+// instead of 82, 512 of 8 25 instead of 32, of 64 198 instead of 206.  (8 units 74, 29 and 206; all of them 74, 29 and 243: then the blocks that wait for HBM no longer
+// run beside those that compute.)  Scores, all units: 2000 tokens of 16 sequences 297 us instead of 425, 1024 of 16 (28 on 4) on 2464 slots 380 instead of 474, 512 of
+// 64 676 instead of 661.
+__device__ __forceinline__ bool chunk_map(int group, int n_blk, int n_units, int &unit, int &blk) {
+  const int id = blockIdx.x, xcd = id & 7, slot = id >> 3, per_xcd = (n_units + 7) >> 3;
+  group = group < per_xcd ? group : per_xcd;
+  const int first = slot / (group * n_blk) * group, left = per_xcd - first, size = left < group ? left : group, rem = slot - first * n_blk;
+  blk = rem / size;
+  unit = (first + rem - blk * size) * 8 + xcd;
+  return unit < n_units;
+}
+constexpr int kAllUnits = 0x7fffffff;
+
 // This workgroup's share of the tiles of its rows, as [from, to); false: it has none.
 __device__ __forceinline__ bool chunk_share(const ChunkAttendParams &p, int tiles, int split, int place, int &shares, int &from, int &to) {
   shares = 1;
@@ -230,7 +245,7 @@ __global__ __launch_bounds__(kChThreads, D == 128 ? 3 : 4) void chunk_attend_ker
   const int col = lane & 31, hf = lane >> 5, r16 = lane & 15;
   int unit, blk;
   const int n_blk = (p.T * c.G + kChRows - 1) / kChRows;
-  if (!sb_map(n_blk * p.n_split, c.Nb * c.Hkv, unit, blk)) return;
+  if (!chunk_map(4, n_blk * p.n_split, c.Nb * c.Hkv, unit, blk)) return;
   const int split = blk / n_blk;
   blk -= split * n_blk;
   const int b = unit / c.Hkv, h = unit - b * c.Hkv;

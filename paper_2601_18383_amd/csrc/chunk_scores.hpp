@@ -190,7 +190,7 @@ __global__ __launch_bounds__(kSbWaves * 64, D == 128 || SHAPED ? 3 : 4) void chu
   __shared__ __attribute__((aligned(16))) ChunkRows<SHAPED, BIASED, kCsGroup> sm_rows[2];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, hf = lane >> 5;
   int unit, blk;
-  if (!sb_map((c.cap + kCsKeys - 1) / kCsKeys, c.Nb * c.Hkv, unit, blk)) return;
+  if (!chunk_map(kAllUnits, (c.cap + kCsKeys - 1) / kCsKeys, c.Nb * c.Hkv, unit, blk)) return;
   const int b = unit / c.Hkv, h = unit - b * c.Hkv;
   int n;
   const int m = chunk_tokens(c, p.n_new, p.T, b, n);
