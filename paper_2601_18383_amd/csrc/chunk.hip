@@ -39,27 +39,27 @@ constexpr long long kMostPartials = 65536;
 // Which kernel, and into how many shares the keys of a row block are cut at most.  slots: how many a token can see.
 //
 // Few rows, F row blocks of 32, one workgroup a compute unit (two with head_dim 64): a row block is done in 5 + 5.8 us per 1000 slots; many rows, W
-// of 128, three or four a compute unit: 4.5 + 23 us per 1000 slots, 21 where all of them are busy.  us, few / many, each with its best shares:
-//   head_dim 128, 8 units: 1000 slots R = 4 10.3 / 10.2, R = 256 12.8 / 16.7, R = 1024 15.6 / 25.5; 4500 slots R = 64 14.9 / 18.6, R = 512 27.3 / 30.9,
-//     R = 1024 41.5 / 39.2; 16000 slots R = 128 27.0 / 31.2, R = 256 39.8 / 38.4, R = 512 69.5 / 52.3
-//   32 units: 200 slots R = 256 8.8 / 12.0, R = 512 16.4 / 13.8; 4500 slots R = 128 27.9 / 28.3, R = 256 40.8 / 37.6; 16000 slots R = 64 49.0 / 52.3, R = 128
-//     71.0 / 60.7
-//   128 units: R = 64 200 slots 8.5 / 10.3, 4500 52.9 / 59.7, 16000 189 / 199; R = 128 200 slots 15.0 / 11.8, 4500 91.3 / 72.4
-//   512 units: R = 16 300 slots 18.8 / 17.6, 2600 119.7 / 129.6; R = 64 300 slots 32.9 / 20.0, 2600 144.6 / 130.1
-//   head_dim 64: 2 units of 6000 slots R = 1024 30.5 / 27.6, R = 2048 53.5 / 41.8; 10 of 400 R = 308 7.9 / 11.0; 128 of 400 R = 77 9.1 / 12.0, R = 128 9.6 / 11.3, R =
-//     256 18.6 / 15.8
-// Shares, at least 512 slots each, until the chip is full.  us by their number:
-//   few rows, head_dim 128: 8 units of 1000 slots 1 / 2 / 4: 10.6 / 10.5 / 10.6, of 4500 1 / 4 / 8 / 16: 31.0 / 14.0 / 11.5 / 11.0, of 16000 8 / 16 / 32: 21.1 /
-//     19.3 / 22.1; 128 units of 1200 1 / 2: 16.8 / 19.0, of 2464 27.0 / 30.2, of 4000 39.9 / 44.6; head_dim 64, 128 units of 6000 1 / 2: 30.5 / 33.2, 10 of 1500
-//     9.4 / 10.5
-//   many rows, W = 64, 4500 slots 1 / 4 / 8 / 16: 114 / 44.6 / 39.2 / 50.1; W = 128 of 1000 1 / 2 / 4: 30.7 / 27.1 / 30.1; W = 256 of 4500 1 / 2 / 4: 123 /
-//     106 / 119, of 1000 34.6 / 37.4 / 49.0; W = 16 of 16000 8 / 16 / 32: 58.3 / 39.5 / 38.4
+// of 128, three or four a compute unit: 4 + 21 us per 1000 slots.  us, few / many, each with its shares:
+//   head_dim 128, 2 units: 16000 slots R = 256 23.1 / 27.9, R = 1024 39.4 / 37.6; 8 units: 1000 slots R = 4 10.9 / 24.1, R = 1024 14.2 / 25.6; 4500 slots R = 64
+//     15.2 / 20.8, R = 512 27.2 / 29.5, R = 1024 36.8 / 36.8; 16000 slots R = 128 25.1 / 29.0, R = 256 37.7 / 36.1, R = 512 64.4 / 47.9
+//   32 units: 200 slots R = 256 8.0 / 9.0, R = 512 14.4 / 9.3; 4500 slots R = 128 26.6 / 26.5, R = 256 37.8 / 35.5; 16000 slots R = 64 50.0 / 52.3, R = 128
+//     68.4 / 58.4
+//   128 units: R = 64 200 slots 8.0 / 8.8, 4500 52.3 / 58.7, 16000 184 / 197; R = 128 200 slots 14.5 / 9.2, 1000 26.3 / 26.1, 4500 89.7 / 68.8
+//   512 units: R = 16 300 slots 19.1 / 17.2, 2600 120 / 124; R = 64 300 slots 32.3 / 18.2, 2600 140 / 126
+//   head_dim 64: 2 units of 6000 slots R = 1024 15.1 / 20.4, R = 2048 20.9 / 25.2; 8 of 400 R = 304 6.3 / 9.9; 32 of 2000 R = 512 20.2 / 26.8, of 8000 R = 128
+//     24.6 / 24.2; 128 of 400 R = 128 8.8 / 10.1, R = 256 14.9 / 10.8, of 2000 R = 128 21.0 / 24.6
+// Shares, at least 512 slots each, until the chip is full; none on short caches, where joining them costs more, nor two of few rows of many units, which are
+// bound by HBM.  us by their number:
+//   few rows, head_dim 128: 8 units of 1000 slots 1 / 2 / 4: 12.6 / 13.0 / 12.9, of 4500 1 / 4 / 8 / 16: 33.0 / 16.7 / 14.6 / 14.4, of 16000 8 / 16 / 31: 24.0 /
+//     21.7 / 24.2; R = 128, 32 units of 4500 1 / 2: 34.6 / 26.8; 64 units of 4000 1 / 2 / 4: 30.9 / 27.8 / 27.6; 128 units of 1200 1 / 2: 17.2 / 20.4, of 2464 28.1 /
+//     32.0, of 4000 42.9 / 47.5; head_dim 64, 128 units of 6000 1 / 2: 30.8 / 35.2, 10 of 1500 9.9 / 10.4
+//   many rows, W = 64, 4500 slots 1 / 4 / 8 / 16: 94.9 / 41.6 / 37.3 / 37.1, 1000 1 / 2: 24.8 / 28.1; W = 128 of 1000 1 / 2 / 4: 25.4 / 30.5 / 31.4; W = 256 of 4500
+//     1 / 2 / 4: 97.8 / 84.7 / 84.4, of 1000 25.6 / 33.2 / 33.2; W = 16 of 16000 8 / 16 / 31: 50.9 / 35.4 / 36.4
 ChunkPlan chunk_plan(const dynts_config &c, int n_tokens, int slots) {
   ChunkPlan pl;
   const long long R = (long long)n_tokens * (c.n_q_heads / c.n_kv_heads), units = (long long)c.batch * c.n_kv_heads;
   const long long F = units * ((R + dynts::kFewRows - 1) / dynts::kFewRows), W = units * ((R + dynts::kChRows - 1) / dynts::kChRows);
-  const bool wide_head = c.head_dim == 128;
-  pl.few = R <= dynts::kFewRows || (F <= (wide_head ? 256 : 512) && (R <= 2 * dynts::kFewRows || F * slots <= (wide_head ? 1 << 20 : 1 << 19)));
+  pl.few = R <= dynts::kFewRows || (F <= (c.head_dim == 128 ? 256 : 512) && (R <= 2 * dynts::kFewRows || F * slots <= 1 << 20));
   pl.rows = pl.few ? dynts::kFewRows : dynts::kChRows;
   pl.blocks = (int)((R + pl.rows - 1) / pl.rows);
   pl.Rpad = pl.blocks * pl.rows;
@@ -67,11 +67,12 @@ ChunkPlan chunk_plan(const dynts_config &c, int n_tokens, int slots) {
   if (pl.few) {
     shares = shares < 16 ? shares : 16;
     shares = shares < 256 / F ? shares : 256 / F;
-    if (slots < 1536 || shares < 3) shares = 1;
+    if (shares < 3 && units > 64) shares = 1;
   } else {
     shares = shares < 32 ? shares : 32;
     shares = shares < 512 / W ? shares : 512 / W;
   }
+  if (slots < 1536) shares = 1;
   while (shares > 1 && units * pl.Rpad * shares > kMostPartials) --shares;
   pl.n_split = shares < 1 ? 1 : (int)shares;
   size_t off = align_up((size_t)c.batch * sizeof(int32_t));
@@ -158,9 +159,10 @@ int launch_append(const ChunkCache &c, const uint16_t *k_new, const uint16_t *v_
   return launch_status();
 }
 
-// workgroups of `blocks` a unit, units rounded up to the 8 XCDs; 0 if a grid cannot hold their threads (2^32)
+// workgroups of `blocks` a unit as chunk_map has them, units rounded up to the 8 XCDs; 0 if a grid cannot hold their threads (2^32)
 unsigned chunk_grid(const ChunkCache &c, long long blocks, int threads) {
-  const long long wgs = blocks * (((long long)c.Nb * c.Hkv + 7) / 8 * 8);
+  const long long units = (long long)c.Nb * c.Hkv, share = units > 4 ? 1 : units > 2 ? 2 : 8 / units;  // XCDs of a unit
+  const long long wgs = (blocks + share - 1) / share * ((units + 7) / 8 * 8);
   return wgs >= (1LL << 32) / threads ? 0u : (unsigned)wgs;
 }
 unsigned attend_grid(const ChunkCache &c, const ChunkPlan &pl) {

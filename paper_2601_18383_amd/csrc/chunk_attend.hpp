@@ -58,13 +58,20 @@ struct ChunkAttendParams {
 
 constexpr int kShareTiles = 16;  // least tiles of 32 slots in a share
 
-// Workgroup to unit and block: a unit's blocks on one XCD, as sb_map has them, but block by block through `group` units at a time, so that those that have least
+// Workgroup to unit and block: a unit's blocks on one XCD (four units and fewer: on 8 / units of them, or XCDs would be idle; 256 rows of 2 units on 16000 slots
+// 23 us instead of 56), block by block through `group` units at a time, so that those that have least
 // to do (the first rows, the last slots) come last and fill what the others leave.  Attention, 4 units: 1024 tokens of 8 sequences, 32 heads on 8, 73 us
 // instead of 82, 512 of 8 25 instead of 32, of 64 198 instead of 206.  (8 units 74, 29 and 206; all of them 74, 29 and 243: then the blocks that wait for HBM no longer
 // run beside those that compute.)  Scores, all units: 2000 tokens of 16 sequences 297 us instead of 425, 1024 of 16 (28 on 4) on 2464 slots 380 instead of 474, 512 of
 // 64 676 instead of 661.
 __device__ __forceinline__ bool chunk_map(int group, int n_blk, int n_units, int &unit, int &blk) {
   const int id = blockIdx.x, xcd = id & 7, slot = id >> 3, per_xcd = (n_units + 7) >> 3;
+  if (n_units <= 4) {
+    const int bits = n_units > 2 ? 2 : n_units - 1;
+    unit = xcd & ((1 << bits) - 1);
+    blk = (slot << (3 - bits)) + (xcd >> bits);
+    return unit < n_units && blk < n_blk;
+  }
   group = group < per_xcd ? group : per_xcd;
   const int first = slot / (group * n_blk) * group, left = per_xcd - first, size = left < group ? left : group, rem = slot - first * n_blk;
   blk = rem / size;
@@ -607,7 +614,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void chunk_attend_few_kernel(const 
   const int col = lane & 31, hf = lane >> 5, r16 = lane & 15;
   int unit, blk;
   const int n_blk = (p.T * c.G + kFewRows - 1) / kFewRows;
-  if (!sb_map(n_blk * p.n_split, c.Nb * c.Hkv, unit, blk)) return;
+  if (!chunk_map(1, n_blk * p.n_split, c.Nb * c.Hkv, unit, blk)) return;
   const int split = blk / n_blk;  // (the blocks of one share side by side: they read the same keys)
   blk -= split * n_blk;
   const int b = unit / c.Hkv, h = unit - b * c.Hkv;

@@ -297,7 +297,7 @@ __global__ __launch_bounds__(kCfWaves * 64, 2) void chunk_scores_few_kernel(cons
   __shared__ float sm_sum[kCfWaves][kCfKeys];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, hf = lane >> 5;
   int unit, blk;
-  if (!sb_map((c.cap + kCfKeys - 1) / kCfKeys, c.Nb * c.Hkv, unit, blk)) return;
+  if (!chunk_map(1, (c.cap + kCfKeys - 1) / kCfKeys, c.Nb * c.Hkv, unit, blk)) return;
   const int b = unit / c.Hkv, h = unit - b * c.Hkv;
   int n;
   const int m = chunk_tokens(c, p.n_new, p.T, b, n);
