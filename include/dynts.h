@@ -328,7 +328,7 @@ int dynts_predict_scores(const dynts_predictor *w, const uint16_t *h, int32_t ba
 
 /* What is done to the logits of a chunk, in this order (s the scaled product of a query at position p and a key at
  * position j; positions are those of the `pos` array, not slots: evictions leave gaps in them):
- *   softcap > 0      s = softcap * tanh(s / softcap)
+ *   softcap > 0      s = softcap * tanh(s / softcap), off by 6 * 2^-24 of softcap at most (a cap far above the logits costs their accuracy)
  *   slope            s = s - slope[hq] * |p - j|
  *   hidden keys      s = -inf unless max(first[b][i], p - window + 1) <= j <= last[b][i]
  * first, last: positions token i of the chunk sees from and up to (`last` may lie behind the token's own position: a

@@ -232,7 +232,7 @@ __device__ __forceinline__ int chunk_lds_v(int row, int piece) {
 }
 
 // Bound by instruction issue and by the clock that the matrix cores leave: 2048 queries on 16384 slots, 32 heads on 8 of 128, 584 GFLOP in 517 us, 1.13
-// PFLOP/s (a product of 8192 x 8192 x 8192 reaches 1.27); the matrix cores are busy 59 % of the cycles, at 1.75 GHz.  Short prompts by HBM: 512
+// PFLOP/s (a product of 8192 x 8192 x 8192 reaches 1.27); the matrix cores are busy 57 % of the cycles, at 1.8 GHz.  Short prompts by HBM: 512
 // tokens of 64 sequences into an empty cache move 0.8 GB in 235 us.
 //   Three workgroups a compute unit (168 registers): with two and twice the rows a wave 640 us, with the next tile's products among a tile's weights 551.
 //   Tiles by loads straight to LDS: through registers there is no room for three workgroups (1610 us, spilled).

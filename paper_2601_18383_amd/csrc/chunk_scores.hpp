@@ -8,7 +8,7 @@
 // those that see none skip the products.
 //
 // Bound by instruction issue (one exponential a 256 operations, twice the density of the attention) and the clock: 512 tokens of 32 sequences on 2464
-// slots, 28 heads on 4 of 128, 320 GFLOP in 347 us; the matrix cores are busy 37 % of the cycles, the vector units 51 %.  Two chunks a
+// slots, 28 heads on 4 of 128, 320 GFLOP in 347 us; the matrix cores are busy 43 % of the cycles, the vector units 59 %.  Two chunks a
 // barrier: 343 us instead of 353 with one; with a bias, where registers are short, 263 with one instead of 278 (16 of these sequences).  Rows' addresses
 // stepped instead of computed: 1 % faster for 6 registers, left out.
 #pragma once
