@@ -335,6 +335,55 @@ def test_chunks_among_single_steps_and_triggers(B, layout, Hq, Hkv, d):
 
 
 @pytest.mark.parametrize("layout", ["dense", "paged"])
+@pytest.mark.parametrize("Hq,Hkv,d", [(8, 2, 64), (28, 4, 128)])
+@pytest.mark.parametrize("T", [3, 40])
+@pytest.mark.parametrize("hinted", [False, True])
+def test_a_chunk_while_an_update_is_owed(B, layout, Hq, Hkv, d, T, hinted):
+    """A step's score update applied before a chunk, or behind it: by dynts_update_scores, by the next step, or by a trigger (for which the step
+    may have kept its logits)."""
+    gen = torch.Generator().manual_seed(21)
+    Nb, M, n0 = 3, 8, 150
+    cap = n0 + T + 4
+    mk = lambda: (B.Cache if layout == "dense" else B.PagedCache)(1, Nb, Hq, Hkv, d, cap, 60, 10, 1)
+    K0, V0 = _rand(gen, Nb, Hkv, n0, d).to(DEV), _rand(gen, Nb, Hkv, n0, d).to(DEV)
+    q, k, v = (_rand(gen, Nb, T, h, d).to(DEV) for h in (Hq, Hkv, Hkv))
+    qs, ks, vs = (_rand(gen, 2, Nb, h, d).to(DEV) for h in (Hq, Hkv, Hkv))
+
+    def run(at_once, end):
+        c = mk()
+        B.dynts_prefill(c.ctx, 0, K0, V0, torch.full((Nb,), n0, dtype=torch.int32, device=DEV))
+        c.n_prompt.fill_(M)
+        c.S[:, :, :, M:] = 0
+        o, out = torch.zeros((Nb, Hq, d), device=DEV), torch.zeros((Nb, T, Hq, d), dtype=torch.bfloat16, device=DEV)
+        scratch = torch.empty(B.dynts_chunk_scratch_bytes(c.cfg, T), dtype=torch.uint8, device=DEV)
+        if hinted:
+            B.dynts_hint_trigger(c.ctx, 0)
+        B.dynts_decode_step(c.ctx, 0, qs[0], ks[0], vs[0], o)
+        if at_once:
+            B.dynts_update_scores(c.ctx, 0)
+        B.dynts_chunk_step(c.ctx, 0, q, k, v, out, scratch)
+        if end == "step":
+            B.dynts_decode_step(c.ctx, 0, qs[1], ks[1], vs[1], o)
+        if end == "trigger":
+            B.dynts_select_evict(c.ctx, 0, c.keep_idx, c.new_len)
+        else:
+            B.dynts_update_scores(c.ctx, 0)
+        assert int(c.status.item()) == 0
+        n = int(c.seq_len[0, 0].item())
+        return c.S[0, :, :, :n].clone(), o, out
+
+    for end in ("update", "step", "trigger"):
+        (S, o, out), (S2, o2, out2) = run(True, end), run(False, end)
+        assert torch.equal(out, out2) and torch.allclose(o, o2, rtol=0, atol=1e-5)
+        assert torch.all(S[:, :, :M] == math.inf) and torch.all(S2[:, :, :M] == math.inf)
+        # (two or three sums of numbers below G * T in another order: a half step each of what they add up to, and the weights of a step, formed
+        # again from kept logits or K, a few half steps of theirs)
+        assert torch.allclose(S[:, :, M:], S2[:, :, M:], rtol=2e-6, atol=2e-6), float((S[:, :, M:] - S2[:, :, M:]).abs().max())
+        # mass: every row of the step, of the chunk and of the last step gives away what the question slots do not take
+        assert float(S2[:, :, M:].sum()) > 0.5 * Nb * Hq * (T + 1)
+
+
+@pytest.mark.parametrize("layout", ["dense", "paged"])
 def test_question_in_chunks(B, layout):
     """A question in three chunks into an empty cache: the same cache as dynts_prefill leaves, and a question behind thinking
     tokens is refused."""
