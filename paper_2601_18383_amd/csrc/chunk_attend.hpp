@@ -428,7 +428,7 @@ __global__ __launch_bounds__(kChThreads, D == 128 ? 3 : 4) void chunk_attend_ker
       const int first = __builtin_amdgcn_readfirstlane(tp[0]), last = __builtin_amdgcn_readfirstlane(tp[kChTile - 1]);
       if (BIASED) {
         const float c = capped ? 1.f : p.scale_log2;
-        if (last - first == kChTile - 1 && last <= own_lo) {  // positions without gaps, none behind a row's own
+        if (t + kChTile <= n && last - first == kChTile - 1 && last <= own_lo) {  // 32 positions without gaps, none behind a row's own
           const float bias = -slope * (float)(own - first - 4 * hf);
 #pragma unroll
           for (int e = 0; e < 16; ++e) s[e] = fmaf(s[e], c, fmaf(slope, (float)(8 * (e >> 2) + (e & 3)), bias));

@@ -201,6 +201,24 @@ def test_shaped_without_gaps(B, kind, Hq, Hkv, d, n_old, n_new):
     c.check(kind, lse=c.lse, recv=dst, **s)
 
 
+@pytest.mark.parametrize("layout", ["dense", "paged"])
+@pytest.mark.parametrize("missing", [1, 3, 5])
+def test_gaps_that_make_up_for_a_short_tile(B, layout, missing):
+    """The last tile has 29 slots, whose positions span 29 + missing: with 3 as many as a whole tile without gaps."""
+    c = Case(B, layout, 32, 2, 128, [54] * 33, [7] * 33, seed=17, qscale=0.5)
+    for b in range(33):
+        c.pos[b] = c.pos[b] + missing * (torch.arange(61) >= 40).to(torch.int32)
+    c.next = [n + missing for n in c.next]
+    c.fill(True)
+    s = _shapings(c, c.gen, "slope")
+    sh = B.Shaping(slope=s["slope"].to(DEV))
+    dst = torch.full((33, 2, c.cap), 7.0, dtype=torch.float32, device=DEV)
+    q = c.q.to(DEV)
+    B.dynts_chunk_attend(c.cache.ctx, 0, q, c.out, c.scratch, lse=c.lse, n_new=c.n, shaping=sh)
+    B.dynts_chunk_scores(c.cache.ctx, 0, q, c.lse, dst=dst, accumulate=False, n_new=c.n, shaping=sh)
+    c.check("slope", lse=c.lse, recv=dst, **s)
+
+
 def test_keys_hidden_from_all_may_be_anything(B):
     """K rows of another document that hold NaN and infinities, and what lies behind the length in the cache."""
     c = Case(B, "dense", 8, 2, 64, [100], [70], seed=3).fill(True)
