@@ -252,17 +252,16 @@ __global__ __launch_bounds__(kChThreads, D == 128 ? 3 : 4) void chunk_attend_ker
   const int col = lane & 31, hf = lane >> 5, r16 = lane & 15;
   int unit, blk;
   const int n_blk = (p.T * c.G + kChRows - 1) / kChRows;
-  // (documents: which rows see most is not known, and units at once cost: 470 tokens in documents, of 21 sequences on 1571 slots, 28 heads on 4, 74 us unit by
-  // unit, 92 four at a time, 98 with the last rows first)
-  const bool documents = SHAPED && p.shape.first;
-  if (!chunk_map(documents ? 1 : 4, n_blk * p.n_split, c.Nb * c.Hkv, unit, blk)) return;
+  // (documents: which rows see most is not known, and units at once cost: means of eight draws, 470 tokens of 21 sequences on 1571 slots, 28 heads on 4, in
+  // documents 71 us unit by unit, 90 four at a time, 75 two; 4096 of 2, 32 on 8, 102 / 102 / 101; first rows first 76 and 110)
+  if (!chunk_map(SHAPED && p.shape.first ? 1 : 4, n_blk * p.n_split, c.Nb * c.Hkv, unit, blk)) return;
   const int split = blk / n_blk;
   blk -= split * n_blk;
   const int b = unit / c.Hkv, h = unit - b * c.Hkv;
   int n;
   const int m = chunk_tokens(c, p.n_new, p.T, b, n);
   const int R = m * c.G;
-  if (!documents) blk = n_blk - 1 - blk;  // (the last rows see most)
+  blk = n_blk - 1 - blk;  // (the last rows see most)
   if (blk * kChRows >= R) return;
   const int base = n - m;  // the chunk's first slot
 
