@@ -136,6 +136,11 @@ def _ptr(t, dtype=None):
     return t.data_ptr()
 
 
+def _gpu_of(t):
+    """The GPU a tensor lies on, -1 for the host, None for a bare address: nothing is known of those."""
+    return None if isinstance(t, int) else t.get_device()
+
+
 # The current stream's handle without the Stream object around it, which takes longer to make (2.8 us) than a launch; the current
 # device without a check that there is one (tensors of it have been made).
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
@@ -199,6 +204,7 @@ def dynts_bind(ctx, K, V, S, pos, seq_len, next_pos, n_prompt, workspace, status
                           _ptr(pos, torch.int32), _ptr(seq_len, torch.int32), _ptr(next_pos, torch.int32),
                           _ptr(n_prompt, torch.int32), _ptr(workspace), workspace.numel() * workspace.element_size(),
                           _ptr(status, torch.int32)), "dynts_bind")
+    ctx.gpu = _gpu_of(K)
 
 
 def dynts_bind_paged(ctx, K_pool, V_pool, block_table, free_stack, free_top, S, pos, seq_len, next_pos, n_prompt,
@@ -209,7 +215,7 @@ def dynts_bind_paged(ctx, K_pool, V_pool, block_table, free_stack, free_top, S, 
                                 _ptr(seq_len, torch.int32), _ptr(next_pos, torch.int32), _ptr(n_prompt, torch.int32),
                                 _ptr(workspace), workspace.numel() * workspace.element_size(),
                                 _ptr(status, torch.int32)), "dynts_bind_paged")
-    ctx.gpu = K_pool.get_device()
+    ctx.gpu = _gpu_of(K_pool)
 
 
 def dynts_prefill(ctx, layer, K0, V0, m, stream=None):
@@ -496,8 +502,8 @@ def _on_device(owner, *tensors):
             dev = _device()
         if at != dev:
             raise ValueError("tensors have to be on the current GPU (%d, not %d)" % (dev, at))
-    bound = getattr(owner, "gpu", dev)
-    if bound != dev:
+    bound = getattr(owner, "gpu", None)  # (None: bound by addresses, or not by this module)
+    if bound is not None and bound != dev:
         raise ValueError("the cache's arrays or the tables are not on the current GPU (%d, not %d)" % (dev, bound))
 
 
