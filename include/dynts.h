@@ -328,7 +328,8 @@ int dynts_predict_scores(const dynts_predictor *w, const uint16_t *h, int32_t ba
 
 /* What is done to the logits of a chunk, in this order (s the scaled product of a query at position p and a key at
  * position j; positions are those of the `pos` array, not slots: evictions leave gaps in them):
- *   softcap > 0      s = softcap * tanh(s / softcap), off by 6 * 2^-24 of softcap at most (a cap far above the logits costs their accuracy)
+ *   softcap > 0      s = softcap * tanh(s / softcap), off by 6 * 2^-24 of softcap at most up to a softcap of 128, above by 24 * 2^-24 of s
+ *                    (and slower on long chunks; a softcap so small that 3 * scale / softcap overflows is refused)
  *   slope            s = s - slope[hq] * |p - j|
  *   hidden keys      s = -inf unless max(first[b][i], p - window + 1) <= j <= last[b][i]
  * first, last: positions token i of the chunk sees from and up to (`last` may lie behind the token's own position: a

@@ -2,6 +2,7 @@
 // Nothing here allocates device memory or synchronises the host.
 #include "chunk.hpp"
 
+#include <cfloat>
 #include <cmath>
 
 #include "chunk_append.hpp"
@@ -36,7 +37,7 @@ struct ChunkPlan {
 // Rows of partials that the shares of one call may leave.
 constexpr long long kMostPartials = 65536;
 
-// Which kernel, and into how many shares the keys of a row block are cut at most.  slots: how many a token can see.
+// Which kernel, and into how many shares the keys of a row block are cut at most.  slots: how many a token can see; far_cap: only the one for few rows knows it.
 //
 // Few rows, F row blocks of 32, one workgroup a compute unit (two with head_dim 64): a row block is done in 5 + 5.8 us per 1000 slots; many rows, W
 // of 128, three or four a compute unit: 4 + 21 us per 1000 slots.  us, few / many, each with its shares:
@@ -55,11 +56,11 @@ constexpr long long kMostPartials = 65536;
 //     32.0, of 4000 42.9 / 47.5; head_dim 64, 128 units of 6000 1 / 2: 30.8 / 35.2, 10 of 1500 9.9 / 10.4
 //   many rows, W = 64, 4500 slots 1 / 4 / 8 / 16: 94.9 / 41.6 / 37.3 / 37.1, 1000 1 / 2: 24.8 / 28.1; W = 128 of 1000 1 / 2 / 4: 25.4 / 30.5 / 31.4; W = 256 of 4500
 //     1 / 2 / 4: 97.8 / 84.7 / 84.4, of 1000 25.6 / 33.2 / 33.2; W = 16 of 16000 8 / 16 / 31: 50.9 / 35.4 / 36.4
-ChunkPlan chunk_plan(const dynts_config &c, int n_tokens, int slots) {
+ChunkPlan chunk_plan(const dynts_config &c, int n_tokens, int slots, bool far_cap = false) {
   ChunkPlan pl;
   const long long R = (long long)n_tokens * (c.n_q_heads / c.n_kv_heads), units = (long long)c.batch * c.n_kv_heads;
   const long long F = units * ((R + dynts::kFewRows - 1) / dynts::kFewRows), W = units * ((R + dynts::kChRows - 1) / dynts::kChRows);
-  pl.few = R <= dynts::kFewRows || (F <= (c.head_dim == 128 ? 256 : 512) && (R <= 2 * dynts::kFewRows || F * slots <= 1 << 20));
+  pl.few = far_cap || R <= dynts::kFewRows || (F <= (c.head_dim == 128 ? 256 : 512) && (R <= 2 * dynts::kFewRows || F * slots <= 1 << 20));
   pl.rows = pl.few ? dynts::kFewRows : dynts::kChRows;
   pl.blocks = (int)((R + pl.rows - 1) / pl.rows);
   pl.Rpad = pl.blocks * pl.rows;
@@ -91,17 +92,24 @@ ChunkPlan chunk_plan(const dynts_config &c, int n_tokens, int slots) {
   return pl;
 }
 
+// a cap that takes the longer form of soft_caps
+bool far_cap(const dynts_shaping *s) { return s && s->softcap * kLog2E > dynts::kCapNear; }
+
 ChunkPlan chunk_plan(const ChunkCache &c, int n_tokens, const dynts_shaping *shaping = nullptr) {
   dynts_config cfg{};
   cfg.batch = c.Nb; cfg.n_q_heads = c.Hq; cfg.n_kv_heads = c.Hkv; cfg.head_dim = c.D; cfg.capacity = c.cap;
   // (slots of a window: no more than its positions, those of the chunk's other tokens beside them)
   const long long seen = shaping && shaping->window > 0 ? (long long)shaping->window + n_tokens : c.cap;
-  return chunk_plan(cfg, n_tokens, (int)(seen < c.cap ? seen : c.cap));
+  return chunk_plan(cfg, n_tokens, (int)(seen < c.cap ? seen : c.cap), far_cap(shaping));
 }
 
-int check_shaping(const dynts_shaping *s) {
+// the factor of a logit's exponent, 2 z log2 e; infinite for a softcap below the smallest normal numbers
+float cap_in(float softcap, float scale) { return 2.f * kLog2E * scale / softcap; }
+
+int check_shaping(const dynts_shaping *s, float scale) {
   if (!s) return DYNTS_OK;
   if (!(s->softcap >= 0.f) || std::isinf(s->softcap) || s->window < 0) return DYNTS_EINVAL;
+  if (s->softcap > 0.f && std::isinf(cap_in(s->softcap, scale))) return DYNTS_EINVAL;
   if (misaligned(s->slope, 4) || misaligned(s->first, 4) || misaligned(s->last, 4)) return DYNTS_EINVAL;
   return DYNTS_OK;
 }
@@ -110,13 +118,14 @@ uint32_t group_magic(int G) { return G == 1 ? 0u : (uint32_t)(((1ull << 32) + G 
 
 bool shaped(const dynts_shaping *s) { return s && (s->softcap > 0.f || s->window > 0 || s->slope || s->first || s->last); }
 bool shaped(const dynts::ChunkShape &s) { return s.cap > 0.f || s.window > 0 || s.slope || s.first || s.last; }
-
 dynts::ChunkShape chunk_shape(const dynts_shaping *s, float scale) {
   dynts::ChunkShape out{};
   if (!s) return out;
   if (s->softcap > 0.f) {
-    out.cap = s->softcap * kLog2E;
-    out.cap_in = 2.f * kLog2E * scale / s->softcap;
+    out.cap = std::fmin(s->softcap * kLog2E, FLT_MAX);
+    out.cap_in = cap_in(s->softcap, scale);
+    // (scale / softcap, or what is still not 0: then z is, and the logit stays as it is)
+    if (far_cap(s)) out.far_in = std::fmax(scale / s->softcap, FLT_MIN);
   }
   out.window = s->window;
   out.slope = s->slope;
@@ -173,7 +182,8 @@ unsigned attend_grid(const ChunkCache &c, const ChunkPlan &pl) {
 //   head_dim 128: C = 66, W = 168 21.9 / 60.4, W = 672 60.9 / 61.5; C = 219, W = 152 57.0 / 170, W = 512 97.6 / 184; C = 389, W = 432 100 / 304; C = 112,
 //     W = 752 93.1 / 92.2, W = 1504 183 / 122; C = 14, W = 640 26.3 / 16.8; C = 2, W = 568 14.5 / 5.9
 //   head_dim 64: C = 164, W = 78 23.1 / 128; C = 10, W = 64 6.0 / 10.9; C = 38, W = 288 15.7 / 29.8, W = 1152 38.2 / 40.2
-bool scores_few(const ChunkCache &c, int n_tokens) {
+bool scores_few(const ChunkCache &c, int n_tokens, const dynts_shaping *shaping) {
+  if (far_cap(shaping)) return true;  // (the other one does not know it)
   const long long W = (long long)c.Nb * c.Hkv * ((c.cap + dynts::kCfKeys - 1) / dynts::kCfKeys);
   const long long C = ((long long)n_tokens * c.G + dynts::kSbChunk - 1) / dynts::kSbChunk;
   return W <= 256 ? C >= 8 : W <= 512 && C >= 32;
@@ -238,7 +248,7 @@ int launch_scores(const ChunkCache &c, const uint16_t *q, int n_tokens, const in
                   float *dst, int accumulate, hipStream_t st) {
   const dynts::ChunkScoreParams p{c, q, n_new, lse, dst ? dst : c.S, chunk_shape(shaping, c.scale), n_tokens, dst ? 0 : 1, accumulate ? 1 : 0,
                                   c.scale * kLog2E, group_magic(c.G)};
-  const bool few = scores_few(c, n_tokens);
+  const bool few = scores_few(c, n_tokens, shaping);
   const unsigned grid = scores_grid(c, few);
   if (!grid) return DYNTS_EINVAL;
   if (c.D == 128) launch_scores_d<128>(p, few, grid, st);
@@ -274,7 +284,7 @@ int dynts_chunk_attend(dynts_ctx *ctx, int32_t layer, const uint16_t *q, int32_t
   ChunkCache c;
   int rc = dynts::chunk_cache(ctx, layer, &c);
   if (rc == DYNTS_OK) rc = check_tokens(n_tokens);
-  if (rc == DYNTS_OK) rc = check_shaping(shaping);
+  if (rc == DYNTS_OK) rc = check_shaping(shaping, c.scale);
   if (rc != DYNTS_OK) return rc;
   if (!q || !out) return DYNTS_ENULL;
   if (misaligned(q, 16) || misaligned(out, 16)) return DYNTS_EINVAL;
@@ -290,7 +300,7 @@ int dynts_chunk_scores(dynts_ctx *ctx, int32_t layer, const uint16_t *q, int32_t
   ChunkCache c;
   int rc = dynts::chunk_cache(ctx, layer, &c);
   if (rc == DYNTS_OK) rc = check_tokens(n_tokens);
-  if (rc == DYNTS_OK) rc = check_shaping(shaping);
+  if (rc == DYNTS_OK) rc = check_shaping(shaping, c.scale);
   if (rc != DYNTS_OK) return rc;
   if (!q || !lse) return DYNTS_ENULL;
   if (misaligned(q, 16)) return DYNTS_EINVAL;
@@ -303,7 +313,7 @@ int dynts_chunk_step(dynts_ctx *ctx, int32_t layer, const uint16_t *q, const uin
   ChunkCache c;
   int rc = dynts::chunk_cache(ctx, layer, &c);
   if (rc == DYNTS_OK) rc = check_tokens(n_tokens);
-  if (rc == DYNTS_OK) rc = check_shaping(shaping);
+  if (rc == DYNTS_OK) rc = check_shaping(shaping, c.scale);
   if (rc == DYNTS_OK) rc = check_append(c, k_new, v_new, s_new, question);
   if (rc != DYNTS_OK) return rc;
   if (!q || !out) return DYNTS_ENULL;
@@ -314,7 +324,7 @@ int dynts_chunk_step(dynts_ctx *ctx, int32_t layer, const uint16_t *q, const uin
   hipStream_t st = static_cast<hipStream_t>(stream);
   int32_t *taken = static_cast<int32_t *>(scratch);
   const bool scores = c.score_mode == DYNTS_SCORE_ACCUMULATE && !question;
-  if (!attend_grid(c, pl) || (scores && !scores_grid(c, scores_few(c, n_tokens)))) return DYNTS_EINVAL;  // (before the append)
+  if (!attend_grid(c, pl) || (scores && !scores_grid(c, scores_few(c, n_tokens, shaping)))) return DYNTS_EINVAL;  // (before the append)
   const size_t row = (size_t)c.Nb * n_tokens * c.D * 2, q_bytes = row * c.Hq, k_bytes = row * c.Hkv;
   if (overlap(out, q_bytes, q, q_bytes) || overlap(out, q_bytes, k_new, k_bytes) || overlap(out, q_bytes, v_new, k_bytes)) return DYNTS_EINVAL;
   if (scores && !lse) lse = reinterpret_cast<float *>(static_cast<char *>(scratch) + pl.off_lse);

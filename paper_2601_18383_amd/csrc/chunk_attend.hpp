@@ -29,6 +29,7 @@ namespace dynts {
 // dynts_shaping in log2 units
 struct ChunkShape {
   float cap, cap_in;      // softcap * log2 e, or 0; 2 * log2 e * scale / softcap
+  float far_in;           // scale / softcap where the cap lies above kCapNear, else 0
   int window;             // 0: none
   const float *slope;     // [Hq] or null
   const int32_t *first, *last;  // [Nb][T] or null
@@ -207,6 +208,29 @@ __device__ __forceinline__ void chunk_range(const ChunkShape &s, const int32_t *
 // tokens of 16 on 2464 slots, 28 on 4, 346 and so 307).
 __device__ __forceinline__ float soft_cap(float dot, const ChunkShape &s) {
   return fmaf(-2.f * s.cap, __builtin_amdgcn_rcpf(1.f + fast_exp2(dot * s.cap_in)), s.cap);
+}
+// The same for a cap that may lie far above the logits, whose bits that form loses: where |z| < 0.3 the logit times the series of tanh(z) / z, to z^8 (the next
+// term is half a step of 2^-24), elsewhere cap * (1 - 2 / (1 + e^(2 z))); off by 24 half steps of the logit at most.
+__device__ __forceinline__ float soft_cap_far(float dot, float scale_log2, const ChunkShape &s) {
+  const float z = dot * s.far_in, t = z * z;
+  const float series = fmaf(t, fmaf(t, fmaf(t, fmaf(t, 62.f / 2835.f, -17.f / 315.f), 2.f / 15.f), -1.f / 3.f), 1.f);
+  const float whole = s.cap * fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + fast_exp2(dot * s.cap_in)), 1.f);
+  return fabsf(z) < 0.3f ? dot * scale_log2 * series : whole;
+}
+// Caps up to here (log2 units: a softcap of 128) take the short form, whose error is 2^-14 then; above, a logit costs fifteen operations.  FAR: a kernel that
+// knows both; those for few rows and few slots do, which far caps take at every size.  (Code for both cost the others registers: with a window scores 160 us
+// instead of 149, capped 319 instead of 309, attention 336 instead of 332; in the forms with a bias alone, scores 263 instead of 253, attention 90.7 instead of 89.0.  A far cap takes attention of 2048 tokens of 8 sequences, 32 heads
+// on 8, 1070 us, scores of 512 of 16 on 2464 slots, 28 on 4, 590.)
+constexpr float kCapNear = 128.f * 1.4426950408889634f;
+template <bool FAR>
+__device__ __forceinline__ void soft_caps(f32x16 &x, float scale_log2, const ChunkShape &s) {
+  if (!FAR || s.far_in == 0.f) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[e] = soft_cap(x[e], s);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[e] = soft_cap_far(x[e], scale_log2, s);
+  }
 }
 
 // Eight neighbouring elements of an output row, and its lse, from their unnormalised values, shift and sum.
@@ -420,10 +444,7 @@ __global__ __launch_bounds__(kChThreads, D == 128 ? 3 : 4) void chunk_attend_ker
   const float scale = capped || BIASED ? 1.f : p.scale_log2;
   auto shape = [&](f32x16 &s, int t, const int *tp) {
     if (SHAPED) {
-      if (capped) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) s[e] = soft_cap(s[e], p.shape);
-      }
+      if (capped) soft_caps<false>(s, p.scale_log2, p.shape);
       const int first = __builtin_amdgcn_readfirstlane(tp[0]), last = __builtin_amdgcn_readfirstlane(tp[kChTile - 1]);
       if (BIASED) {
         const float c = capped ? 1.f : p.scale_log2;
@@ -708,11 +729,13 @@ __global__ __launch_bounds__(kFewThreads, 2) void chunk_attend_few_kernel(const 
       s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], s, 0, 0, 0);
     }
     float mx = -INFINITY;
+    const bool capped = SHAPED && p.shape.cap > 0.f;
+    if (capped) soft_caps<true>(s, p.scale_log2, p.shape);
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
       const int key = 8 * (e >> 2) + 4 * hf + (e & 3);
       if (SHAPED) {
-        float x = p.shape.cap > 0.f ? soft_cap(s[e], p.shape) : s[e] * p.scale_log2;
+        float x = capped ? s[e] : s[e] * p.scale_log2;
         const int kp = sm_pos[wave][key];
         x -= slope * fabsf(at - (float)(kp - ref));
         s[e] = (uint32_t)(kp - lo) <= span ? x : -INFINITY;

@@ -123,8 +123,8 @@ __device__ __forceinline__ void chunk_sees(const ChunkRows<SHAPED, BIASED, ROWS>
   }
 }
 
-// The weights of a chunk's products, added to the lane's sums.  r0: the chunk's first row among `rows`.
-template <bool SHAPED, bool BIASED, int ROWS>
+// The weights of a chunk's products, added to the lane's sums.  r0: the chunk's first row among `rows`.  FAR: as in soft_caps.
+template <bool FAR, bool SHAPED, bool BIASED, int ROWS>
 __device__ __forceinline__ void chunk_add(float (&sum)[kSbTiles], f32x16 (&acc)[kSbTiles], const ChunkRows<SHAPED, BIASED, ROWS> &rows, const ChunkScoreParams &p,
                                           const int (&kpos)[kSbTiles], int r0, bool all, int hf) {
   f32x4 ml[4];  // of the rows 8 j + 4 hf .. +3 that this lane's products belong to
@@ -134,9 +134,7 @@ __device__ __forceinline__ void chunk_add(float (&sum)[kSbTiles], f32x16 (&acc)[
   if (SHAPED && p.shape.cap > 0.f) {
     scale = 1.f;
 #pragma unroll
-    for (int kt = 0; kt < kSbTiles; ++kt)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) acc[kt][e] = soft_cap(acc[kt][e], p.shape);
+    for (int kt = 0; kt < kSbTiles; ++kt) soft_caps<FAR>(acc[kt], p.scale_log2, p.shape);
   }
   if (BIASED) {
 #pragma unroll
@@ -256,7 +254,7 @@ __global__ __launch_bounds__(kSbWaves * 64, D == 128 || SHAPED ? 3 : 4) void chu
     if (__builtin_amdgcn_readfirstlane((int)(any && has_keys))) {
       f32x16 acc[kSbTiles];
       sb_multiply<D>(acc, q, kf, col, hf);
-      chunk_add(sum, acc, rows, p, kpos, in_group * kSbChunk, __builtin_amdgcn_readfirstlane((int)all), hf);
+      chunk_add<false>(sum, acc, rows, p, kpos, in_group * kSbChunk, __builtin_amdgcn_readfirstlane((int)all), hf);
     }
   };
   int buf = 0;
@@ -345,7 +343,7 @@ __global__ __launch_bounds__(kCfWaves * 64, 2) void chunk_scores_few_kernel(cons
       for (int ks = 0; ks < D / 16; ++ks)
 #pragma unroll
         for (int kt = 0; kt < kSbTiles; ++kt) acc[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[ks], kf[kt][ks], acc[kt], 0, 0, 0);
-      chunk_add(sum, acc, rows, p, kpos, 0, __builtin_amdgcn_readfirstlane((int)all), hf);
+      chunk_add<true>(sum, acc, rows, p, kpos, 0, __builtin_amdgcn_readfirstlane((int)all), hf);
     }
     wave_lds_fence();
   };
