@@ -655,16 +655,15 @@ __global__ __launch_bounds__(kFewThreads, 2) void chunk_attend_few_kernel(const 
 
   const int32_t *pos = c.pos + (size_t)unit * c.cap;
   const int lim = base + i;
-  int lo = 0, ref = 0;
+  int lo = 0, own = 0;
   uint32_t span = 0;
-  float at = 0.f, slope = 0.f;
+  float slope = 0.f;
   int t_lo = 0, t_hi;
   const int i0 = chunk_token(row0, p.g_magic), i1 = chunk_token(row0 + kFewRows - 1 < R ? row0 + kFewRows - 1 : R - 1, p.g_magic);
   if (SHAPED) {
-    const int own = pos[base + i], head = pos[0], tail = pos[n - 1];
+    const int head = pos[0], tail = pos[n - 1];
+    own = pos[base + i];
     chunk_interval(p.shape, (size_t)b * p.T + i, own, lo, span);
-    ref = __builtin_amdgcn_readfirstlane(pos[base]);
-    at = (float)(own - ref);
     if (p.shape.slope) slope = p.shape.slope[h * c.G + g] * 1.4426950408889634f;
     // the slots that some row sees (every wave has all rows)
     int first = lo, last = lo == kNowhere ? -1 : (int)(lo + span);
@@ -737,7 +736,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void chunk_attend_few_kernel(const 
       if (SHAPED) {
         float x = capped ? s[e] : s[e] * p.scale_log2;
         const int kp = sm_pos[wave][key];
-        x -= slope * fabsf(at - (float)(kp - ref));
+        x -= slope * fabsf((float)(own - kp));
         s[e] = (uint32_t)(kp - lo) <= span ? x : -INFINITY;
       } else {
         s[e] = t + key <= lim ? s[e] * p.scale_log2 : -INFINITY;
