@@ -487,7 +487,7 @@ __global__ __launch_bounds__(kChThreads, D == 128 ? 3 : 4) void chunk_attend_ker
     }
     return (q[0] + q[1]) + (q[2] + q[3]);
   };
-  // the shift that takes the tile's largest logit to 1 or 2, if it is above the one at hand
+  // the shift that takes the weight of the tile's largest logit to between 1/2 and 1, if it is above the one at hand
   auto above = [&](const f32x16 &s) {
     float mx = s[0];
 #pragma unroll
@@ -753,7 +753,8 @@ __global__ __launch_bounds__(kFewThreads, 2) void chunk_attend_few_kernel(const 
     for (int e = 0; e < 16; ++e) {
       const float w = fast_exp2(s[e] - m_use);
       sum += w;
-      pf[e >> 3][e & 7] = (__bf16)w;
+      pf[e >> 3][e & 7] = (__bf16)w;  // (half a step of 2^-8, as the output's rounding; with the low part as well, as single steps have it, drafts of four
+                                      // tokens 29.5 us instead of 28.4, 175 rows of 4 units on 16000 slots 27.2 instead of 24.8)
     }
     l_run = l_run * corr + sum;
     park(sv, vr);
