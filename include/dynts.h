@@ -315,16 +315,18 @@ int dynts_predict_scores(const dynts_predictor *w, const uint16_t *h, int32_t ba
 /* ---- chunks of new tokens ----------------------------------------------------------------------------------------
  * Several new tokens of every sequence at once: a prompt, the next question, a tool's answer, drafted tokens to be
  * checked, a known answer that is scored.  A chunk of m tokens is what m single steps are (Eq. attn-score, Eq. attn-o,
- * Eq. importance-score): every token enters the cache, attends to what is there and to itself, and its attention
- * weights are added to the scores of the thinking slots; but K and V are read once a chunk.  Dense and paged layouts.
+ * Eq. importance-score), up to the roundings below: every token enters the cache, attends to what is there and to itself, and its
+ * attention weights are added to the scores of the thinking slots; but K and V are read once a chunk.  Dense and paged layouts.
  *   n_tokens: tokens of the longest chunk, the row count of the arrays, 1 <= n_tokens <= 2^20.
  *   n_new int32 [Nb] or NULL (= n_tokens each): tokens of each sequence (clamped to [0, n_tokens]); the rows behind
- *     them are padding, not read as keys or written as outputs.  A sequence with none is left alone.
+ *     them are padding, not read as keys or written as outputs.  A sequence with none is left alone: no output of any of these
+ *     calls is written for it, the dst of dynts_chunk_scores neither, whatever `accumulate` says.
  *   scratch: >= dynts_chunk_scratch_bytes(cfg, n_tokens) bytes of device memory, 256-byte aligned, contents irrelevant
  *     before and after (what serves a chunk serves every smaller one; it may be shared by calls that are
  *     stream-ordered with respect to each other).
- * Arrays that are written overlap no other argument.  Outputs are bf16, as what a projection reads next; the weights are rounded to bf16 for their product with V, sums,
- * products and statistics are fp32. */
+ * Arrays that are written overlap no other argument.  Outputs are bf16, as what a projection reads next, and the weights are rounded to bf16 for their
+ * product with V, half a step of 2^-8 each (a single step keeps 16 bits of a weight and returns fp32); sums, products, statistics and the weights that
+ * slots receive are fp32. */
 
 /* What is done to the logits of a chunk, in this order (s the scaled product of a query at position p and a key at
  * position j; positions are those of the `pos` array, not slots: evictions leave gaps in them):
@@ -335,7 +337,9 @@ int dynts_predict_scores(const dynts_predictor *w, const uint16_t *h, int32_t ba
  * first, last: positions token i of the chunk sees from and up to (`last` may lie behind the token's own position: a
  * prefix whose tokens see each other; `first` at the start of a document keeps documents apart).  Positions are taken to
  * be 0 or more and below 2^31 - 1.  A token that sees nothing gets zeros and lse = -inf.  Rows of V that are hidden from a token have
- * to be finite; rows of K need not.  n_tokens = 1 is the form for single tokens. */
+ * to be finite; rows of K need not.
+ * n_tokens = 1 is the form for single tokens, and the only one: dynts_decode_step, dynts_decode_loop and dynts_score_block know no shaping.  A model that
+ * has one pays a score launch a token, and has no runs of steps and no logits kept for a trigger. */
 typedef struct dynts_shaping {
   float softcap;        /* 0: none */
   int32_t window;       /* positions a token sees, its own the last of them; 0: all */
@@ -375,7 +379,11 @@ int dynts_chunk_scores(dynts_ctx *ctx, int32_t layer, const uint16_t *q, int32_t
                        const dynts_shaping *shaping, const float *lse, float *dst, int32_t accumulate, void *stream);
 
 /* A chunk's whole step: dynts_chunk_append, dynts_chunk_attend and, unless the tokens are question slots or scores come from outside,
- * dynts_chunk_scores into S.  A sequence whose chunk does not fit is left alone in all of them. */
+ * dynts_chunk_scores into S.  A sequence whose chunk does not fit is left alone in all of them.
+ * The weights of all its tokens are in S then, and stay there.  Drafted tokens that may be dropped again take the parts instead: dynts_chunk_append and
+ * dynts_chunk_attend; then dynts_compact with the slots that stay (it gives a paged sequence's pages back, which a smaller seq_len alone would lose; a
+ * score update owed by a single step has to be applied before), next_pos[b] reduced by the number dropped; then dynts_chunk_scores with the same q and
+ * lse and n_new = the number that stays. */
 int dynts_chunk_step(dynts_ctx *ctx, int32_t layer, const uint16_t *q, const uint16_t *k_new, const uint16_t *v_new,
                      const float *s_new, int32_t n_tokens, const int32_t *n_new, int32_t question,
                      const dynts_shaping *shaping, uint16_t *out, float *lse, void *scratch, size_t scratch_bytes,

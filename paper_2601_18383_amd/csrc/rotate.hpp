@@ -2,8 +2,8 @@
 //   a' = a cos theta - b sin theta,   b' = b cos theta + a sin theta;
 // the gradient with respect to the input is the turn back, by -theta.
 //
-// Bound by HBM: every element is read and written once.  8192 tokens of 40 heads of 128, 168 MB in 25 us (6.7 TB/s, part of it out of the memory-side
-// cache).  A token a workgroup: its angles are computed once, in LDS, for all heads.  Small calls are a launch, 3 us.
+// Bound by HBM: every element is read and written once.  8192 tokens of 40 heads of 128, 168 MB in 32 us (5.2 TB/s, a large copy's rate), on the same arrays
+// again in 25 (part of it out of the memory-side cache).  A token a workgroup: its angles are computed once, in LDS, for all heads.  Small calls are a launch, 3 us.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
