@@ -21,7 +21,8 @@
  *    would overflow `capacity`) are latched into the bound `status` word: bit 0 = an
  *    append was dropped because the cache was full; bit 1 (value 2) = keep_idx too short for a sequence
  *    (dynts_select_evict left it alone); bit 2 (value 4) = the page pool of the paged layout ran dry; bit 3
- *    (value 8) = a chunk of question tokens behind thinking tokens (dynts_chunk_append).
+ *    (value 8) = a chunk of question tokens behind thinking tokens (dynts_chunk_append); bit 4 (value 16) = a leaf that is
+ *    none of its sequence's drafted tokens (dynts_tree_keep).
  *  - Layout (C order, L = n_layers, Nb = batch, Hkv = n_kv_heads, cap = capacity, d = head_dim):
  *      K, V      bf16  [L][Nb][Hkv][cap][d]   rows in position order
  *      S         fp32  [L][Nb][Hkv][cap]      importance score; +inf on question slots
@@ -53,6 +54,7 @@ extern "C" {
 #define DYNTS_EWORKSPACE (-6) /* workspace smaller than dynts_workspace_bytes, or misaligned */
 #define DYNTS_EHIP (-7)       /* the HIP runtime refused a launch */
 #define DYNTS_EPENDING (-8)   /* rows would move while a score update is still deferred */
+#define DYNTS_ECODES (-9)     /* the context's cache holds codes (dynts_bind_codes), the call takes bf16 caches */
 
 #define DYNTS_SCORE_ACCUMULATE 0 /* score = attention received so far (Eq. importance-score) */
 #define DYNTS_SCORE_EXTERNAL 1   /* score supplied at append (the predictor's output, Sec. 4.1) */
@@ -388,6 +390,77 @@ int dynts_chunk_step(dynts_ctx *ctx, int32_t layer, const uint16_t *q, const uin
                      const float *s_new, int32_t n_tokens, const int32_t *n_new, int32_t question,
                      const dynts_shaping *shaping, uint16_t *out, float *lse, void *scratch, size_t scratch_bytes,
                      void *stream);
+
+/* ---- caches of 8-bit codes ----------------------------------------------------------------------------------------
+ * Rows are quantised as they are written: a block of 32 neighbouring elements of a row shares a scale byte s, and
+ *   value = code * 2^(s - 127),   s the least, 27 at least, with  max |x| <= top * 2^(s - 127)  over the block,
+ * codes rounded to nearest, ties to even.  33 bytes in place of 64 a block; every value is exact in bf16.
+ *   DYNTS_CODE_E4M3  a float of 4 bits of exponent, 3 of mantissa, top 448: off by 2^-4 of the value at most, or by 2^-10 of 2^(s - 127)
+ *   DYNTS_CODE_INT8  a whole number, two's complement, top 127: off by half of 2^(s - 127) at most
+ * A block with an infinity, a NaN or a magnitude of 2^126 and more has s = 255 and reads as NaN.
+ *
+ * dynts_bind_codes takes such a cache in place of dynts_bind's or (block_table not NULL) dynts_bind_paged's: K, V uint8 [L][Nb][Hkv][cap][d] with scales
+ * [L][Nb][Hkv][cap][d / 32], or pools [n_pages][64][d] with scales [n_pages][64][d / 32]; everything else as there.  16-byte aligned; pools zero-filled
+ * before first use.  Chunks (dynts_chunk_append, _attend, _scores, _step; n_tokens = 1 is the form for single tokens, question = 1 fills a prompt), drafts
+ * (dynts_tree_*), dynts_read_rows, dynts_select_evict, dynts_compact and dynts_update_scores (which has nothing to do) serve it; the new tokens of a
+ * chunk see each other's rows as the cache holds them.  The other calls on rows return DYNTS_ECODES: dynts_prefill, dynts_append, dynts_decode_attend,
+ * dynts_decode_attend_update, dynts_decode_step, dynts_decode_step_static, dynts_hint_trigger, dynts_score_block, dynts_decode_loop. */
+#define DYNTS_CODE_E4M3 1
+#define DYNTS_CODE_INT8 2
+typedef struct dynts_codes {
+  int32_t code; /* DYNTS_CODE_* */
+  uint8_t *K, *V;
+  uint8_t *K_scale, *V_scale;
+  /* pages, as in dynts_bind_paged; block_table NULL: the dense layout */
+  int32_t n_pages, max_pages;
+  int32_t *block_table, *free_stack, *free_top;
+} dynts_codes;
+int dynts_bind_codes(dynts_ctx *ctx, const dynts_codes *codes, float *S, int32_t *pos, int32_t *seq_len, int32_t *next_pos,
+                     int32_t *n_prompt, void *workspace, size_t workspace_bytes, int32_t *status);
+
+/* dynts_chunk_scratch_bytes for a cache of codes, and for drafts on one.  Where a chunk has many rows there is room in it for one layer's rows as bf16. */
+size_t dynts_codes_scratch_bytes(const dynts_config *cfg, int32_t n_tokens);
+
+/* Rows of a layer as bf16, of any cache: slot first[b] + i (first int32 [Nb], NULL: 0) of every KV head goes to row i of K_out, V_out bf16
+ * [Nb][Hkv][n_rows][d], n_rows <= capacity.  Rows of slots that the sequence does not have are left as they were. */
+int dynts_read_rows(dynts_ctx *ctx, int32_t layer, const int32_t *first, int32_t n_rows, uint16_t *K_out, uint16_t *V_out,
+                    void *stream);
+
+/* ---- drafts that branch -----------------------------------------------------------------------------------------------
+ * Drafted tokens that form trees over the cache: a token sees the whole cache, its ancestors and itself.  A step of a model that drafts:
+ *   dynts_tree_build once, then in every layer dynts_tree_step; when the model has chosen, in every layer dynts_tree_keep with the last token that is
+ *   accepted, and dynts_chunk_scores with the q and lse that it has gathered.
+ * Rotary positions are the caller's: a token of depth t lies t behind the first of the draft.  Dense and paged caches, bf16 or codes.
+ *   n_tokens: tokens of the largest draft, 1 <= n_tokens <= 4096; n_new int32 [Nb] or NULL as for chunks, the rest of the arrays is padding.
+ *   seen uint32 [Nb][n_tokens][ceil(n_tokens / 32)]: bit j % 32 of word j / 32 of token i says that it sees token j of the draft.  What
+ *     dynts_tree_build writes, or any other pattern; bits of tokens behind the sequence's last count as 0.
+ * Arrays that are written overlap no other argument. */
+
+/* seen, and depth int32 [Nb][n_tokens] (0 for a token whose parent is the cache; may be NULL), from parents int32 [Nb][n_tokens]: the draft's
+ * token before it that a token follows, or -1, the cache (as does any number that is not of a token before it).  Padding gets zeros. */
+int dynts_tree_build(const int32_t *parents, const int32_t *n_new, int32_t batch, int32_t n_tokens, uint32_t *seen,
+                     int32_t *depth, void *stream);
+
+/* dynts_chunk_attend for a draft: the LAST n_new[b] tokens in the cache see what lies before them, and of each other what `seen` says.  A token
+ * that sees nothing gets zeros and lse = -inf.  scratch as dynts_chunk_scratch_bytes (or dynts_codes_scratch_bytes) says. */
+int dynts_tree_attend(dynts_ctx *ctx, int32_t layer, const uint16_t *q, int32_t n_tokens, const int32_t *n_new,
+                      const uint32_t *seen, uint16_t *out, float *lse, void *scratch, size_t scratch_bytes, void *stream);
+
+/* dynts_chunk_append of the draft (as thinking tokens, in their order) and dynts_tree_attend.  n_taken int32 [Nb] receives the tokens of each sequence that
+ * the cache took, n_new[b] or 0 (see dynts_chunk_append): dynts_tree_keep wants it. */
+int dynts_tree_step(dynts_ctx *ctx, int32_t layer, const uint16_t *q, const uint16_t *k_new, const uint16_t *v_new,
+                    const float *s_new, int32_t n_tokens, const int32_t *n_new, const uint32_t *seen, int32_t *n_taken,
+                    uint16_t *out, float *lse, void *scratch, size_t scratch_bytes, void *stream);
+
+/* Of the last n_taken[b] (NULL: n_tokens) tokens in the cache those stay that token leaf[b] sees, in order, right behind what lay before the draft;
+ * leaf[b] = -1: none.  Scores move with them, positions are those of a chunk, both lengths and the pages follow; rows behind the new length
+ * keep what they held.  n_kept int32 [Nb] receives the number that stays.  q_kept and lse_kept (NULL, or of the shapes of q and
+ * lse, those of dynts_tree_step) receive the rows of q and lse of the tokens that stay, one after the other; rows behind them are left
+ * alone: dynts_chunk_scores takes them with n_new = n_kept.  A leaf that is not one of the n_taken[b] tokens keeps none and latches bit 4
+ * (value 16) in the status word. */
+int dynts_tree_keep(dynts_ctx *ctx, int32_t layer, int32_t n_tokens, const int32_t *n_taken, const uint32_t *seen,
+                    const int32_t *leaf, const uint16_t *q, const float *lse, uint16_t *q_kept, float *lse_kept,
+                    int32_t *n_kept, void *stream);
 
 /* Rotary positions with several axes (time, height and width of an image's patches, say): pair p of every head, elements (a, b), is
  * turned by theta = positions[axis[p]][t] * freq[p],

@@ -15,6 +15,7 @@ LIB_PATH = os.environ.get("DYNTS_LIBRARY") or os.path.join(_HERE, "libdynts.so")
 DYNTS_OK = 0
 DYNTS_EINVAL, DYNTS_ENULL, DYNTS_ESHAPE, DYNTS_ECAPACITY = -1, -2, -3, -4
 DYNTS_ENOTBOUND, DYNTS_EWORKSPACE, DYNTS_EHIP, DYNTS_EPENDING = -5, -6, -7, -8
+DYNTS_ECODES = -9
 DYNTS_SCORE_ACCUMULATE, DYNTS_SCORE_EXTERNAL = 0, 1
 
 EXPORTS = [
@@ -28,6 +29,8 @@ EXPORTS = [
     "dynts_decode_step_static", "dynts_probe_exp_rate", "dynts_probe_issue_mix", "dynts_hint_trigger",
     "dynts_chunk_scratch_bytes", "dynts_chunk_append", "dynts_chunk_attend", "dynts_chunk_scores", "dynts_chunk_step",
     "dynts_rotate",
+    "dynts_bind_codes", "dynts_codes_scratch_bytes", "dynts_read_rows",
+    "dynts_tree_build", "dynts_tree_attend", "dynts_tree_step", "dynts_tree_keep",
 ]
 
 
@@ -51,6 +54,16 @@ class dynts_rotary(C.Structure):
 
 
 DYNTS_PAIR_HALVES, DYNTS_PAIR_ADJACENT = 0, 1
+
+
+class dynts_codes(C.Structure):
+    _fields_ = [("code", C.c_int32), ("K", C.c_void_p), ("V", C.c_void_p), ("K_scale", C.c_void_p), ("V_scale", C.c_void_p),
+                ("n_pages", C.c_int32), ("max_pages", C.c_int32), ("block_table", C.c_void_p), ("free_stack", C.c_void_p),
+                ("free_top", C.c_void_p)]
+
+
+DYNTS_CODE_E4M3, DYNTS_CODE_INT8 = 1, 2
+CODE_BLOCK = 32
 
 
 class dynts_config(C.Structure):
@@ -110,6 +123,14 @@ def _load():
     lib.dynts_chunk_scores.argtypes = [vp, i32, vp, i32, vp, shaping, vp, vp, i32, vp]
     lib.dynts_chunk_step.argtypes = [vp, i32, vp, vp, vp, vp, i32, vp, i32, shaping, vp, vp, vp, sz, vp]
     lib.dynts_rotate.argtypes = [C.POINTER(dynts_rotary), vp, i32, vp, i32, vp, i32, i32, vp, vp, vp]
+    lib.dynts_bind_codes.argtypes = [vp, C.POINTER(dynts_codes)] + [vp] * 6 + [sz, vp]
+    lib.dynts_codes_scratch_bytes.restype = sz
+    lib.dynts_codes_scratch_bytes.argtypes = [C.POINTER(dynts_config), i32]
+    lib.dynts_read_rows.argtypes = [vp, i32, vp, i32, vp, vp, vp]
+    lib.dynts_tree_build.argtypes = [vp, vp, i32, i32, vp, vp, vp]
+    lib.dynts_tree_attend.argtypes = [vp, i32, vp, i32, vp, vp, vp, vp, vp, sz, vp]
+    lib.dynts_tree_step.argtypes = [vp, i32, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.dynts_tree_keep.argtypes = [vp, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp]
     for name in EXPORTS:
         getattr(lib, name)
     return lib
@@ -601,6 +622,169 @@ def dynts_rotate(rotary, q, k, positions, q_out, k_out, inverse=False, stream=No
     _check(lib.dynts_rotate(rotary.ref, _ptr(q, torch.bfloat16), hq, _ptr(k, torch.bfloat16), hk,
                             _ptr(positions, torch.int32), n, 1 if inverse else 0, _ptr(q_out, torch.bfloat16),
                             _ptr(k_out, torch.bfloat16) if k is not None else None, _stream(stream)), "dynts_rotate")
+
+
+def dynts_bind_codes(ctx, code, K_codes, V_codes, K_scale, V_scale, S, pos, seq_len, next_pos, n_prompt, workspace, status,
+                     block_table=None, free_stack=None, free_top=None):
+    """K_codes, V_codes uint8 [L][Nb][Hkv][cap][d] and scales uint8 [L][Nb][Hkv][cap][d / 32]; with a block_table, pools [n_pages][64][d] and
+    [n_pages][64][d / 32]."""
+    for codes, scales in ((K_codes, K_scale), (V_codes, V_scale)):
+        assert isinstance(codes, int) or isinstance(scales, int) or scales.numel() * CODE_BLOCK == codes.numel(), "one scale for 32 codes"
+    paged = block_table is not None
+    codes = dynts_codes(code, _ptr(K_codes, torch.uint8), _ptr(V_codes, torch.uint8), _ptr(K_scale, torch.uint8), _ptr(V_scale, torch.uint8),
+                        K_codes.shape[0] if paged else 0, block_table.shape[-1] if paged else 0, _ptr(block_table, torch.int32),
+                        _ptr(free_stack, torch.int32), _ptr(free_top, torch.int32))
+    _check(lib.dynts_bind_codes(ctx, C.byref(codes), _ptr(S, torch.float32), _ptr(pos, torch.int32), _ptr(seq_len, torch.int32),
+                                _ptr(next_pos, torch.int32), _ptr(n_prompt, torch.int32), _ptr(workspace),
+                                workspace.numel() * workspace.element_size(), _ptr(status, torch.int32)), "dynts_bind_codes")
+    ctx.gpu = _gpu_of(K_codes)
+
+
+def dynts_codes_scratch_bytes(cfg, n_tokens):
+    return int(lib.dynts_codes_scratch_bytes(C.byref(cfg), n_tokens))
+
+
+def dynts_read_rows(ctx, layer, K_out, V_out, first=None, stream=None):
+    """K_out, V_out bf16 [Nb][Hkv][n_rows][d]; first int32 [Nb] or None."""
+    Nb, Hkv, n_rows, d = K_out.shape
+    dims = getattr(ctx, "dims", None)
+    assert dims is None or (Nb, Hkv, d) == (dims[0], dims[2], dims[3]), "the context's batch, KV heads and head_dim"
+    assert V_out.numel() == K_out.numel() and (first is None or first.numel() == Nb), "V_out as K_out, first one number a sequence"
+    _on_device(ctx, K_out, V_out, first)
+    _check(lib.dynts_read_rows(ctx, layer, _ptr(first, torch.int32), n_rows, _ptr(K_out, torch.bfloat16), _ptr(V_out, torch.bfloat16),
+                               _stream(stream)), "dynts_read_rows")
+
+
+def tree_words(n_tokens):
+    """Words of 32 bits that say which of n_tokens drafted tokens one of them sees."""
+    return (n_tokens + 31) // 32
+
+
+def dynts_tree_build(parents, seen, depth=None, n_new=None, stream=None):
+    """parents, depth int32 [Nb][T]; seen int32 [Nb][T][tree_words(T)]; n_new int32 [Nb]."""
+    Nb, T = parents.shape
+    assert seen.numel() == Nb * T * tree_words(T), "seen holds tree_words(T) words a token"
+    assert depth is None or depth.numel() == Nb * T, "depth holds one number a token"
+    assert n_new is None or n_new.numel() == Nb, "n_new holds one number a sequence"
+    _on_device(None, parents, seen, depth, n_new)
+    _check(lib.dynts_tree_build(_ptr(parents, torch.int32), _ptr(n_new, torch.int32), Nb, T, _ptr(seen, torch.int32), _ptr(depth, torch.int32),
+                                _stream(stream)), "dynts_tree_build")
+
+
+def _draft(q, seen):
+    Nb, T = q.shape[:2]
+    assert seen.numel() == Nb * T * tree_words(T), "seen holds tree_words(T) words a token"
+
+
+def dynts_tree_attend(ctx, layer, q, seen, out, scratch, lse=None, n_new=None, stream=None):
+    """q, out bf16 [Nb][T][Hq][d], lse fp32 [Nb][T][Hq] or None, seen int32 [Nb][T][tree_words(T)]."""
+    T = _chunk_sizes(ctx, q, n_new, None, lse, seen, out, scratch)
+    _draft(q, seen)
+    assert out.numel() == q.numel(), "out has the shape of q"
+    _check(lib.dynts_tree_attend(ctx, layer, _ptr(q, torch.bfloat16), T, _ptr(n_new, torch.int32), _ptr(seen, torch.int32),
+                                 _ptr(out, torch.bfloat16), _ptr(lse, torch.float32), scratch.data_ptr(),
+                                 scratch.numel() * scratch.element_size(), _stream(stream)), "dynts_tree_attend")
+
+
+def dynts_tree_step(ctx, layer, q, k_new, v_new, seen, n_taken, out, scratch, lse=None, n_new=None, s_new=None, stream=None):
+    """k_new, v_new bf16 [Nb][T][Hkv][d], s_new fp32 [Nb][T][Hkv], n_taken int32 [Nb]; the rest as in dynts_tree_attend."""
+    T = _chunk_sizes(ctx, q, n_new, None, lse, k_new, v_new, s_new, seen, n_taken, out, scratch)
+    assert _chunk_rows(ctx, k_new, v_new, s_new) == (q.shape[0], T) and out.numel() == q.numel(), "q, k_new, v_new and out are of one draft"
+    _draft(q, seen)
+    assert n_taken.numel() == q.shape[0], "n_taken holds one number a sequence"
+    _check(lib.dynts_tree_step(ctx, layer, _ptr(q, torch.bfloat16), _ptr(k_new, torch.bfloat16), _ptr(v_new, torch.bfloat16),
+                               _ptr(s_new, torch.float32), T, _ptr(n_new, torch.int32), _ptr(seen, torch.int32), _ptr(n_taken, torch.int32),
+                               _ptr(out, torch.bfloat16), _ptr(lse, torch.float32), scratch.data_ptr(),
+                               scratch.numel() * scratch.element_size(), _stream(stream)), "dynts_tree_step")
+
+
+def dynts_tree_keep(ctx, layer, seen, leaf, n_taken, n_kept, q=None, lse=None, q_kept=None, lse_kept=None, stream=None):
+    """seen int32 [Nb][T][tree_words(T)]; leaf, n_taken (or None), n_kept int32 [Nb]; q, q_kept bf16 [Nb][T][Hq][d], lse, lse_kept fp32 [Nb][T][Hq]."""
+    Nb, T = seen.shape[:2]
+    dims = getattr(ctx, "dims", None)
+    assert dims is None or Nb == dims[0], "the context's batch"
+    assert seen.numel() == Nb * T * tree_words(T), "seen holds tree_words(T) words a token"
+    assert all(t is None or t.numel() == Nb for t in (leaf, n_taken, n_kept)), "leaf, n_taken and n_kept hold one number a sequence"
+    assert q_kept is None or (q is not None and q_kept.numel() == q.numel()), "q_kept has the shape of q"
+    assert lse_kept is None or (lse is not None and lse_kept.numel() == lse.numel()), "lse_kept has the shape of lse"
+    assert dims is None or q_kept is None or q.numel() == Nb * T * dims[1] * dims[3], "q is of the draft"
+    assert dims is None or lse_kept is None or lse.numel() == Nb * T * dims[1], "lse is of the draft"
+    _on_device(ctx, seen, leaf, n_taken, n_kept, q, lse, q_kept, lse_kept)
+    _check(lib.dynts_tree_keep(ctx, layer, T, _ptr(n_taken, torch.int32), _ptr(seen, torch.int32), _ptr(leaf, torch.int32),
+                               _ptr(q, torch.bfloat16), _ptr(lse, torch.float32), _ptr(q_kept, torch.bfloat16), _ptr(lse_kept, torch.float32),
+                               _ptr(n_kept, torch.int32), _stream(stream)), "dynts_tree_keep")
+
+
+class CodedCache:
+    """A cache of codes (dynts_bind_codes), dense or paged, allocated with torch and bound; `K` and `V` give its rows as bf16,
+    [L][Nb][Hkv][cap][d] with zeros behind every sequence's length (for inspection)."""
+
+    def __init__(self, n_layers, batch, n_q_heads, n_kv_heads, head_dim, capacity, budget, window, evict_every, code=DYNTS_CODE_E4M3,
+                 paged=False, n_pages=None, softmax_scale=0.0, external_scores=False, device="cuda:0"):
+        self.cfg = make_config(n_layers, batch, n_q_heads, n_kv_heads, head_dim, capacity, budget, window, evict_every, softmax_scale,
+                               DYNTS_SCORE_EXTERNAL if external_scores else DYNTS_SCORE_ACCUMULATE)
+        self.ctx = dynts_create(self.cfg)
+        dev = torch.device(device)
+        L, Nb, Hkv, cap, d = n_layers, batch, n_kv_heads, capacity, head_dim
+        self.code, self.paged = code, paged
+        z = lambda dtype, *shape: torch.zeros(shape, dtype=dtype, device=dev)
+        pages = {}
+        if paged:
+            self.max_pages = (cap + PAGE_SLOTS - 1) // PAGE_SLOTS
+            self.n_pages = L * Nb * Hkv * self.max_pages if n_pages is None else n_pages
+            at = (self.n_pages, PAGE_SLOTS)
+            self.block_table = torch.full((L, Nb, Hkv, self.max_pages), -1, dtype=torch.int32, device=dev)
+            self.free_stack = torch.arange(self.n_pages, dtype=torch.int32, device=dev)
+            self.free_top = torch.full((1,), self.n_pages, dtype=torch.int32, device=dev)
+            pages = dict(block_table=self.block_table, free_stack=self.free_stack, free_top=self.free_top)
+        else:
+            at = (L, Nb, Hkv, cap)
+        self.K_codes, self.V_codes = z(torch.uint8, *at, d), z(torch.uint8, *at, d)
+        self.K_scale, self.V_scale = z(torch.uint8, *at, d // CODE_BLOCK), z(torch.uint8, *at, d // CODE_BLOCK)
+        self.S, self.pos = z(torch.float32, L, Nb, Hkv, cap), z(torch.int32, L, Nb, Hkv, cap)
+        self.seq_len, self.next_pos, self.n_prompt = z(torch.int32, L, Nb), z(torch.int32, L, Nb), z(torch.int32, Nb)
+        self.status = z(torch.int32, 1)
+        # (without the room for runs of steps, which caches of codes never make)
+        self.workspace = z(torch.uint8, dynts_workspace_bytes(self.cfg))
+        self.keep_idx, self.new_len = z(torch.int32, Nb, Hkv, cap), z(torch.int32, Nb)
+        dynts_bind_codes(self.ctx, code, self.K_codes, self.V_codes, self.K_scale, self.V_scale, self.S, self.pos, self.seq_len, self.next_pos,
+                         self.n_prompt, self.workspace, self.status, **pages)
+
+    @classmethod
+    def for_workload(cls, wl, device="cuda:0", n_layers=None, **kw):
+        return cls(wl.n_layers if n_layers is None else n_layers, wl.batch, wl.n_q_heads, wl.n_kv_heads, wl.head_dim, wl.capacity,
+                   wl.budget, wl.window, wl.evict_every, external_scores=wl.external_scores, device=device, **kw)
+
+    def _rows(self, which):
+        c = self.cfg
+        out = [torch.zeros((c.n_layers, c.batch, c.n_kv_heads, c.capacity, c.head_dim), dtype=torch.bfloat16, device=self.S.device) for _ in range(2)]
+        for layer in range(c.n_layers):
+            dynts_read_rows(self.ctx, layer, out[0][layer], out[1][layer])
+        return out[which]
+
+    @property
+    def K(self):
+        return self._rows(0)
+
+    @property
+    def V(self):
+        return self._rows(1)
+
+    def pages_in_use(self):
+        """As PagedCache.pages_in_use."""
+        per_unit = (self.seq_len + PAGE_SLOTS - 1) // PAGE_SLOTS
+        return int(per_unit.sum().item()) * self.cfg.n_kv_heads, self.n_pages - int(self.free_top.item())
+
+    def close(self):
+        if self.ctx is not None:
+            dynts_destroy(self.ctx)
+            self.ctx = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
 
 
 class Cache:

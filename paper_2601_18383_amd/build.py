@@ -4,7 +4,7 @@ import subprocess
 import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
-SRC = [os.path.join(HERE, "csrc", f) for f in ("dynts.hip", "chunk.hip")]  # linked in this order
+SRC = [os.path.join(HERE, "csrc", f) for f in ("dynts.hip", "chunk.hip", "forms.hip")]  # linked in this order
 LIB = os.path.join(HERE, "libdynts.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 

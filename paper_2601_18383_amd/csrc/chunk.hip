@@ -8,6 +8,7 @@
 #include "chunk_append.hpp"
 #include "chunk_attend.hpp"
 #include "chunk_scores.hpp"
+#include "forms.hpp"
 #include "rotate.hpp"
 
 namespace {
@@ -15,7 +16,7 @@ namespace {
 using dynts::ChunkCache;
 
 constexpr size_t kAlign = 256;
-constexpr int kMostTokens = 1 << 20;
+constexpr int kMostTokens = 1 << 20, kMostDraft = dynts::kTreeMost;
 constexpr float kLog2E = 1.4426950408889634f;
 
 size_t align_up(size_t v) { return (v + kAlign - 1) / kAlign * kAlign; }
@@ -95,13 +96,24 @@ ChunkPlan chunk_plan(const dynts_config &c, int n_tokens, int slots, bool far_ca
 // a cap that takes the longer form of soft_caps
 bool far_cap(const dynts_shaping *s) { return s && s->softcap * kLog2E > dynts::kCapNear; }
 
-ChunkPlan chunk_plan(const ChunkCache &c, int n_tokens, const dynts_shaping *shaping = nullptr) {
+dynts_config config_of(const ChunkCache &c) {
   dynts_config cfg{};
   cfg.batch = c.Nb; cfg.n_q_heads = c.Hq; cfg.n_kv_heads = c.Hkv; cfg.head_dim = c.D; cfg.capacity = c.cap;
+  return cfg;
+}
+ChunkPlan chunk_plan(const ChunkCache &c, int n_tokens, const dynts_shaping *shaping = nullptr) {
   // (slots of a window: no more than its positions, those of the chunk's other tokens beside them)
   const long long seen = shaping && shaping->window > 0 ? (long long)shaping->window + n_tokens : c.cap;
-  return chunk_plan(cfg, n_tokens, (int)(seen < c.cap ? seen : c.cap), far_cap(shaping));
+  return chunk_plan(config_of(c), n_tokens, (int)(seen < c.cap ? seen : c.cap), far_cap(shaping));
 }
+
+// Room behind a chunk's scratch where the layer's codes lie as bf16, for the kernel of many rows.
+size_t unpacked_bytes(const dynts_config &c) { return align_up((size_t)c.batch * c.n_kv_heads * c.capacity * c.head_dim * 2); }
+size_t scratch_bytes_of(const dynts_config &c, int n_tokens, bool codes) {
+  const ChunkPlan pl = chunk_plan(c, n_tokens, c.capacity);
+  return pl.bytes + (codes && !pl.few ? 2 * unpacked_bytes(c) : 0);
+}
+size_t scratch_bytes_of(const ChunkCache &c, int n_tokens) { return scratch_bytes_of(config_of(c), n_tokens, c.code != 0); }
 
 // the factor of a logit's exponent, 2 z log2 e; infinite for a softcap below the smallest normal numbers
 float cap_in(float softcap, float scale) { return 2.f * kLog2E * scale / softcap; }
@@ -152,12 +164,17 @@ int launch_append(const ChunkCache &c, const uint16_t *k_new, const uint16_t *v_
   const dynts::ChunkAppendParams p{c, k_new, v_new, s_new, n_new, taken, n_tokens, question};
   const long long pieces = (long long)n_tokens * c.Hkv * (c.D / 8);
   const dim3 block(dynts::kAppendThreads);
+  if (c.code && pieces <= dynts::kAppendSmall) {
+    dynts::launch_coded_append(p, true, 0, st);
+    return launch_status();
+  }
   if (copy && pieces <= dynts::kAppendSmall) {
     if (c.D == 128) hipLaunchKernelGGL((dynts::chunk_reserve_kernel<128, true>), dim3(c.Nb), block, 0, st, p);
     else hipLaunchKernelGGL((dynts::chunk_reserve_kernel<64, true>), dim3(c.Nb), block, 0, st, p);
     return launch_status();
   }
   const dim3 grid((unsigned)((pieces + dynts::kAppendThreads - 1) / dynts::kAppendThreads), c.Nb);
+  if (c.code) copy = false;
   if (c.D == 128) {
     hipLaunchKernelGGL((dynts::chunk_reserve_kernel<128, false>), dim3(c.Nb), block, 0, st, p);
     if (copy) hipLaunchKernelGGL((dynts::chunk_copy_kernel<128>), grid, block, 0, st, p);
@@ -165,6 +182,7 @@ int launch_append(const ChunkCache &c, const uint16_t *k_new, const uint16_t *v_
     hipLaunchKernelGGL((dynts::chunk_reserve_kernel<64, false>), dim3(c.Nb), block, 0, st, p);
     if (copy) hipLaunchKernelGGL((dynts::chunk_copy_kernel<64>), grid, block, 0, st, p);
   }
+  if (c.code) dynts::launch_coded_append(p, false, grid.x, st);
   return launch_status();
 }
 
@@ -195,7 +213,9 @@ unsigned scores_grid(const ChunkCache &c, bool few) {
 
 template <int D, bool SHAPED>
 void launch_attend_d(const dynts::ChunkAttendParams &p, const ChunkPlan &pl, unsigned grid, hipStream_t st) {
-  if (pl.few) hipLaunchKernelGGL((dynts::chunk_attend_few_kernel<D, SHAPED>), dim3(grid), dim3(dynts::kFewThreads), 0, st, p);
+  if (pl.few && (p.seen || p.c.code)) dynts::launch_few_form(p, p.seen ? dynts::kTree : SHAPED ? dynts::kShaped : dynts::kPlain, grid, st);
+  else if (p.seen) dynts::launch_tree_attend(p, grid, st);
+  else if (pl.few) hipLaunchKernelGGL((dynts::chunk_attend_few_kernel<D, SHAPED>), dim3(grid), dim3(dynts::kFewThreads), 0, st, p);
   else if (SHAPED && p.shape.slope) hipLaunchKernelGGL((dynts::chunk_attend_kernel<D, SHAPED, SHAPED, false>), dim3(grid), dim3(dynts::kChThreads), 0, st, p);
   else if (!SHAPED && p.k_new) hipLaunchKernelGGL((dynts::chunk_attend_kernel<D, false, false, !SHAPED>), dim3(grid), dim3(dynts::kChThreads), 0, st, p);
   else hipLaunchKernelGGL((dynts::chunk_attend_kernel<D, SHAPED, false, false>), dim3(grid), dim3(dynts::kChThreads), 0, st, p);
@@ -213,13 +233,23 @@ struct Fresh {
   int question = 0;
 };
 
-int launch_attend(const ChunkCache &c, const uint16_t *q, int n_tokens, const int32_t *n_new, const dynts_shaping *shaping, uint16_t *out,
+// seen: of a draft's tokens, or null
+int launch_attend(ChunkCache c, const uint16_t *q, int n_tokens, const int32_t *n_new, const dynts_shaping *shaping, const uint32_t *seen, uint16_t *out,
                   float *lse, void *scratch, const Fresh &fresh, hipStream_t st) {
   const ChunkPlan pl = chunk_plan(c, n_tokens, shaping);
   char *const base = static_cast<char *>(scratch);
+  if (c.code && !pl.few) {  // the codes as bf16, in a dense cache in scratch
+    uint16_t *const K = reinterpret_cast<uint16_t *>(base + pl.bytes), *const V = reinterpret_cast<uint16_t *>(base + pl.bytes + unpacked_bytes(config_of(c)));
+    dynts::launch_read_rows(c, nullptr, c.cap, K, V, st);
+    c.K = K;
+    c.V = V;
+    c.code = 0;
+    c.block_table = nullptr;
+  }
   const dynts::ChunkAttendParams p{c, q, n_new, out, lse, chunk_shape(shaping, c.scale), n_tokens, c.scale * kLog2E, group_magic(c.G), pl.n_split, pl.Rpad,
                                    reinterpret_cast<float *>(base + pl.off_o), reinterpret_cast<float *>(base + pl.off_ml),
-                                   reinterpret_cast<int32_t *>(base + pl.off_n), fresh.k_new, fresh.v_new, fresh.s_new, fresh.question};
+                                   reinterpret_cast<int32_t *>(base + pl.off_n), fresh.k_new, fresh.v_new, fresh.s_new, fresh.question,
+                                   seen, (n_tokens + 31) / 32};
   const unsigned grid = attend_grid(c, pl);
   if (!grid) return DYNTS_EINVAL;
   if (c.D == 128) {
@@ -251,12 +281,22 @@ int launch_scores(const ChunkCache &c, const uint16_t *q, int n_tokens, const in
   const bool few = scores_few(c, n_tokens, shaping);
   const unsigned grid = scores_grid(c, few);
   if (!grid) return DYNTS_EINVAL;
-  if (c.D == 128) launch_scores_d<128>(p, few, grid, st);
+  if (c.code) dynts::launch_coded_scores(p, few, shaped(p.shape), p.shape.slope != nullptr, grid, st);
+  else if (c.D == 128) launch_scores_d<128>(p, few, grid, st);
   else launch_scores_d<64>(p, few, grid, st);
   return launch_status();
 }
 
 int check_tokens(int32_t n_tokens) { return n_tokens <= 0 || n_tokens > kMostTokens ? DYNTS_EINVAL : DYNTS_OK; }
+
+int check_draft(const ChunkCache &c, const uint16_t *q, int n_tokens, const uint32_t *seen, const uint16_t *out) {
+  if (n_tokens <= 0 || n_tokens > kMostDraft) return DYNTS_EINVAL;
+  if (!q || !seen || !out) return DYNTS_ENULL;
+  if (misaligned(q, 16) || misaligned(out, 16) || misaligned(seen, 4)) return DYNTS_EINVAL;
+  const size_t q_bytes = (size_t)c.Nb * n_tokens * c.Hq * c.D * 2;
+  if (overlap(out, q_bytes, q, q_bytes)) return DYNTS_EINVAL;
+  return attend_grid(c, chunk_plan(c, n_tokens)) ? DYNTS_OK : DYNTS_EINVAL;
+}
 
 }  // namespace
 
@@ -267,13 +307,18 @@ size_t dynts_chunk_scratch_bytes(const dynts_config *cfg, int32_t n_tokens) {
   return chunk_plan(*cfg, n_tokens, cfg->capacity).bytes;
 }
 
+size_t dynts_codes_scratch_bytes(const dynts_config *cfg, int32_t n_tokens) {
+  if (dynts::chunk_check_config(cfg) != DYNTS_OK || check_tokens(n_tokens) != DYNTS_OK) return 0;
+  return scratch_bytes_of(*cfg, n_tokens, true);
+}
+
 int dynts_chunk_append(dynts_ctx *ctx, int32_t layer, const uint16_t *k_new, const uint16_t *v_new, const float *s_new, int32_t n_tokens,
                        const int32_t *n_new, int32_t question, void *scratch, size_t scratch_bytes, void *stream) {
   ChunkCache c;
   int rc = dynts::chunk_cache(ctx, layer, &c);
   if (rc == DYNTS_OK) rc = check_tokens(n_tokens);
   if (rc == DYNTS_OK) rc = check_append(c, k_new, v_new, s_new, question);
-  if (rc == DYNTS_OK) rc = check_scratch(scratch, scratch_bytes, chunk_plan(c, n_tokens).bytes);
+  if (rc == DYNTS_OK) rc = check_scratch(scratch, scratch_bytes, scratch_bytes_of(c, n_tokens));
   if (rc != DYNTS_OK) return rc;
   if (c.score_mode != DYNTS_SCORE_EXTERNAL) s_new = nullptr;
   return launch_append(c, k_new, v_new, s_new, n_tokens, n_new, question ? 1 : 0, static_cast<int32_t *>(scratch), true, static_cast<hipStream_t>(stream));
@@ -288,11 +333,11 @@ int dynts_chunk_attend(dynts_ctx *ctx, int32_t layer, const uint16_t *q, int32_t
   if (rc != DYNTS_OK) return rc;
   if (!q || !out) return DYNTS_ENULL;
   if (misaligned(q, 16) || misaligned(out, 16)) return DYNTS_EINVAL;
-  rc = check_scratch(scratch, scratch_bytes, chunk_plan(c, n_tokens).bytes);
+  rc = check_scratch(scratch, scratch_bytes, scratch_bytes_of(c, n_tokens));
   if (rc != DYNTS_OK) return rc;
   const size_t q_bytes = (size_t)c.Nb * n_tokens * c.Hq * c.D * 2;
   if (overlap(out, q_bytes, q, q_bytes)) return DYNTS_EINVAL;
-  return launch_attend(c, q, n_tokens, n_new, shaping, out, lse, scratch, Fresh{}, static_cast<hipStream_t>(stream));
+  return launch_attend(c, q, n_tokens, n_new, shaping, nullptr, out, lse, scratch, Fresh{}, static_cast<hipStream_t>(stream));
 }
 
 int dynts_chunk_scores(dynts_ctx *ctx, int32_t layer, const uint16_t *q, int32_t n_tokens, const int32_t *n_new, const dynts_shaping *shaping,
@@ -319,7 +364,7 @@ int dynts_chunk_step(dynts_ctx *ctx, int32_t layer, const uint16_t *q, const uin
   if (!q || !out) return DYNTS_ENULL;
   if (misaligned(q, 16) || misaligned(out, 16)) return DYNTS_EINVAL;
   const ChunkPlan pl = chunk_plan(c, n_tokens, shaping);
-  rc = check_scratch(scratch, scratch_bytes, pl.bytes);
+  rc = check_scratch(scratch, scratch_bytes, c.code ? scratch_bytes_of(c, n_tokens) : pl.bytes);
   if (rc != DYNTS_OK) return rc;
   hipStream_t st = static_cast<hipStream_t>(stream);
   int32_t *taken = static_cast<int32_t *>(scratch);
@@ -330,11 +375,40 @@ int dynts_chunk_step(dynts_ctx *ctx, int32_t layer, const uint16_t *q, const uin
   if (scores && !lse) lse = reinterpret_cast<float *>(static_cast<char *>(scratch) + pl.off_lse);
   if (c.score_mode != DYNTS_SCORE_EXTERNAL) s_new = nullptr;
   question = question ? 1 : 0;
-  const bool on_the_way = !pl.few && !shaped(shaping);
+  const bool on_the_way = !pl.few && !shaped(shaping) && !c.code;
   rc = launch_append(c, k_new, v_new, s_new, n_tokens, n_new, question, taken, !on_the_way, st);
   if (rc == DYNTS_OK)
-    rc = launch_attend(c, q, n_tokens, taken, shaping, out, lse, scratch, on_the_way ? Fresh{k_new, v_new, s_new, question} : Fresh{}, st);
+    rc = launch_attend(c, q, n_tokens, taken, shaping, nullptr, out, lse, scratch, on_the_way ? Fresh{k_new, v_new, s_new, question} : Fresh{}, st);
   if (rc == DYNTS_OK && scores) rc = launch_scores(c, q, n_tokens, taken, shaping, lse, nullptr, 1, st);
+  return rc;
+}
+
+int dynts_tree_attend(dynts_ctx *ctx, int32_t layer, const uint16_t *q, int32_t n_tokens, const int32_t *n_new, const uint32_t *seen, uint16_t *out,
+                      float *lse, void *scratch, size_t scratch_bytes, void *stream) {
+  ChunkCache c;
+  int rc = dynts::chunk_cache(ctx, layer, &c);
+  if (rc == DYNTS_OK) rc = check_draft(c, q, n_tokens, seen, out);
+  if (rc == DYNTS_OK) rc = check_scratch(scratch, scratch_bytes, scratch_bytes_of(c, n_tokens));
+  if (rc != DYNTS_OK) return rc;
+  return launch_attend(c, q, n_tokens, n_new, nullptr, seen, out, lse, scratch, Fresh{}, static_cast<hipStream_t>(stream));
+}
+
+int dynts_tree_step(dynts_ctx *ctx, int32_t layer, const uint16_t *q, const uint16_t *k_new, const uint16_t *v_new, const float *s_new, int32_t n_tokens,
+                    const int32_t *n_new, const uint32_t *seen, int32_t *n_taken, uint16_t *out, float *lse, void *scratch, size_t scratch_bytes,
+                    void *stream) {
+  ChunkCache c;
+  int rc = dynts::chunk_cache(ctx, layer, &c);
+  if (rc == DYNTS_OK) rc = check_draft(c, q, n_tokens, seen, out);
+  if (rc == DYNTS_OK) rc = check_append(c, k_new, v_new, s_new, 0);
+  if (rc == DYNTS_OK && !n_taken) rc = DYNTS_ENULL;
+  if (rc == DYNTS_OK) rc = check_scratch(scratch, scratch_bytes, scratch_bytes_of(c, n_tokens));
+  if (rc != DYNTS_OK) return rc;
+  const size_t row = (size_t)c.Nb * n_tokens * c.D * 2, q_bytes = row * c.Hq, k_bytes = row * c.Hkv;
+  if (overlap(out, q_bytes, k_new, k_bytes) || overlap(out, q_bytes, v_new, k_bytes)) return DYNTS_EINVAL;
+  if (c.score_mode != DYNTS_SCORE_EXTERNAL) s_new = nullptr;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  rc = launch_append(c, k_new, v_new, s_new, n_tokens, n_new, 0, n_taken, true, st);
+  if (rc == DYNTS_OK) rc = launch_attend(c, q, n_tokens, n_taken, nullptr, seen, out, lse, scratch, Fresh{}, st);
   return rc;
 }
 

@@ -19,6 +19,9 @@ struct ChunkCache {
   int Nb, Hq, Hkv, G, D, cap;
   int score_mode;
   float scale;  // of the softmax
+  // caches of codes (dynts_bind_codes; K and V then are theirs, one byte an element): DYNTS_CODE_*, else 0, and a byte for 32 elements
+  int code;
+  uint8_t *K_scale, *V_scale;
 };
 
 // Looks the layer up; DYNTS_OK or the error that a call on this context and layer has to return.

@@ -7,6 +7,7 @@
 
 #include "attend.hpp"
 #include "chunk.hpp"
+#include "codes.hpp"
 
 namespace dynts {
 
@@ -24,8 +25,9 @@ constexpr int kAppendThreads = 256;
 // Pieces of 16 bytes, K's, that the first launch copies itself: a workgroup has 16 a thread then.
 constexpr int kAppendSmall = 16 * kAppendThreads;
 
+// (CODE: the cache holds codes; codes.hpp)
 // Pieces [from, ...) of sequence b, `step` apart: piece p is part p % (D / 8) of head (p / (D / 8)) % Hkv of token p / (D / 8) / Hkv.
-template <int D>
+template <int D, int CODE = 0>
 __device__ __forceinline__ void chunk_copy(const ChunkAppendParams &p, int b, int n, int m, int pos0, int from, int step) {
   constexpr int LPR = D / 8;
   const ChunkCache &c = p.c;
@@ -36,8 +38,13 @@ __device__ __forceinline__ void chunk_copy(const ChunkAppendParams &p, int b, in
     size_t dst;
     if (c.block_table) dst = paged_row<D>(c.block_table + unit * c.max_pages, slot, c.max_pages, c.n_pages) + 8 * piece;
     else dst = (unit * (size_t)c.cap + slot) * D + 8 * piece;
-    store_u32x4(c.K + dst, load_u32x4(p.k_new + src));
-    store_u32x4(c.V + dst, load_u32x4(p.v_new + src));
+    if (CODE) {
+      encode8<CODE>(load_u32x4(p.k_new + src), reinterpret_cast<uint8_t *>(c.K), c.K_scale, dst, piece);
+      encode8<CODE>(load_u32x4(p.v_new + src), reinterpret_cast<uint8_t *>(c.V), c.V_scale, dst, piece);
+    } else {
+      store_u32x4(c.K + dst, load_u32x4(p.k_new + src));
+      store_u32x4(c.V + dst, load_u32x4(p.v_new + src));
+    }
     if (piece == 0) {
       const size_t e = unit * (size_t)c.cap + slot;
       c.S[e] = p.question ? INFINITY : p.s_new ? p.s_new[((size_t)b * p.T + i) * c.Hkv + h] : 0.f;
@@ -70,8 +77,8 @@ __device__ __forceinline__ void chunk_copy_head(const ChunkCache &c, const uint1
 }
 
 // grid (Nb).  A chunk that does not fit leaves its sequence alone: status bit 0 (no room), 2 (no pages), 3 (a question behind thinking tokens).
-template <int D, bool COPY>
-__global__ __launch_bounds__(kAppendThreads) void chunk_reserve_kernel(const ChunkAppendParams p) {
+template <int D, bool COPY, int CODE>
+__device__ __forceinline__ void chunk_reserve(const ChunkAppendParams &p) {
   const ChunkCache &c = p.c;
   const int b = blockIdx.x, tid = threadIdx.x;
   __shared__ int sm_m, sm_top;
@@ -119,8 +126,16 @@ __global__ __launch_bounds__(kAppendThreads) void chunk_reserve_kernel(const Chu
   }
   if (COPY) {
     __syncthreads();  // (the pages above)
-    chunk_copy<D>(p, b, n, m, pos0, tid, kAppendThreads);
+    chunk_copy<D, CODE>(p, b, n, m, pos0, tid, kAppendThreads);
   }
+}
+template <int D, bool COPY>
+__global__ __launch_bounds__(kAppendThreads) void chunk_reserve_kernel(const ChunkAppendParams p) {
+  chunk_reserve<D, COPY, 0>(p);
+}
+template <int D, int CODE>
+__global__ __launch_bounds__(kAppendThreads) void coded_reserve_kernel(const ChunkAppendParams p) {
+  chunk_reserve<D, true, CODE>(p);
 }
 
 // grid (ceil(T * Hkv * D / 8 / 256), Nb), behind chunk_reserve_kernel
@@ -128,6 +143,11 @@ template <int D>
 __global__ __launch_bounds__(kAppendThreads) void chunk_copy_kernel(const ChunkAppendParams p) {
   const int b = blockIdx.y, m = p.taken[b];
   chunk_copy<D>(p, b, p.c.seq_len[b] - m, m, p.c.next_pos[b] - m, blockIdx.x * kAppendThreads + threadIdx.x, gridDim.x * kAppendThreads);
+}
+template <int D, int CODE>
+__global__ __launch_bounds__(kAppendThreads) void coded_copy_kernel(const ChunkAppendParams p) {
+  const int b = blockIdx.y, m = p.taken[b];
+  chunk_copy<D, CODE>(p, b, p.c.seq_len[b] - m, m, p.c.next_pos[b] - m, blockIdx.x * kAppendThreads + threadIdx.x, gridDim.x * kAppendThreads);
 }
 
 }  // namespace dynts

@@ -22,6 +22,7 @@
 #include "attend.hpp"
 #include "chunk.hpp"
 #include "chunk_append.hpp"
+#include "codes.hpp"
 #include "score_block.hpp"
 
 namespace dynts {
@@ -55,7 +56,13 @@ struct ChunkAttendParams {
   const uint16_t *k_new, *v_new;
   const float *s_new;
   int question;
+  // a draft's tokens: which of each other they see, 32 to a word, [Nb][T][words] (see tree_bits)
+  const uint32_t *seen;
+  int words;
 };
+
+// What decides which slots a row sees: the order of the slots, a dynts_shaping, or (below the cache's end, where a draft's tokens are) bits.
+constexpr int kPlain = 0, kShaped = 1, kTree = 2;
 
 constexpr int kShareTiles = 16;  // least tiles of 32 slots in a share
 
@@ -168,6 +175,15 @@ __device__ __forceinline__ void chunk_interval(const ChunkShape &s, size_t at, i
   chunk_bounds(s, first, last, own, lo, span);
 }
 
+// Which of the 32 slots from t on a row of a draft's token sees, slot t + k by bit k.  bits: the token's words; base: the slot of the draft's first token.  Slots
+// before it are seen, slots behind the sequence's last (n) not, whatever the words say.
+__device__ __forceinline__ uint32_t tree_bits(const uint32_t *bits, int words, int t, int base, int n) {
+  const int at = t - base, w = at >> 5;  // (at > -32)
+  const uint32_t lo = w < 0 ? ~0u : w < words ? bits[w] : 0u, hi = w + 1 < words ? bits[w + 1] : 0u;
+  const uint32_t own = __builtin_amdgcn_alignbit(hi, lo, (uint32_t)at & 31u);
+  return n - t < 32 ? own & ((1u << (n - t)) - 1u) : own;
+}
+
 // The token a row belongs to (rows below 2^28).
 __device__ __forceinline__ int chunk_token(int r, uint32_t magic) { return magic ? (int)__umulhi((uint32_t)r, magic) : r; }
 
@@ -265,8 +281,9 @@ __device__ __forceinline__ int chunk_lds_v(int row, int piece) {
 // form): the chunk's own rows are not in the cache yet; they are read where the caller has them, and every workgroup copies those of its tokens at its
 // end.  (Copied by a launch of their own before, 512 tokens of 64 sequences, 32 heads on 8: 244 us a step instead of 236, heads of 64 134 instead of
 // 123, 28 on 4 of 32 sequences, 600 tokens, 122 instead of 123.)
-template <int D, bool SHAPED, bool BIASED, bool APPEND>
-__global__ __launch_bounds__(kChThreads, D == 128 ? 3 : 4) void chunk_attend_kernel(const ChunkAttendParams p) {
+template <int D, int MASK, bool BIASED, bool APPEND>
+__device__ __forceinline__ void chunk_attend_rows(const ChunkAttendParams &p) {
+  constexpr bool SHAPED = MASK == kShaped, TREE = MASK == kTree;
   using Lds = ChunkLds<D>;
   const ChunkCache &c = p.c;
   // Three tiles' places: one is worked on, one is on its way, one is being asked for.
@@ -333,6 +350,10 @@ __global__ __launch_bounds__(kChThreads, D == 128 ? 3 : 4) void chunk_attend_ker
     t_lo = t_lo / kChTile * kChTile;
     all_lo = __builtin_amdgcn_readfirstlane(all_lo);
     if (BIASED) own_lo = __builtin_amdgcn_readlane(own, 0);
+  } else if (TREE) {
+    lim = tok * p.words;  // (its words, from the sequence's first on)
+    t_hi = n;
+    all_hi = base - 1;
   } else {
     lim = base + tok;
     t_hi = base + i1 + 1;
@@ -464,6 +485,13 @@ __global__ __launch_bounds__(kChThreads, D == 128 ? 3 : 4) void chunk_attend_ker
           const int key = 8 * (e >> 2) + 4 * hf + (e & 3), kp = t + key < n ? tp[key] : -1;
           if ((uint32_t)(kp - lim) > span) s[e] = -INFINITY;
         }
+      }
+    } else if (TREE) {
+      if (t + kChTile - 1 > all_hi) {
+        const uint32_t sees = tree_bits(p.seen + (size_t)b * p.T * p.words + lim, p.words, t, base, n) >> (4 * hf);
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (!(sees >> (8 * (e >> 2) + (e & 3)) & 1u)) s[e] = -INFINITY;
       }
     } else if (t + kChTile - 1 > all_hi) {
       asm volatile("; some keys are hidden");
@@ -614,6 +642,16 @@ __global__ __launch_bounds__(kChThreads, D == 128 ? 3 : 4) void chunk_attend_ker
   }
 }
 
+template <int D, bool SHAPED, bool BIASED, bool APPEND>
+__global__ __launch_bounds__(kChThreads, D == 128 ? 3 : 4) void chunk_attend_kernel(const ChunkAttendParams p) {
+  chunk_attend_rows<D, SHAPED ? kShaped : kPlain, BIASED, APPEND>(p);
+}
+// The same for a draft's tokens.
+template <int D>
+__global__ __launch_bounds__(kChThreads, D == 128 ? 3 : 4) void tree_attend_kernel(const ChunkAttendParams p) {
+  chunk_attend_rows<D, kTree, false, false>(p);
+}
+
 // ---- few rows: 32 of them a workgroup, its eight waves share out the keys --------------------------------------------------
 // Bound by HBM (or the memory-side cache): every wave streams 32 slots at a time through registers and a part of LDS of its own, the next
 // tile's loads in flight while it works on one, no barrier before the end.  There the waves' outputs are joined through LDS.  Four tokens of 32
@@ -626,8 +664,10 @@ struct FewLds {
   static constexpr int kWave = 2 * kTileBytes > kJoin ? 2 * kTileBytes : kJoin;
 };
 
-template <int D, bool SHAPED>
-__global__ __launch_bounds__(kFewThreads, 2) void chunk_attend_few_kernel(const ChunkAttendParams p) {
+// CODE: the cache holds codes (codes.hpp), which become bf16 on their way from registers to LDS.
+template <int D, int MASK, int CODE>
+__device__ __forceinline__ void chunk_attend_few(const ChunkAttendParams &p) {
+  constexpr bool SHAPED = MASK == kShaped, TREE = MASK == kTree;
   using Lds = FewLds<D>;
   const ChunkCache &c = p.c;
   __shared__ __attribute__((aligned(16))) char sm[kFewWaves][Lds::kWave];
@@ -655,6 +695,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void chunk_attend_few_kernel(const 
 
   const int32_t *pos = c.pos + (size_t)unit * c.cap;
   const int lim = base + i;
+  const uint32_t *bits = TREE ? p.seen + ((size_t)b * p.T + i) * p.words : nullptr;
   int lo = 0, own = 0;
   uint32_t span = 0;
   float slope = 0.f;
@@ -677,7 +718,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void chunk_attend_few_kernel(const 
                 __builtin_amdgcn_readfirstlane(tail), lane, t_lo, t_hi);
     t_lo = t_lo / kFewTile * kFewTile;
   } else {
-    t_hi = base + i1 + 1;
+    t_hi = TREE ? n : base + i1 + 1;
   }
   // this share's tiles, every kFewWaves'th of them this wave's
   const int tiles = t_hi > t_lo ? (t_hi - t_lo + kFewTile - 1) / kFewTile : 0;
@@ -694,29 +735,50 @@ __global__ __launch_bounds__(kFewThreads, 2) void chunk_attend_few_kernel(const 
   float m_run = -INFINITY, l_run = 0.f;
 
   char *const sk = sm[wave], *const sv = sm[wave] + Lds::kTileBytes;
-  constexpr int PPR = D / 8, PIECES = kFewTile * PPR / 64;  // 16-byte pieces a row, and of K or V a lane
+  constexpr int PPR = CODE ? D / 16 : D / 8, PIECES = kFewTile * PPR / 64;  // 16-byte pieces a row, and of K or V a lane
   u32x4 kr[PIECES], vr[PIECES];
+  uint32_t k_scale[CODE ? PIECES : 1], v_scale[CODE ? PIECES : 1];  // the scales of a lane's codes
   int pr = 0;
-  auto fetch = [&](int tile, u32x4 (&x)[PIECES], const uint16_t *pool) {
+  auto fetch = [&](int tile, u32x4 (&x)[PIECES], uint32_t (&scale)[CODE ? PIECES : 1], const uint16_t *pool, const uint8_t *scales) {
     // (past the share's end: a buffer of no rows, nothing is fetched)
     const int rows = tile < t_end ? (n - tile < kFewTile ? n - tile : kFewTile) : 0;
+    if (CODE) {
+      const size_t row = rows > 0 ? chunk_tile<1>(c, unit, tile, c.block_table ? chunk_page(c, unit, tile) : 0) : 0;
+      const RowBuffer buf = row_buffer<D / 2>(pool + row * (D / 2), rows), sb = scale_buffer<D>(scales + row * (D / kCodeBlock), rows);
+#pragma unroll
+      for (int k = 0; k < PIECES; ++k) {
+        x[k] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(buf, 16 * (lane + 64 * k), 0, 0));
+        scale[CODE ? k : 0] = __builtin_amdgcn_raw_buffer_load_b8(sb, (lane + 64 * k) / 2, 0, 0);
+      }
+      return;
+    }
     const RowBuffer buf = row_buffer<D>(pool + (rows > 0 ? chunk_tile<D>(c, unit, tile, c.block_table ? chunk_page(c, unit, tile) : 0) : 0), rows);
 #pragma unroll
     for (int k = 0; k < PIECES; ++k) x[k] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(buf, 16 * (lane + 64 * k), 0, 0));
   };
-  auto park = [&](char *dst, const u32x4 (&x)[PIECES]) {
+  auto park = [&](char *dst, const u32x4 (&x)[PIECES], const uint32_t (&scale)[CODE ? PIECES : 1]) {
 #pragma unroll
-    for (int k = 0; k < PIECES; ++k) *reinterpret_cast<u32x4 *>(dst + chunk_lds<D>((lane + 64 * k) / PPR, (lane + 64 * k) % PPR)) = x[k];
+    for (int k = 0; k < PIECES; ++k) {
+      const int row = (lane + 64 * k) / PPR, piece = (lane + 64 * k) % PPR;
+      if (CODE) {
+        u32x4 lo, hi;
+        decode16<CODE>(x[k], scale[CODE ? k : 0], lo, hi);
+        *reinterpret_cast<u32x4 *>(dst + chunk_lds<D>(row, 2 * piece)) = lo;
+        *reinterpret_cast<u32x4 *>(dst + chunk_lds<D>(row, 2 * piece + 1)) = hi;
+      } else {
+        *reinterpret_cast<u32x4 *>(dst + chunk_lds<D>(row, piece)) = x[k];
+      }
+    }
   };
   auto fetch_pos = [&](int tile) { pr = tile < t_end && tile + col < n ? pos[tile + col] : -1; };
-  fetch(t, kr, c.K);
+  fetch(t, kr, k_scale, c.K, c.K_scale);
   if (SHAPED) fetch_pos(t);
-  fetch(t, vr, c.V);
+  fetch(t, vr, v_scale, c.V, c.V_scale);
   for (; t < t_end; t += kFewWaves * kFewTile) {
     const int next = t + kFewWaves * kFewTile;
-    park(sk, kr);
+    park(sk, kr, k_scale);
     if (SHAPED && hf == 0) sm_pos[wave][col] = pr;
-    fetch(next, kr, c.K);
+    fetch(next, kr, k_scale, c.K, c.K_scale);
     if (SHAPED) fetch_pos(next);
     wave_lds_fence();
     f32x16 s;
@@ -730,10 +792,14 @@ __global__ __launch_bounds__(kFewThreads, 2) void chunk_attend_few_kernel(const 
     float mx = -INFINITY;
     const bool capped = SHAPED && p.shape.cap > 0.f;
     if (capped) soft_caps<true>(s, p.scale_log2, p.shape);
+    uint32_t sees = ~0u;
+    if (TREE && t + kFewTile > base) sees = tree_bits(bits, p.words, t, base, n) >> (4 * hf);
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
       const int key = 8 * (e >> 2) + 4 * hf + (e & 3);
-      if (SHAPED) {
+      if (TREE) {
+        s[e] = sees >> (8 * (e >> 2) + (e & 3)) & 1u ? s[e] * p.scale_log2 : -INFINITY;
+      } else if (SHAPED) {
         float x = capped ? s[e] : s[e] * p.scale_log2;
         const int kp = sm_pos[wave][key];
         x -= slope * fabsf((float)(own - kp));
@@ -757,8 +823,8 @@ __global__ __launch_bounds__(kFewThreads, 2) void chunk_attend_few_kernel(const 
                                       // tokens 29.5 us instead of 28.4, 175 rows of 4 units on 16000 slots 27.2 instead of 24.8)
     }
     l_run = l_run * corr + sum;
-    park(sv, vr);
-    fetch(next, vr, c.V);
+    park(sv, vr, v_scale);
+    fetch(next, vr, v_scale, c.V, c.V_scale);
     wave_lds_fence();
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt) {
@@ -813,6 +879,16 @@ __global__ __launch_bounds__(kFewThreads, 2) void chunk_attend_few_kernel(const 
     *reinterpret_cast<f32x4 *>(p.part_o + prow * D + d0 + 4) = f32x4{o[4], o[5], o[6], o[7]};
     if (d0 == 0) *reinterpret_cast<float2 *>(p.part_ml + 2 * prow) = float2{use, sum};
   }
+}
+
+template <int D, bool SHAPED>
+__global__ __launch_bounds__(kFewThreads, 2) void chunk_attend_few_kernel(const ChunkAttendParams p) {
+  chunk_attend_few<D, SHAPED ? kShaped : kPlain, 0>(p);
+}
+// A draft's tokens; caches of codes.
+template <int D, int MASK, int CODE>
+__global__ __launch_bounds__(kFewThreads, 2) void forms_attend_few_kernel(const ChunkAttendParams p) {
+  chunk_attend_few<D, MASK, CODE>(p);
 }
 
 // The shares of a row together.  grid (ceil(T * G / kMergeRows), units), D / 8 threads a row.

@@ -163,7 +163,7 @@ __device__ __forceinline__ void chunk_add(float (&sum)[kSbTiles], f32x16 (&acc)[
 }
 
 // A wave's keys, 64 from key0 on, as stationary operands.
-template <int D, bool SHAPED>
+template <int D, bool SHAPED, int CODE>
 __device__ __forceinline__ void chunk_keys(bf16x8 (&kf)[kSbTiles][D / 16], int (&kpos)[kSbTiles], const ChunkCache &c, const int32_t *pos, int unit, int n,
                                            int key0, int col, int hf) {
 #pragma unroll
@@ -172,15 +172,17 @@ __device__ __forceinline__ void chunk_keys(bf16x8 (&kf)[kSbTiles][D / 16], int (
     slot = slot < n ? slot : n - 1;
     const size_t row = c.block_table ? paged_row<D>(c.block_table + (size_t)unit * c.max_pages, slot, c.max_pages, c.n_pages)
                                      : ((size_t)unit * c.cap + slot) * D;
-    load_row_frags<D>(kf[kt], reinterpret_cast<const char *>(c.K + row), hf);
+    if (CODE) decode_row_frags<D, CODE>(kf[kt], reinterpret_cast<const uint8_t *>(c.K) + row, c.K_scale + row / kCodeBlock, hf);
+    else load_row_frags<D>(kf[kt], reinterpret_cast<const char *>(c.K + row), hf);
     kpos[kt] = SHAPED ? pos[slot] : slot;
   }
 }
 
 // 1-D grid of ceil(cap / 256) * round_up(units, 8) workgroups, 256 threads.
 // SHAPED, BIASED as in chunk_attend_kernel.
-template <int D, bool SHAPED, bool BIASED>
-__global__ __launch_bounds__(kSbWaves * 64, D == 128 || SHAPED ? 3 : 4) void chunk_scores_kernel(const ChunkScoreParams p) {
+// CODE: the cache holds codes, which become bf16 as the keys are loaded.
+template <int D, bool SHAPED, bool BIASED, int CODE>
+__device__ __forceinline__ void chunk_scores(const ChunkScoreParams &p) {
   using St = SbStage<D>;
   const ChunkCache &c = p.c;
   constexpr int kCsStage = BIASED && D == 128 ? 1 : 2;  // chunks staged at a time, one barrier for all
@@ -203,7 +205,7 @@ __global__ __launch_bounds__(kSbWaves * 64, D == 128 || SHAPED ? 3 : 4) void chu
   bf16x8 kf[kSbTiles][D / 16];
   int kpos[kSbTiles];  // of the lane's keys: slot, or shaped position
   float sum[kSbTiles] = {};
-  chunk_keys<D, SHAPED>(kf, kpos, c, pos, unit, n, key0, col, hf);
+  chunk_keys<D, SHAPED, CODE>(kf, kpos, c, pos, unit, n, key0, col, hf);
   const bool has_keys = key0 < n && key0 + kSbRowsPerWave > skip;  // else: staging and barriers only
   const int k_first = __builtin_amdgcn_readfirstlane(kpos[0]), k_last = __shfl(kpos[kSbTiles - 1], 31);
 
@@ -282,14 +284,23 @@ __global__ __launch_bounds__(kSbWaves * 64, D == 128 || SHAPED ? 3 : 4) void chu
   }
 }
 
+template <int D, bool SHAPED, bool BIASED>
+__global__ __launch_bounds__(kSbWaves * 64, D == 128 || SHAPED ? 3 : 4) void chunk_scores_kernel(const ChunkScoreParams p) {
+  chunk_scores<D, SHAPED, BIASED, 0>(p);
+}
+template <int D, bool SHAPED, bool BIASED, int CODE>
+__global__ __launch_bounds__(kSbWaves * 64, D == 128 || SHAPED ? 3 : 4) void coded_scores_kernel(const ChunkScoreParams p) {
+  chunk_scores<D, SHAPED, BIASED, CODE>(p);
+}
+
 // ---- few keys: 64 of them a workgroup, its eight waves share out the rows ----------------------------------------------------
 // For few units on short caches, where workgroups of 256 slots would leave compute units without work and every wave with all of the rows.  A wave takes
 // every eighth chunk straight from global memory, the next one's on its way while it works on one, no barrier before the end; there the waves' sums
 // are added up in their order.  Bound by the latency of a wave's chain, 1 to 2 us a chunk: 328 tokens of 13 sequences, 16 heads on 1 of 64, 23 us (the kernel
 // above 128).
 constexpr int kCfWaves = 8, kCfKeys = 64;
-template <int D, bool SHAPED, bool BIASED>
-__global__ __launch_bounds__(kCfWaves * 64, 2) void chunk_scores_few_kernel(const ChunkScoreParams p) {
+template <int D, bool SHAPED, bool BIASED, int CODE>
+__device__ __forceinline__ void chunk_scores_few(const ChunkScoreParams &p) {
   const ChunkCache &c = p.c;
   __shared__ __attribute__((aligned(16))) ChunkRows<SHAPED, BIASED, kSbChunk> sm_rows[kCfWaves];
   __shared__ float sm_sum[kCfWaves][kCfKeys];
@@ -310,7 +321,7 @@ __global__ __launch_bounds__(kCfWaves * 64, 2) void chunk_scores_few_kernel(cons
   bf16x8 kf[kSbTiles][D / 16];
   int kpos[kSbTiles];
   float sum[kSbTiles] = {};
-  chunk_keys<D, SHAPED>(kf, kpos, c, pos, unit, n, key0, col, hf);
+  chunk_keys<D, SHAPED, CODE>(kf, kpos, c, pos, unit, n, key0, col, hf);
   const int k_first = __builtin_amdgcn_readfirstlane(kpos[0]), k_last = __shfl(kpos[kSbTiles - 1], 31);
 
   const int i0 = (SHAPED && p.shape.last) || key0 <= base ? 0 : key0 - base;  // (as above)
@@ -370,6 +381,15 @@ __global__ __launch_bounds__(kCfWaves * 64, 2) void chunk_scores_few_kernel(cons
     float *d = p.dst + (size_t)unit * c.cap + slot;
     *d = p.accumulate ? *d + v : v;
   }
+}
+
+template <int D, bool SHAPED, bool BIASED>
+__global__ __launch_bounds__(kCfWaves * 64, 2) void chunk_scores_few_kernel(const ChunkScoreParams p) {
+  chunk_scores_few<D, SHAPED, BIASED, 0>(p);
+}
+template <int D, bool SHAPED, bool BIASED, int CODE>
+__global__ __launch_bounds__(kCfWaves * 64, 2) void coded_scores_few_kernel(const ChunkScoreParams p) {
+  chunk_scores_few<D, SHAPED, BIASED, CODE>(p);
 }
 
 }  // namespace dynts

@@ -15,6 +15,7 @@
 
 #include "attend.hpp"
 #include "chunk.hpp"
+#include "codes.hpp"
 #include "compact.hpp"
 #include "paged.hpp"
 #include "predictor.hpp"
@@ -142,6 +143,9 @@ struct dynts_ctx {
   bool paged = false;
   int32_t *block_table = nullptr, *free_stack = nullptr, *free_top = nullptr;
   int max_pages = 0, n_pages = 0;
+  // codes in place of bf16 (dynts_bind_codes): K and V above are theirs
+  int code = 0;
+  uint8_t *K_scale = nullptr, *V_scale = nullptr;
 };
 
 namespace {
@@ -174,6 +178,12 @@ int check_call(const dynts_ctx *ctx, int32_t layer) {
   return DYNTS_OK;
 }
 
+// The calls that know bf16 caches alone.
+int check_bf16(const dynts_ctx *ctx, int32_t layer) {
+  const int rc = check_call(ctx, layer);
+  return rc == DYNTS_OK && ctx->code ? DYNTS_ECODES : rc;
+}
+
 struct LayerView {
   uint16_t *K, *V;
   float *S;
@@ -189,8 +199,9 @@ LayerView layer_view(const dynts_ctx *ctx, int layer) {
   const size_t units = (size_t)c.batch * c.n_kv_heads;
   const size_t rows = units * c.capacity;
   LayerView v;
-  v.K = ctx->paged ? ctx->K : ctx->K + (size_t)layer * rows * c.head_dim;
-  v.V = ctx->paged ? ctx->V : ctx->V + (size_t)layer * rows * c.head_dim;
+  const size_t row = ctx->code ? c.head_dim / 2 : c.head_dim;  // (in words of 16 bits)
+  v.K = ctx->paged ? ctx->K : ctx->K + (size_t)layer * rows * row;
+  v.V = ctx->paged ? ctx->V : ctx->V + (size_t)layer * rows * row;
   v.block_table = ctx->paged ? ctx->block_table + (size_t)layer * units * ctx->max_pages : nullptr;
   v.S = ctx->S + (size_t)layer * rows;
   v.pos = ctx->pos + (size_t)layer * rows;
@@ -447,6 +458,17 @@ void launch_compact(const dynts::CompactParams &p, const dynts_ctx *ctx, const d
     hipLaunchKernelGGL((dynts::compact_kernel<128, T>), grid, block, 0, st, p);
   } else {
     hipLaunchKernelGGL((dynts::compact_kernel<64, T>), grid, block, 0, st, p);
+  }
+}
+
+void launch_coded_compact(const dynts::CompactParams &p, const dynts::ChunkCache &c, hipStream_t st) {
+  const dim3 grid(6, c.Hkv, c.Nb), block(512);
+  if (c.D == 128) {
+    if (c.block_table) hipLaunchKernelGGL((dynts::coded_compact_kernel<128, true, 512>), grid, block, 0, st, p, c);
+    else hipLaunchKernelGGL((dynts::coded_compact_kernel<128, false, 512>), grid, block, 0, st, p, c);
+  } else {
+    if (c.block_table) hipLaunchKernelGGL((dynts::coded_compact_kernel<64, true, 512>), grid, block, 0, st, p, c);
+    else hipLaunchKernelGGL((dynts::coded_compact_kernel<64, false, 512>), grid, block, 0, st, p, c);
   }
 }
 
@@ -834,7 +856,12 @@ int chunk_cache(const dynts_ctx *ctx, int32_t layer, ChunkCache *out) {
   const LayerView lv = layer_view(ctx, layer);
   *out = ChunkCache{lv.K, lv.V, lv.S, lv.pos, lv.seq_len, lv.next_pos, ctx->n_prompt, ctx->status, lv.block_table, ctx->free_stack, ctx->free_top,
                     ctx->max_pages, ctx->n_pages, c.batch, c.n_q_heads, c.n_kv_heads, ctx->plan.G, c.head_dim, c.capacity, c.score_mode,
-                    c.softmax_scale > 0.f ? c.softmax_scale : 1.0f / std::sqrt((float)c.head_dim)};
+                    c.softmax_scale > 0.f ? c.softmax_scale : 1.0f / std::sqrt((float)c.head_dim), ctx->code, nullptr, nullptr};
+  if (ctx->code) {
+    const size_t scales = ctx->paged ? 0 : (size_t)layer * c.batch * c.n_kv_heads * c.capacity * (c.head_dim / dynts::kCodeBlock);
+    out->K_scale = ctx->K_scale + scales;
+    out->V_scale = ctx->V_scale + scales;
+  }
   return DYNTS_OK;
 }
 
@@ -854,6 +881,7 @@ const char *dynts_strerror(int code) {
     case DYNTS_ENOTBOUND: return "no buffers bound (call dynts_bind)";
     case DYNTS_EWORKSPACE: return "workspace too small or misaligned";
     case DYNTS_EHIP: return "HIP runtime error at kernel launch";
+    case DYNTS_ECODES: return "the cache holds codes, this call takes bf16 caches (see dynts_bind_codes)";
     case DYNTS_EPENDING: return "a score update is outstanding (call dynts_update_scores first)";
     default: return "unknown error";
   }
@@ -911,6 +939,7 @@ int dynts_bind(dynts_ctx *ctx, uint16_t *K, uint16_t *V, float *S, int32_t *pos,
   ctx->run_steps = workspace_bytes >= ctx->plan.run_bytes ? ctx->plan.run_steps : 0;
   ctx->paged = false; ctx->block_table = nullptr; ctx->free_stack = nullptr; ctx->free_top = nullptr;
   ctx->max_pages = ctx->n_pages = 0;
+  ctx->code = 0; ctx->K_scale = ctx->V_scale = nullptr;
   ctx->pending.assign(ctx->pending.size(), 0);
   ctx->hint.assign(ctx->hint.size(), 0);
   ctx->spill_layer = -1;
@@ -936,9 +965,23 @@ int dynts_bind_paged(dynts_ctx *ctx, uint16_t *K_pool, uint16_t *V_pool, int32_t
   return DYNTS_OK;
 }
 
+int dynts_bind_codes(dynts_ctx *ctx, const dynts_codes *codes, float *S, int32_t *pos, int32_t *seq_len, int32_t *next_pos, int32_t *n_prompt,
+                     void *workspace, size_t workspace_bytes, int32_t *status) {
+  if (!ctx || !codes || !codes->K_scale || !codes->V_scale) return DYNTS_ENULL;
+  if (codes->code != DYNTS_CODE_E4M3 && codes->code != DYNTS_CODE_INT8) return DYNTS_EINVAL;
+  if ((reinterpret_cast<uintptr_t>(codes->K_scale) | reinterpret_cast<uintptr_t>(codes->V_scale)) % 16) return DYNTS_EINVAL;
+  uint16_t *const K = reinterpret_cast<uint16_t *>(codes->K), *const V = reinterpret_cast<uint16_t *>(codes->V);
+  const int rc = codes->block_table ? dynts_bind_paged(ctx, K, V, codes->n_pages, codes->block_table, codes->max_pages, codes->free_stack, codes->free_top, S,
+                                                       pos, seq_len, next_pos, n_prompt, workspace, workspace_bytes, status)
+                                    : dynts_bind(ctx, K, V, S, pos, seq_len, next_pos, n_prompt, workspace, workspace_bytes, status);
+  if (rc != DYNTS_OK) return rc;
+  ctx->code = codes->code; ctx->K_scale = codes->K_scale; ctx->V_scale = codes->V_scale;
+  return DYNTS_OK;
+}
+
 int dynts_prefill(dynts_ctx *ctx, int32_t layer, const uint16_t *K0, const uint16_t *V0, int32_t m_max,
                   const int32_t *m, void *stream) {
-  int rc = check_call(ctx, layer);
+  int rc = check_bf16(ctx, layer);
   if (rc != DYNTS_OK) return rc;
   if (!K0 || !V0 || !m) return DYNTS_ENULL;
   if (m_max <= 0) return DYNTS_EINVAL;
@@ -971,7 +1014,7 @@ int dynts_prefill(dynts_ctx *ctx, int32_t layer, const uint16_t *K0, const uint1
 
 int dynts_append(dynts_ctx *ctx, int32_t layer, const uint16_t *k_new, const uint16_t *v_new, const float *s_new,
                  const uint8_t *active, void *stream) {
-  int rc = check_call(ctx, layer);
+  int rc = check_bf16(ctx, layer);
   if (rc != DYNTS_OK) return rc;
   if (!k_new || !v_new) return DYNTS_ENULL;
   const dynts_config &c = ctx->cfg;
@@ -997,7 +1040,7 @@ int dynts_append(dynts_ctx *ctx, int32_t layer, const uint16_t *k_new, const uin
 
 int dynts_decode_attend(dynts_ctx *ctx, int32_t layer, const uint16_t *q, const uint8_t *active, float *out,
                         float *lse, void *stream) {
-  int rc = check_call(ctx, layer);
+  int rc = check_bf16(ctx, layer);
   if (rc != DYNTS_OK) return rc;
   if (!q || !out) return DYNTS_ENULL;
   if (reinterpret_cast<uintptr_t>(q) % 16) return DYNTS_EINVAL;
@@ -1043,7 +1086,7 @@ int dynts_update_scores(dynts_ctx *ctx, int32_t layer, void *stream) {
 
 int dynts_decode_attend_update(dynts_ctx *ctx, int32_t layer, const uint16_t *q, const uint8_t *active,
                                float *out, float *lse, void *stream) {
-  int rc = check_call(ctx, layer);
+  int rc = check_bf16(ctx, layer);
   if (rc != DYNTS_OK) return rc;
   if (!q || !out) return DYNTS_ENULL;
   if (reinterpret_cast<uintptr_t>(q) % 16) return DYNTS_EINVAL;
@@ -1054,7 +1097,7 @@ int dynts_decode_attend_update(dynts_ctx *ctx, int32_t layer, const uint16_t *q,
 int dynts_decode_step(dynts_ctx *ctx, int32_t layer, const uint16_t *q, const uint16_t *k_new,
                       const uint16_t *v_new, const float *s_new, const uint8_t *active, float *out, float *lse,
                       void *stream) {
-  int rc = check_call(ctx, layer);
+  int rc = check_bf16(ctx, layer);
   if (rc != DYNTS_OK) return rc;
   if (!q || !out || !k_new || !v_new) return DYNTS_ENULL;
   const bool ext = ctx->cfg.score_mode == DYNTS_SCORE_EXTERNAL;
@@ -1068,7 +1111,7 @@ int dynts_decode_step(dynts_ctx *ctx, int32_t layer, const uint16_t *q, const ui
 int dynts_decode_step_static(dynts_ctx *ctx, int32_t layer, const uint16_t *q, const uint16_t *k_new,
                              const uint16_t *v_new, const float *s_new, const uint8_t *active, float *out, float *lse,
                              void *stream) {
-  int rc = check_call(ctx, layer);
+  int rc = check_bf16(ctx, layer);
   if (rc != DYNTS_OK) return rc;
   if (!q || !out || !k_new || !v_new) return DYNTS_ENULL;
   const bool ext = ctx->cfg.score_mode == DYNTS_SCORE_EXTERNAL;
@@ -1100,7 +1143,7 @@ int dynts_decode_step_static(dynts_ctx *ctx, int32_t layer, const uint16_t *q, c
 }
 
 int dynts_hint_trigger(dynts_ctx *ctx, int32_t layer) {
-  const int rc = check_call(ctx, layer);
+  const int rc = check_bf16(ctx, layer);
   if (rc != DYNTS_OK) return rc;
   ctx->hint[layer] = 1;
   return DYNTS_OK;
@@ -1148,7 +1191,12 @@ int dynts_compact(dynts_ctx *ctx, int32_t layer, const uint8_t *trigger, const i
                          c.n_kv_heads, c.capacity, keep_stride};
   const dynts::PagedView pv{lv.K, lv.V, lv.block_table, ctx->free_stack, ctx->free_top, ctx->max_pages, ctx->n_pages};
   hipStream_t st = static_cast<hipStream_t>(stream);
-  if (compact_threads(ctx) == 256) launch_compact<256>(p, ctx, pv, st);
+  if (ctx->code) {
+    dynts::ChunkCache cc;
+    rc = dynts::chunk_cache(ctx, layer, &cc);
+    if (rc != DYNTS_OK) return rc;
+    launch_coded_compact(p, cc, st);
+  } else if (compact_threads(ctx) == 256) launch_compact<256>(p, ctx, pv, st);
   else launch_compact<512>(p, ctx, pv, st);
   if (ctx->paged)
     hipLaunchKernelGGL(dynts::paged_trim_kernel, dim3((c.batch + 63) / 64), dim3(64), 0, st, pv, trigger, new_len,
@@ -1187,7 +1235,7 @@ size_t dynts_score_block_scratch_bytes(const dynts_config *cfg, int32_t n_querie
 int dynts_score_block(dynts_ctx *ctx, int32_t layer, const uint16_t *q_blk, const uint16_t *k_blk,
                       int32_t n_queries, const uint8_t *active, float *dst, int32_t accumulate, void *scratch,
                       size_t scratch_bytes, void *stream) {
-  int rc = check_call(ctx, layer);
+  int rc = check_bf16(ctx, layer);
   if (rc != DYNTS_OK) return rc;
   if (!q_blk || !scratch) return DYNTS_ENULL;
   if (n_queries <= 0 || n_queries > (1 << 20)) return DYNTS_EINVAL;
@@ -1341,7 +1389,7 @@ int dynts_decode_loop(dynts_ctx *ctx, int32_t n_steps, const uint16_t *q, const 
                       const uint16_t *v_new, const float *s_new, const uint8_t *active, const uint8_t *evict_steps,
                       const uint8_t *trigger, float *out, size_t out_step_stride, int32_t *keep_idx,
                       int32_t *new_len, void *stream) {
-  int rc = check_call(ctx, 0);
+  int rc = check_bf16(ctx, 0);
   if (rc != DYNTS_OK) return rc;
   if (n_steps < 0) return DYNTS_EINVAL;
   if (!q || !k_new || !v_new || !out) return DYNTS_ENULL;

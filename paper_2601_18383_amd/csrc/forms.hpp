@@ -1,0 +1,21 @@
+// Launches of the kernels for caches of codes and for drafts that branch (forms.hip).
+#pragma once
+#include "chunk_attend.hpp"
+#include "chunk_scores.hpp"
+
+namespace dynts {
+
+// tokens of a draft (tree_keep_kernel has them in LDS)
+constexpr int kTreeMost = 4096;
+
+// chunk_attend_few_kernel's other forms: mask kTree, or a cache of codes with any mask.
+__attribute__((visibility("hidden"))) void launch_few_form(const ChunkAttendParams &p, int mask, unsigned grid, hipStream_t st);
+// a draft's tokens, many rows
+__attribute__((visibility("hidden"))) void launch_tree_attend(const ChunkAttendParams &p, unsigned grid, hipStream_t st);
+__attribute__((visibility("hidden"))) void launch_coded_scores(const ChunkScoreParams &p, bool few, bool shaped, bool biased, unsigned grid, hipStream_t st);
+// small: one launch that makes room and writes; else (behind chunk_reserve_kernel) `blocks` workgroups a sequence that write
+__attribute__((visibility("hidden"))) void launch_coded_append(const ChunkAppendParams &p, bool small, unsigned blocks, hipStream_t st);
+// rows of any cache as bf16
+__attribute__((visibility("hidden"))) void launch_read_rows(const ChunkCache &c, const int32_t *first, int n_rows, uint16_t *K, uint16_t *V, hipStream_t st);
+
+}  // namespace dynts
