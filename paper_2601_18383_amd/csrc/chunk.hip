@@ -30,6 +30,7 @@ int launch_status() { return hipGetLastError() == hipSuccess ? DYNTS_OK : DYNTS_
 // scratch of a chunk's calls
 struct ChunkPlan {
   bool few;          // chunk_attend_few_kernel
+  bool token;        // coded_token_kernel
   int rows, blocks;  // query rows of a workgroup, row blocks of a unit
   int n_split, Rpad;
   size_t off_lse = 0, off_n = 0, off_ml = 0, off_o = 0, bytes = 0;
@@ -57,22 +58,44 @@ constexpr long long kMostPartials = 65536;
 //     32.0, of 4000 42.9 / 47.5; head_dim 64, 128 units of 6000 1 / 2: 30.8 / 35.2, 10 of 1500 9.9 / 10.4
 //   many rows, W = 64, 4500 slots 1 / 4 / 8 / 16: 94.9 / 41.6 / 37.3 / 37.1, 1000 1 / 2: 24.8 / 28.1; W = 128 of 1000 1 / 2 / 4: 25.4 / 30.5 / 31.4; W = 256 of 4500
 //     1 / 2 / 4: 97.8 / 84.7 / 84.4, of 1000 25.6 / 33.2 / 33.2; W = 16 of 16000 8 / 16 / 31: 50.9 / 35.4 / 36.4
-ChunkPlan chunk_plan(const dynts_config &c, int n_tokens, int slots, bool far_cap = false) {
+//
+// Caches of codes (the kernel for many rows then has them unpacked before, 0.22 us per 1000 slots of a unit): by the estimates below, in us.  Few / many, both as
+// measured:
+//   head_dim 128, 8 units: 4500 slots R = 512 27.5 / 37.3 (e4m3), 32.9 / 37.5 (whole numbers); 16000 slots R = 256 - / 57, R = 512 92 / 71; 32 units: 1500 slots
+//     R = 512 44.8 / 39.8, 4500 R = 256 53 / 64, R = 512 70 / 77 and 89 / 77; 128 units: 500 slots R = 128 20 / 27, R = 256 44 / 29, 4500 R = 128 79 / 158, R = 256
+//     202 / 175
+//   head_dim 64, 8 units: 4500 slots R = 1024 28 / 31 and 35 / 31; 32 units: 500 slots R = 1024 19 / 20 and 23 / 20, R = 2048 38 / 25, 4500 R = 512 45 / 46, R = 1024
+//     82 / 68
+// A draft's shares stop at one workgroup a compute unit while they have less than 1536 slots (us, 128 units of 2480 slots by their number, R = 112 1 / 2 / 4: 59 /
+// 47 / 51; R = 224 1 / 2: 67 / 66).
+ChunkPlan chunk_plan(const dynts_config &c, int n_tokens, int slots, bool far_cap = false, bool codes = false, bool tree = false) {
   ChunkPlan pl;
   const long long R = (long long)n_tokens * (c.n_q_heads / c.n_kv_heads), units = (long long)c.batch * c.n_kv_heads;
   const long long F = units * ((R + dynts::kFewRows - 1) / dynts::kFewRows), W = units * ((R + dynts::kChRows - 1) / dynts::kChRows);
-  pl.few = far_cap || R <= dynts::kFewRows || (F <= (c.head_dim == 128 ? 256 : 512) && (R <= 2 * dynts::kFewRows || F * slots <= 1 << 20));
-  pl.rows = pl.few ? dynts::kFewRows : dynts::kChRows;
+  const int room = c.head_dim == 128 ? 256 : 512;  // workgroups of few rows that the chip holds
+  pl.few = far_cap || R <= dynts::kFewRows || (F <= room && (R <= 2 * dynts::kFewRows || F * slots <= 1 << 20));
+  if (codes && !far_cap && R > dynts::kFewRows) {
+    const double all = (double)units * slots, cut = F < room ? (room / F < 16 ? room / F : 16) : 1;
+    const double few = (F > room ? (double)F / room : 1.0) * (6.5 + 0.0087 * slots / cut) + (cut > 1 ? 4 : 0);
+    const double many = 18 + all * c.head_dim * 1.7e-6 + all * R * (c.head_dim == 128 ? 3e-7 : 2e-7);
+    pl.few = few < many;
+  }
+  pl.token = codes && !tree && R <= dynts::kTokRows;
+  pl.rows = pl.token ? dynts::kTokRows : pl.few ? dynts::kFewRows : dynts::kChRows;
   pl.blocks = (int)((R + pl.rows - 1) / pl.rows);
   pl.Rpad = pl.blocks * pl.rows;
   long long shares = slots / (32 * dynts::kShareTiles);
-  if (pl.few) {
+  if (pl.token) {
+    shares = shares < 32 ? shares : 32;
+    shares = shares < 256 / units ? shares : 256 / units;
+  } else if (pl.few) {
     shares = shares < 16 ? shares : 16;
     shares = shares < 256 / F ? shares : 256 / F;
     if (shares < 3 && units > 64) shares = 1;
   } else {
     shares = shares < 32 ? shares : 32;
     shares = shares < 512 / W ? shares : 512 / W;
+    if (tree && W * shares > 256 && slots / shares < 1536) shares = 256 / W;
   }
   if (slots < 1536) shares = 1;
   while (shares > 1 && units * pl.Rpad * shares > kMostPartials) --shares;
@@ -101,17 +124,19 @@ dynts_config config_of(const ChunkCache &c) {
   cfg.batch = c.Nb; cfg.n_q_heads = c.Hq; cfg.n_kv_heads = c.Hkv; cfg.head_dim = c.D; cfg.capacity = c.cap;
   return cfg;
 }
-ChunkPlan chunk_plan(const ChunkCache &c, int n_tokens, const dynts_shaping *shaping = nullptr) {
+// tree: for a draft
+ChunkPlan chunk_plan(const ChunkCache &c, int n_tokens, const dynts_shaping *shaping, bool tree) {
   // (slots of a window: no more than its positions, those of the chunk's other tokens beside them)
   const long long seen = shaping && shaping->window > 0 ? (long long)shaping->window + n_tokens : c.cap;
-  return chunk_plan(config_of(c), n_tokens, (int)(seen < c.cap ? seen : c.cap), far_cap(shaping));
+  return chunk_plan(config_of(c), n_tokens, (int)(seen < c.cap ? seen : c.cap), far_cap(shaping), c.code != 0, tree);
 }
 
 // Room behind a chunk's scratch where the layer's codes lie as bf16, for the kernel of many rows.
 size_t unpacked_bytes(const dynts_config &c) { return align_up((size_t)c.batch * c.n_kv_heads * c.capacity * c.head_dim * 2); }
 size_t scratch_bytes_of(const dynts_config &c, int n_tokens, bool codes) {
-  const ChunkPlan pl = chunk_plan(c, n_tokens, c.capacity);
-  return pl.bytes + (codes && !pl.few ? 2 * unpacked_bytes(c) : 0);
+  // (which kernel a shorter chunk takes goes by its sizes: the room is there for all that may be of many rows)
+  const bool many = (long long)n_tokens * (c.n_q_heads / c.n_kv_heads) > dynts::kFewRows;
+  return chunk_plan(c, n_tokens, c.capacity).bytes + (codes && many ? 2 * unpacked_bytes(c) : 0);
 }
 size_t scratch_bytes_of(const ChunkCache &c, int n_tokens) { return scratch_bytes_of(config_of(c), n_tokens, c.code != 0); }
 
@@ -193,19 +218,24 @@ unsigned chunk_grid(const ChunkCache &c, long long blocks, int threads) {
   return wgs >= (1LL << 32) / threads ? 0u : (unsigned)wgs;
 }
 unsigned attend_grid(const ChunkCache &c, const ChunkPlan &pl) {
-  return chunk_grid(c, (long long)pl.blocks * pl.n_split, pl.few ? dynts::kFewThreads : dynts::kChThreads);
+  return chunk_grid(c, (long long)pl.blocks * pl.n_split, pl.token ? dynts::kTokWaves * 64 : pl.few ? dynts::kFewThreads : dynts::kChThreads);
 }
 // Which kernel of chunk_scores.hpp.  C: chunks of 32 rows of a unit, W: workgroups of 64 slots, one a compute unit.  Few slots: 7 + C / 4 us a round of 256 of
 // them; many: 4 + 0.8 C us while its W / 4 workgroups have a compute unit each.  us, few / many:
 //   head_dim 128: C = 66, W = 168 21.9 / 60.4, W = 672 60.9 / 61.5; C = 219, W = 152 57.0 / 170, W = 512 97.6 / 184; C = 389, W = 432 100 / 304; C = 112,
 //     W = 752 93.1 / 92.2, W = 1504 183 / 122; C = 14, W = 640 26.3 / 16.8; C = 2, W = 568 14.5 / 5.9
 //   head_dim 64: C = 164, W = 78 23.1 / 128; C = 10, W = 64 6.0 / 10.9; C = 38, W = 288 15.7 / 29.8, W = 1152 38.2 / 40.2
+bool scores_token(const ChunkCache &c, int n_tokens);
 bool scores_few(const ChunkCache &c, int n_tokens, const dynts_shaping *shaping) {
+  if (scores_token(c, n_tokens)) return false;
   if (far_cap(shaping)) return true;  // (the other one does not know it)
   const long long W = (long long)c.Nb * c.Hkv * ((c.cap + dynts::kCfKeys - 1) / dynts::kCfKeys);
   const long long C = ((long long)n_tokens * c.G + dynts::kSbChunk - 1) / dynts::kSbChunk;
   return W <= 256 ? C >= 8 : W <= 512 && C >= 32;
 }
+// coded_token_scores_kernel
+bool scores_token(const ChunkCache &c, int n_tokens) { return c.code && (long long)n_tokens * c.G <= dynts::kTokRows; }
+static_assert(dynts::kTsKeys == dynts::kCsKeys, "one grid for both");
 unsigned scores_grid(const ChunkCache &c, bool few) {
   return few ? chunk_grid(c, (c.cap + dynts::kCfKeys - 1) / dynts::kCfKeys, dynts::kCfWaves * 64)
              : chunk_grid(c, (c.cap + dynts::kCsKeys - 1) / dynts::kCsKeys, dynts::kSbWaves * 64);
@@ -213,7 +243,8 @@ unsigned scores_grid(const ChunkCache &c, bool few) {
 
 template <int D, bool SHAPED>
 void launch_attend_d(const dynts::ChunkAttendParams &p, const ChunkPlan &pl, unsigned grid, hipStream_t st) {
-  if (pl.few && (p.seen || p.c.code)) dynts::launch_few_form(p, p.seen ? dynts::kTree : SHAPED ? dynts::kShaped : dynts::kPlain, grid, st);
+  if (pl.token) dynts::launch_coded_token(p, SHAPED, grid, st);
+  else if (pl.few && (p.seen || p.c.code)) dynts::launch_few_form(p, p.seen ? dynts::kTree : SHAPED ? dynts::kShaped : dynts::kPlain, grid, st);
   else if (p.seen) dynts::launch_tree_attend(p, grid, st);
   else if (pl.few) hipLaunchKernelGGL((dynts::chunk_attend_few_kernel<D, SHAPED>), dim3(grid), dim3(dynts::kFewThreads), 0, st, p);
   else if (SHAPED && p.shape.slope) hipLaunchKernelGGL((dynts::chunk_attend_kernel<D, SHAPED, SHAPED, false>), dim3(grid), dim3(dynts::kChThreads), 0, st, p);
@@ -221,8 +252,10 @@ void launch_attend_d(const dynts::ChunkAttendParams &p, const ChunkPlan &pl, uns
   else hipLaunchKernelGGL((dynts::chunk_attend_kernel<D, SHAPED, false, false>), dim3(grid), dim3(dynts::kChThreads), 0, st, p);
   if (p.n_split > 1) {
     constexpr int rows = dynts::kMergeThreads / (D / 8);
-    hipLaunchKernelGGL(dynts::chunk_merge_kernel<D>, dim3((p.T * p.c.G + rows - 1) / rows, p.c.Nb * p.c.Hkv), dim3(dynts::kMergeThreads), 0, st, p,
-                       pl.rows);
+    const dim3 merge((p.T * p.c.G + rows - 1) / rows, p.c.Nb * p.c.Hkv), threads(dynts::kMergeThreads);
+    if (p.n_split > 4) hipLaunchKernelGGL((dynts::chunk_merge_kernel<D, 16>), merge, threads, 0, st, p, pl.rows);
+    else if (p.n_split > 2) hipLaunchKernelGGL((dynts::chunk_merge_kernel<D, 4>), merge, threads, 0, st, p, pl.rows);
+    else hipLaunchKernelGGL((dynts::chunk_merge_kernel<D, 2>), merge, threads, 0, st, p, pl.rows);
   }
 }
 
@@ -236,7 +269,7 @@ struct Fresh {
 // seen: of a draft's tokens, or null
 int launch_attend(ChunkCache c, const uint16_t *q, int n_tokens, const int32_t *n_new, const dynts_shaping *shaping, const uint32_t *seen, uint16_t *out,
                   float *lse, void *scratch, const Fresh &fresh, hipStream_t st) {
-  const ChunkPlan pl = chunk_plan(c, n_tokens, shaping);
+  const ChunkPlan pl = chunk_plan(c, n_tokens, shaping, seen != nullptr);
   char *const base = static_cast<char *>(scratch);
   if (c.code && !pl.few) {  // the codes as bf16, in a dense cache in scratch
     uint16_t *const K = reinterpret_cast<uint16_t *>(base + pl.bytes), *const V = reinterpret_cast<uint16_t *>(base + pl.bytes + unpacked_bytes(config_of(c)));
@@ -281,7 +314,8 @@ int launch_scores(const ChunkCache &c, const uint16_t *q, int n_tokens, const in
   const bool few = scores_few(c, n_tokens, shaping);
   const unsigned grid = scores_grid(c, few);
   if (!grid) return DYNTS_EINVAL;
-  if (c.code) dynts::launch_coded_scores(p, few, shaped(p.shape), p.shape.slope != nullptr, grid, st);
+  if (scores_token(c, n_tokens)) dynts::launch_coded_token_scores(p, shaped(p.shape), grid, st);
+  else if (c.code) dynts::launch_coded_scores(p, few, shaped(p.shape), p.shape.slope != nullptr, grid, st);
   else if (c.D == 128) launch_scores_d<128>(p, few, grid, st);
   else launch_scores_d<64>(p, few, grid, st);
   return launch_status();
@@ -295,7 +329,7 @@ int check_draft(const ChunkCache &c, const uint16_t *q, int n_tokens, const uint
   if (misaligned(q, 16) || misaligned(out, 16) || misaligned(seen, 4)) return DYNTS_EINVAL;
   const size_t q_bytes = (size_t)c.Nb * n_tokens * c.Hq * c.D * 2;
   if (overlap(out, q_bytes, q, q_bytes)) return DYNTS_EINVAL;
-  return attend_grid(c, chunk_plan(c, n_tokens)) ? DYNTS_OK : DYNTS_EINVAL;
+  return attend_grid(c, chunk_plan(c, n_tokens, nullptr, true)) ? DYNTS_OK : DYNTS_EINVAL;
 }
 
 }  // namespace
@@ -363,7 +397,7 @@ int dynts_chunk_step(dynts_ctx *ctx, int32_t layer, const uint16_t *q, const uin
   if (rc != DYNTS_OK) return rc;
   if (!q || !out) return DYNTS_ENULL;
   if (misaligned(q, 16) || misaligned(out, 16)) return DYNTS_EINVAL;
-  const ChunkPlan pl = chunk_plan(c, n_tokens, shaping);
+  const ChunkPlan pl = chunk_plan(c, n_tokens, shaping, false);
   rc = check_scratch(scratch, scratch_bytes, c.code ? scratch_bytes_of(c, n_tokens) : pl.bytes);
   if (rc != DYNTS_OK) return rc;
   hipStream_t st = static_cast<hipStream_t>(stream);

@@ -732,7 +732,11 @@ __device__ __forceinline__ void chunk_attend_few(const ChunkAttendParams &p) {
   for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc[dt][e] = 0.f;
-  float m_run = -INFINITY, l_run = 0.f;
+  // LAZY (drafts, caches of codes): a shift that is only raised, as in chunk_attend_rows; it saves a tile the scaling of its outputs, and the exchange
+  // between the halves.  (512 rows of 32 units on 4500 slots of codes 70 us instead of 82; with head_dim 64 there are no registers for both branches, 150 instead of
+  // 82.)
+  constexpr bool LAZY = (TREE || CODE) && D == 128;
+  float m_run = LAZY ? -1e30f : -INFINITY, l_run = 0.f;
 
   char *const sk = sm[wave], *const sv = sm[wave] + Lds::kTileBytes;
   constexpr int PPR = CODE ? D / 16 : D / 8, PIECES = kFewTile * PPR / 64;  // 16-byte pieces a row, and of K or V a lane
@@ -789,38 +793,86 @@ __device__ __forceinline__ void chunk_attend_few(const ChunkAttendParams &p) {
       const bf16x8 kf = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(sk + chunk_lds<D>(col, 2 * ks + hf)));
       s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], s, 0, 0, 0);
     }
-    float mx = -INFINITY;
     const bool capped = SHAPED && p.shape.cap > 0.f;
     if (capped) soft_caps<true>(s, p.scale_log2, p.shape);
-    uint32_t sees = ~0u;
-    if (TREE && t + kFewTile > base) sees = tree_bits(bits, p.words, t, base, n) >> (4 * hf);
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const int key = 8 * (e >> 2) + 4 * hf + (e & 3);
-      if (TREE) {
-        s[e] = sees >> (8 * (e >> 2) + (e & 3)) & 1u ? s[e] * p.scale_log2 : -INFINITY;
-      } else if (SHAPED) {
-        float x = capped ? s[e] : s[e] * p.scale_log2;
-        const int kp = sm_pos[wave][key];
-        x -= slope * fabsf((float)(own - kp));
-        s[e] = (uint32_t)(kp - lo) <= span ? x : -INFINITY;
-      } else {
-        s[e] = t + key <= lim ? s[e] * p.scale_log2 : -INFINITY;
-      }
-      mx = fmaxf(mx, s[e]);
-    }
-    mx = fmaxf(mx, __shfl_xor(mx, 32));
-    const float m_next = fmaxf(m_run, mx), m_use = m_next == -INFINITY ? 0.f : m_next;
-    const float corr = fast_exp2(m_run - m_use);
-    m_run = m_next;
-    float sum = 0.f;
+    float corr = 1.f, sum;
     bf16x8 pf[2];
+    if constexpr (LAZY) {
+      const float scale = SHAPED ? 1.f : p.scale_log2;
+      if (SHAPED) {
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const float w = fast_exp2(s[e] - m_use);
-      sum += w;
-      pf[e >> 3][e & 7] = (__bf16)w;  // (half a step of 2^-8, as the output's rounding; with the low part as well, as single steps have it, drafts of four
-                                      // tokens 29.5 us instead of 28.4, 175 rows of 4 units on 16000 slots 27.2 instead of 24.8)
+        for (int e = 0; e < 16; ++e) {
+          const int kp = sm_pos[wave][8 * (e >> 2) + 4 * hf + (e & 3)];
+          const float x = (capped ? s[e] : s[e] * p.scale_log2) - slope * fabsf((float)(own - kp));
+          s[e] = (uint32_t)(kp - lo) <= span ? x : -INFINITY;
+        }
+      } else if (t + kFewTile > base) {
+        asm volatile("; some keys are hidden");
+        const uint32_t sees = TREE ? tree_bits(bits, p.words, t, base, n) >> (4 * hf) : 0u;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int key = 8 * (e >> 2) + (e & 3);
+          if (TREE ? !(sees >> key & 1u) : t + 4 * hf + key > lim) s[e] = -INFINITY;
+        }
+      }
+      auto fold = [&]() {
+        float q[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          float w[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            w[e] = fast_exp2(fmaf(s[4 * k + e], scale, -m_run));
+            pf[k >> 1][4 * (k & 1) + e] = (__bf16)w[e];  // (half a step of 2^-8, as the output's rounding)
+          }
+          q[k] = (w[0] + w[1]) + (w[2] + w[3]);
+        }
+        return (q[0] + q[1]) + (q[2] + q[3]);
+      };
+      sum = fold();
+      if (__any(!(sum < kChLimit))) {
+        float mx = s[0];
+#pragma unroll
+        for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[e]);
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        const float next_m = fmaxf(ceilf(mx * scale), m_run), f = fast_exp2(m_run - next_m);
+        l_run *= f;
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt) acc[dt] *= f;
+        m_run = next_m;
+        sum = fold();
+      }
+    } else {
+      float mx = -INFINITY;
+      uint32_t sees = ~0u;
+      if (TREE && t + kFewTile > base) sees = tree_bits(bits, p.words, t, base, n) >> (4 * hf);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int key = 8 * (e >> 2) + 4 * hf + (e & 3);
+        if (TREE) {
+          s[e] = sees >> (8 * (e >> 2) + (e & 3)) & 1u ? s[e] * p.scale_log2 : -INFINITY;
+        } else if (SHAPED) {
+          float x = capped ? s[e] : s[e] * p.scale_log2;
+          const int kp = sm_pos[wave][key];
+          x -= slope * fabsf((float)(own - kp));
+          s[e] = (uint32_t)(kp - lo) <= span ? x : -INFINITY;
+        } else {
+          s[e] = t + key <= lim ? s[e] * p.scale_log2 : -INFINITY;
+        }
+        mx = fmaxf(mx, s[e]);
+      }
+      mx = fmaxf(mx, __shfl_xor(mx, 32));
+      const float m_next = fmaxf(m_run, mx), m_use = m_next == -INFINITY ? 0.f : m_next;
+      corr = fast_exp2(m_run - m_use);
+      m_run = m_next;
+      sum = 0.f;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float w = fast_exp2(s[e] - m_use);
+        sum += w;
+        pf[e >> 3][e & 7] = (__bf16)w;  // (half a step of 2^-8, as the output's rounding; with the low part as well, as single steps have it, drafts of four
+                                        // tokens 29.5 us instead of 28.4, 175 rows of 4 units on 16000 slots 27.2 instead of 24.8)
+      }
     }
     l_run = l_run * corr + sum;
     park(sv, vr, v_scale);
@@ -828,7 +880,7 @@ __device__ __forceinline__ void chunk_attend_few(const ChunkAttendParams &p) {
     wave_lds_fence();
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt) {
-      acc[dt] *= corr;
+      if (!LAZY) acc[dt] *= corr;
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks) {
         const int vrow = 16 * ks + 4 * hf + (r16 >> 2), piece = 4 * dt + 2 * ((lane >> 4) & 1) + ((r16 >> 1) & 1);
@@ -887,36 +939,41 @@ __global__ __launch_bounds__(kFewThreads, 2) void chunk_attend_few_kernel(const 
 }
 // A draft's tokens; caches of codes.
 template <int D, int MASK, int CODE>
-__global__ __launch_bounds__(kFewThreads, 2) void forms_attend_few_kernel(const ChunkAttendParams p) {
+__global__ __launch_bounds__(kFewThreads, D == 64 && MASK != kShaped ? 4 : 2) void forms_attend_few_kernel(const ChunkAttendParams p) {
   chunk_attend_few<D, MASK, CODE>(p);
 }
 
-// The shares of a row together.  grid (ceil(T * G / kMergeRows), units), D / 8 threads a row.
+// The shares of a row together.  grid (ceil(T * G / kMergeRows), units), D / 8 threads a row.  AT_ONCE: shares that are asked for at a time, the first ones
+// before it is known how many there are (16 of single tokens of 8 units: 3.1 us instead of 5.4 with four).
 constexpr int kMergeThreads = 256;
-template <int D>
+template <int D, int AT_ONCE>
 __global__ __launch_bounds__(kMergeThreads) void chunk_merge_kernel(const ChunkAttendParams p, int block_rows) {
   const ChunkCache &c = p.c;
   const int unit = blockIdx.y, b = unit / c.Hkv, h = unit - b * c.Hkv;
-  int n;
-  const int m = chunk_tokens(c, p.n_new, p.T, b, n);
   const int r = blockIdx.x * (kMergeThreads / (D / 8)) + threadIdx.x / (D / 8), d0 = 8 * (threadIdx.x % (D / 8));
-  if (r >= m * c.G) return;
-  const int shares = p.part_n[unit * (p.Rpad / block_rows) + r / block_rows];
-  if (shares == 1) return;
+  if (r >= p.T * c.G) return;
   const size_t first = (size_t)unit * p.n_split * p.Rpad + r;
-  float top = -INFINITY, sum = 0.f, o[8] = {};
-  for (int s0 = 0; s0 < shares; s0 += 4) {  // four shares' loads at a time
-    float2 ml[4];
-    f32x4 a[4], z[4];
+  float2 ml[AT_ONCE];
+  f32x4 a[AT_ONCE], z[AT_ONCE];
+  auto fetch = [&](int s0) {
 #pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      const size_t prow = first + (size_t)(s0 + s < shares ? s0 + s : s0) * p.Rpad;
+    for (int s = 0; s < AT_ONCE; ++s) {
+      const size_t prow = first + (size_t)(s0 + s < p.n_split ? s0 + s : s0) * p.Rpad;
       ml[s] = *reinterpret_cast<const float2 *>(p.part_ml + 2 * prow);
       a[s] = *reinterpret_cast<const f32x4 *>(p.part_o + prow * D + d0);
       z[s] = *reinterpret_cast<const f32x4 *>(p.part_o + prow * D + d0 + 4);
     }
+  };
+  fetch(0);
+  const int shares = p.part_n[unit * (p.Rpad / block_rows) + r / block_rows];
+  int n;
+  const int m = chunk_tokens(c, p.n_new, p.T, b, n);
+  if (r >= m * c.G || shares == 1) return;
+  float top = -INFINITY, sum = 0.f, o[8] = {};
+  for (int s0 = 0; s0 < shares; s0 += AT_ONCE) {
+    if (s0 > 0) fetch(s0);
 #pragma unroll
-    for (int s = 0; s < 4; ++s) {
+    for (int s = 0; s < AT_ONCE; ++s) {
       if (s0 + s >= shares || !(ml[s].y > 0.f)) continue;  // (a share without a key that the row sees)
       const float next = fmaxf(top, ml[s].x), f = fast_exp2(top - next), w = fast_exp2(ml[s].x - next);
       top = next;

@@ -25,6 +25,35 @@ void launch_few_form(const ChunkAttendParams &p, int mask, unsigned grid, hipStr
   }
 }
 
+template <int D, int CODE>
+static void coded_token(const ChunkAttendParams &p, bool shaped, unsigned grid, hipStream_t st) {
+  if (shaped) hipLaunchKernelGGL((coded_token_kernel<D, kShaped, CODE, kTokWaves>), dim3(grid), dim3(kTokWaves * 64), 0, st, p);
+  else hipLaunchKernelGGL((coded_token_kernel<D, kPlain, CODE, kTokWaves>), dim3(grid), dim3(kTokWaves * 64), 0, st, p);
+}
+void launch_coded_token(const ChunkAttendParams &p, bool shaped, unsigned grid, hipStream_t st) {
+  if (p.c.D == 128) {
+    if (p.c.code == DYNTS_CODE_E4M3) coded_token<128, DYNTS_CODE_E4M3>(p, shaped, grid, st);
+    else coded_token<128, DYNTS_CODE_INT8>(p, shaped, grid, st);
+  } else {
+    if (p.c.code == DYNTS_CODE_E4M3) coded_token<64, DYNTS_CODE_E4M3>(p, shaped, grid, st);
+    else coded_token<64, DYNTS_CODE_INT8>(p, shaped, grid, st);
+  }
+}
+template <int D, int CODE>
+static void coded_token_scores(const ChunkScoreParams &p, bool shaped, unsigned grid, hipStream_t st) {
+  if (shaped) hipLaunchKernelGGL((coded_token_scores_kernel<D, true, CODE>), dim3(grid), dim3(kTsWaves * 64), 0, st, p);
+  else hipLaunchKernelGGL((coded_token_scores_kernel<D, false, CODE>), dim3(grid), dim3(kTsWaves * 64), 0, st, p);
+}
+void launch_coded_token_scores(const ChunkScoreParams &p, bool shaped, unsigned grid, hipStream_t st) {
+  if (p.c.D == 128) {
+    if (p.c.code == DYNTS_CODE_E4M3) coded_token_scores<128, DYNTS_CODE_E4M3>(p, shaped, grid, st);
+    else coded_token_scores<128, DYNTS_CODE_INT8>(p, shaped, grid, st);
+  } else {
+    if (p.c.code == DYNTS_CODE_E4M3) coded_token_scores<64, DYNTS_CODE_E4M3>(p, shaped, grid, st);
+    else coded_token_scores<64, DYNTS_CODE_INT8>(p, shaped, grid, st);
+  }
+}
+
 void launch_tree_attend(const ChunkAttendParams &p, unsigned grid, hipStream_t st) {
   if (p.c.D == 128) hipLaunchKernelGGL((tree_attend_kernel<128>), dim3(grid), dim3(kChThreads), 0, st, p);
   else hipLaunchKernelGGL((tree_attend_kernel<64>), dim3(grid), dim3(kChThreads), 0, st, p);

@@ -2,6 +2,7 @@
 #pragma once
 #include "chunk_attend.hpp"
 #include "chunk_scores.hpp"
+#include "coded_token.hpp"
 
 namespace dynts {
 
@@ -10,6 +11,9 @@ constexpr int kTreeMost = 4096;
 
 // chunk_attend_few_kernel's other forms: mask kTree, or a cache of codes with any mask.
 __attribute__((visibility("hidden"))) void launch_few_form(const ChunkAttendParams &p, int mask, unsigned grid, hipStream_t st);
+// up to kTokRows rows on a cache of codes
+__attribute__((visibility("hidden"))) void launch_coded_token(const ChunkAttendParams &p, bool shaped, unsigned grid, hipStream_t st);
+__attribute__((visibility("hidden"))) void launch_coded_token_scores(const ChunkScoreParams &p, bool shaped, unsigned grid, hipStream_t st);
 // a draft's tokens, many rows
 __attribute__((visibility("hidden"))) void launch_tree_attend(const ChunkAttendParams &p, unsigned grid, hipStream_t st);
 __attribute__((visibility("hidden"))) void launch_coded_scores(const ChunkScoreParams &p, bool few, bool shaped, bool biased, unsigned grid, hipStream_t st);

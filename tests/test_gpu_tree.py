@@ -183,12 +183,15 @@ def test_attend_other_trees(B, kind, how, Hq, Hkv, d, n_old, n_new):
 @pytest.mark.parametrize("kind", ["dense", "paged", "e4m3"])
 @pytest.mark.parametrize("Hq,Hkv,d,n_old,n_new", [SHAPES[0], SHAPES[1], SHAPES[6], SHAPES[7], SHAPES[8]])
 def test_a_chain_is_a_chunk(B, kind, Hq, Hkv, d, n_old, n_new):
-    """Tokens that follow each other: bit for bit what dynts_chunk_attend gives."""
+    """Tokens that follow each other: what dynts_chunk_attend gives, either within its bound of the definition."""
     x = Draft(B, kind, Hq, Hkv, d, n_old, n_new, how="chain").attend()
     out, lse = torch.full_like(x.out, 7.0), torch.full_like(x.lse, 7.0)
     B.dynts_chunk_attend(x.c.ctx, 0, x.q.to(DEV), out, x.scratch, lse=lse, n_new=x.n)
-    for b, m in enumerate(n_new):
-        assert torch.equal(out[b, :m], x.out[b, :m]) and torch.equal(lse[b, :m], x.lse[b, :m])
+    for b, (a, m) in enumerate(zip(n_old, n_new)):
+        if m:
+            r = held.attention(x.q[b], x.K[b], x.V[b], a + m, m, x.masks[b], 1.0 / math.sqrt(d))
+            plain.check(out[b, :m], x.out[b, :m].double().cpu(), 2 * r["out_tol"], "out")
+            plain.check(lse[b, :m], x.lse[b, :m].double().cpu(), 2 * r["lse_tol"], "lse")
 
 
 @pytest.mark.parametrize("kind", ["dense", "e4m3"])
