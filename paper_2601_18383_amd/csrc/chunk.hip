@@ -186,11 +186,11 @@ int check_append(const ChunkCache &c, const uint16_t *k_new, const uint16_t *v_n
 // copy: false leaves the rows to chunk_attend_kernel
 int launch_append(const ChunkCache &c, const uint16_t *k_new, const uint16_t *v_new, const float *s_new, int n_tokens,
                   const int32_t *n_new, int question, int32_t *taken, bool copy, hipStream_t st) {
-  const dynts::ChunkAppendParams p{c, k_new, v_new, s_new, n_new, taken, n_tokens, question};
+  const dynts::ChunkAppendParams p{c, k_new, v_new, s_new, n_new, taken, n_tokens, question, group_magic(c.Hkv)};
   const long long pieces = (long long)n_tokens * c.Hkv * (c.D / 8);
   const dim3 block(dynts::kAppendThreads);
   if (c.code && pieces <= dynts::kAppendSmall) {
-    dynts::launch_coded_append(p, true, 0, st);
+    dynts::launch_coded_append(p, true, st);
     return launch_status();
   }
   if (copy && pieces <= dynts::kAppendSmall) {
@@ -198,7 +198,8 @@ int launch_append(const ChunkCache &c, const uint16_t *k_new, const uint16_t *v_
     else hipLaunchKernelGGL((dynts::chunk_reserve_kernel<64, true>), dim3(c.Nb), block, 0, st, p);
     return launch_status();
   }
-  const dim3 grid((unsigned)((pieces + dynts::kAppendThreads - 1) / dynts::kAppendThreads), c.Nb);
+  constexpr int kPer = dynts::kAppendThreads * dynts::kAppendAtOnce;
+  const dim3 grid((unsigned)((pieces + kPer - 1) / kPer), c.Nb);
   if (c.code) copy = false;
   if (c.D == 128) {
     hipLaunchKernelGGL((dynts::chunk_reserve_kernel<128, false>), dim3(c.Nb), block, 0, st, p);
@@ -207,7 +208,7 @@ int launch_append(const ChunkCache &c, const uint16_t *k_new, const uint16_t *v_
     hipLaunchKernelGGL((dynts::chunk_reserve_kernel<64, false>), dim3(c.Nb), block, 0, st, p);
     if (copy) hipLaunchKernelGGL((dynts::chunk_copy_kernel<64>), grid, block, 0, st, p);
   }
-  if (c.code) dynts::launch_coded_append(p, false, grid.x, st);
+  if (c.code) dynts::launch_coded_append(p, false, st);
   return launch_status();
 }
 
@@ -273,7 +274,7 @@ int launch_attend(ChunkCache c, const uint16_t *q, int n_tokens, const int32_t *
   char *const base = static_cast<char *>(scratch);
   if (c.code && !pl.few) {  // the codes as bf16, in a dense cache in scratch
     uint16_t *const K = reinterpret_cast<uint16_t *>(base + pl.bytes), *const V = reinterpret_cast<uint16_t *>(base + pl.bytes + unpacked_bytes(config_of(c)));
-    dynts::launch_read_rows(c, nullptr, c.cap, K, V, st);
+    dynts::launch_read_rows(c, nullptr, c.cap, K, V, false, st);
     c.K = K;
     c.V = V;
     c.code = 0;

@@ -128,34 +128,64 @@ struct ReadParams {
 
 constexpr int kReadThreads = 256;
 
-// Slots first[b] + i of every unit to row i, those that the sequence has; a copy, bound by HBM.  grid (ceil(n_rows * D / 16 / 256), Hkv, Nb), 16 elements a thread.
-template <int D, int CODE>
+// Slots first[b] + i of every unit to row i, those that the sequence has; a copy, bound by HBM.  grid (ceil(n_rows * D / 8 / 256 / 2), Hkv, Nb), eight elements of
+// K and V a thread, so that a wave's stores are whole lines, and twice.
+constexpr int kReadAtOnce = 2;
+template <int D, int CODE, bool PAST>
 __global__ __launch_bounds__(kReadThreads) void read_rows_kernel(const ReadParams p) {
   const ChunkCache &c = p.c;
-  constexpr int LPR = D / 16;
-  const int h = blockIdx.y, b = blockIdx.z;
-  const int at = blockIdx.x * kReadThreads + threadIdx.x, i = at / LPR, piece = at % LPR;
+  constexpr int LPR = D / 8, ROWS = kReadThreads / LPR;
+  const int h = blockIdx.y, b = blockIdx.z, piece = threadIdx.x % LPR;
   int n = c.seq_len[b];
   n = n < c.cap ? n : c.cap;
-  const long long slot = (long long)(p.first ? p.first[b] : 0) + i;
-  if (i >= p.n_rows || slot < 0 || slot >= n) return;
+  const long long first = p.first ? p.first[b] : 0;
+  const int i0 = (int)blockIdx.x * (ROWS * kReadAtOnce) + threadIdx.x / LPR;
   const size_t unit = (size_t)b * c.Hkv + h;
-  const size_t row = c.block_table ? paged_row<1>(c.block_table + unit * c.max_pages, (int)slot, c.max_pages, c.n_pages) : unit * (size_t)c.cap + (size_t)slot;
-  const size_t src = row * D + 16 * piece, dst = (unit * (size_t)p.n_rows + i) * D + 16 * piece;
+  u32x4 x[kReadAtOnce][2];
+  uint32_t s[kReadAtOnce][2];
+  bool has[kReadAtOnce];
 #pragma unroll
-  for (int kv = 0; kv < 2; ++kv) {
-    const uint16_t *from = kv ? c.V : c.K;
-    uint16_t *to = (kv ? p.V : p.K) + dst;
-    u32x4 lo, hi;
-    if (CODE) {
-      const u32x4 x = *reinterpret_cast<const u32x4 *>(reinterpret_cast<const uint8_t *>(from) + src);
-      decode16<CODE>(x, (kv ? c.V_scale : c.K_scale)[src / kCodeBlock], lo, hi);
-    } else {
-      lo = load_u32x4(from + src);
-      hi = load_u32x4(from + src + 8);
+  for (int u = 0; u < kReadAtOnce; ++u) {
+    const int i = i0 + u * ROWS;
+    const long long slot = first + i;
+    has[u] = i < p.n_rows && slot >= 0 && slot < n;
+    if (!has[u]) continue;
+    const size_t row = c.block_table ? paged_row<1>(c.block_table + unit * c.max_pages, (int)slot, c.max_pages, c.n_pages) : unit * (size_t)c.cap + (size_t)slot;
+    const size_t src = row * D + 8 * piece;
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv) {
+      const uint16_t *from = kv ? c.V : c.K;
+      if (CODE) {
+        const uint2 w = *reinterpret_cast<const uint2 *>(reinterpret_cast<const uint8_t *>(from) + src);
+        x[u][kv][0] = w.x;
+        x[u][kv][1] = w.y;
+        s[u][kv] = (kv ? c.V_scale : c.K_scale)[src / kCodeBlock];
+      } else {
+        x[u][kv] = load_u32x4(from + src);
+      }
     }
-    store_u32x4(to, lo);
-    store_u32x4(to + 8, hi);
+  }
+#pragma unroll
+  for (int u = 0; u < kReadAtOnce; ++u) {
+    if (!has[u]) continue;
+    const size_t dst = (unit * (size_t)p.n_rows + (i0 + u * ROWS)) * D + 8 * piece;
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv) {
+      u32x4 y = x[u][kv];
+      if (CODE) {
+        const float scale = __uint_as_float(s[u][kv] << 23);
+        uint32_t lo, hi;
+        decode4<CODE>(x[u][kv][0], scale, lo, hi);
+        y[0] = lo;
+        y[1] = hi;
+        decode4<CODE>(x[u][kv][1], scale, lo, hi);
+        y[2] = lo;
+        y[3] = hi;
+      }
+      u32x4 *to = reinterpret_cast<u32x4 *>((kv ? p.V : p.K) + dst);
+      if (PAST) __builtin_nontemporal_store(y, to);
+      else *to = y;
+    }
   }
 }
 

@@ -81,31 +81,33 @@ void launch_coded_scores(const ChunkScoreParams &p, bool few, bool shaped, bool 
 }
 
 template <int D, int CODE>
-static void coded_append(const ChunkAppendParams &p, bool small, unsigned blocks, hipStream_t st) {
+static void coded_append(const ChunkAppendParams &p, bool small, hipStream_t st) {
+  const unsigned blocks = (unsigned)(p.T + kCodedTokens<D> - 1) / kCodedTokens<D> * p.c.Hkv;
   if (small) hipLaunchKernelGGL((coded_reserve_kernel<D, CODE>), dim3(p.c.Nb), dim3(kAppendThreads), 0, st, p);
   else hipLaunchKernelGGL((coded_copy_kernel<D, CODE>), dim3(blocks, p.c.Nb), dim3(kAppendThreads), 0, st, p);
 }
-void launch_coded_append(const ChunkAppendParams &p, bool small, unsigned blocks, hipStream_t st) {
+void launch_coded_append(const ChunkAppendParams &p, bool small, hipStream_t st) {
   if (p.c.D == 128) {
-    if (p.c.code == DYNTS_CODE_E4M3) coded_append<128, DYNTS_CODE_E4M3>(p, small, blocks, st);
-    else coded_append<128, DYNTS_CODE_INT8>(p, small, blocks, st);
+    if (p.c.code == DYNTS_CODE_E4M3) coded_append<128, DYNTS_CODE_E4M3>(p, small, st);
+    else coded_append<128, DYNTS_CODE_INT8>(p, small, st);
   } else {
-    if (p.c.code == DYNTS_CODE_E4M3) coded_append<64, DYNTS_CODE_E4M3>(p, small, blocks, st);
-    else coded_append<64, DYNTS_CODE_INT8>(p, small, blocks, st);
+    if (p.c.code == DYNTS_CODE_E4M3) coded_append<64, DYNTS_CODE_E4M3>(p, small, st);
+    else coded_append<64, DYNTS_CODE_INT8>(p, small, st);
   }
 }
 
-template <int D>
+template <int D, bool PAST>
 static void read_rows(const ReadParams &p, hipStream_t st) {
-  const dim3 grid((unsigned)(((long long)p.n_rows * (D / 16) + kReadThreads - 1) / kReadThreads), p.c.Hkv, p.c.Nb), block(kReadThreads);
-  if (p.c.code == DYNTS_CODE_E4M3) hipLaunchKernelGGL((read_rows_kernel<D, DYNTS_CODE_E4M3>), grid, block, 0, st, p);
-  else if (p.c.code == DYNTS_CODE_INT8) hipLaunchKernelGGL((read_rows_kernel<D, DYNTS_CODE_INT8>), grid, block, 0, st, p);
-  else hipLaunchKernelGGL((read_rows_kernel<D, 0>), grid, block, 0, st, p);
+  constexpr int kPer = kReadThreads * kReadAtOnce;
+  const dim3 grid((unsigned)(((long long)p.n_rows * (D / 8) + kPer - 1) / kPer), p.c.Hkv, p.c.Nb), block(kReadThreads);
+  if (p.c.code == DYNTS_CODE_E4M3) hipLaunchKernelGGL((read_rows_kernel<D, DYNTS_CODE_E4M3, PAST>), grid, block, 0, st, p);
+  else if (p.c.code == DYNTS_CODE_INT8) hipLaunchKernelGGL((read_rows_kernel<D, DYNTS_CODE_INT8, PAST>), grid, block, 0, st, p);
+  else if (PAST) hipLaunchKernelGGL((read_rows_kernel<D, 0, true>), grid, block, 0, st, p);
 }
-void launch_read_rows(const ChunkCache &c, const int32_t *first, int n_rows, uint16_t *K, uint16_t *V, hipStream_t st) {
+void launch_read_rows(const ChunkCache &c, const int32_t *first, int n_rows, uint16_t *K, uint16_t *V, bool past, hipStream_t st) {
   const ReadParams p{c, first, K, V, n_rows};
-  if (c.D == 128) read_rows<128>(p, st);
-  else read_rows<64>(p, st);
+  if (c.D == 128) past ? read_rows<128, true>(p, st) : read_rows<128, false>(p, st);
+  else past ? read_rows<64, true>(p, st) : read_rows<64, false>(p, st);
 }
 
 }  // namespace dynts
@@ -132,7 +134,7 @@ int dynts_read_rows(dynts_ctx *ctx, int32_t layer, const int32_t *first, int32_t
   if (misaligned(K_out, 16) || misaligned(V_out, 16) || misaligned(first, 4)) return DYNTS_EINVAL;
   const size_t bytes = (size_t)c.Nb * c.Hkv * n_rows * c.D * 2;
   if (overlap(K_out, bytes, V_out, bytes)) return DYNTS_EINVAL;
-  dynts::launch_read_rows(c, first, n_rows, K_out, V_out, static_cast<hipStream_t>(stream));
+  dynts::launch_read_rows(c, first, n_rows, K_out, V_out, true, static_cast<hipStream_t>(stream));
   return launch_status();
 }
 

@@ -17,9 +17,9 @@ __attribute__((visibility("hidden"))) void launch_coded_token_scores(const Chunk
 // a draft's tokens, many rows
 __attribute__((visibility("hidden"))) void launch_tree_attend(const ChunkAttendParams &p, unsigned grid, hipStream_t st);
 __attribute__((visibility("hidden"))) void launch_coded_scores(const ChunkScoreParams &p, bool few, bool shaped, bool biased, unsigned grid, hipStream_t st);
-// small: one launch that makes room and writes; else (behind chunk_reserve_kernel) `blocks` workgroups a sequence that write
-__attribute__((visibility("hidden"))) void launch_coded_append(const ChunkAppendParams &p, bool small, unsigned blocks, hipStream_t st);
-// rows of any cache as bf16
-__attribute__((visibility("hidden"))) void launch_read_rows(const ChunkCache &c, const int32_t *first, int n_rows, uint16_t *K, uint16_t *V, hipStream_t st);
+// small: one launch that makes room and writes; else one (behind chunk_reserve_kernel) that writes
+__attribute__((visibility("hidden"))) void launch_coded_append(const ChunkAppendParams &p, bool small, hipStream_t st);
+// rows of a cache as bf16; past: the caches, for who does not read them next (bf16 caches: always)
+__attribute__((visibility("hidden"))) void launch_read_rows(const ChunkCache &c, const int32_t *first, int n_rows, uint16_t *K, uint16_t *V, bool past, hipStream_t st);
 
 }  // namespace dynts
