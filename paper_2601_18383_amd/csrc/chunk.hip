@@ -31,6 +31,7 @@ int launch_status() { return hipGetLastError() == hipSuccess ? DYNTS_OK : DYNTS_
 struct ChunkPlan {
   bool few;          // chunk_attend_few_kernel
   bool token;        // coded_token_kernel
+  bool groups;       // forms_attend_groups_kernel
   int rows, blocks;  // query rows of a workgroup, row blocks of a unit
   int n_split, Rpad;
   size_t off_lse = 0, off_n = 0, off_ml = 0, off_o = 0, bytes = 0;
@@ -66,9 +67,10 @@ constexpr long long kMostPartials = 65536;
 //     202 / 175
 //   head_dim 64, 8 units: 4500 slots R = 1024 28 / 31 and 35 / 31; 32 units: 500 slots R = 1024 19 / 20 and 23 / 20, R = 2048 38 / 25, 4500 R = 512 45 / 46, R = 1024
 //     82 / 68
-// A draft's shares stop at one workgroup a compute unit while they have less than 1536 slots (us, 128 units of 2480 slots by their number, R = 112 1 / 2 / 4: 59 /
-// 47 / 51; R = 224 1 / 2: 67 / 66).
-ChunkPlan chunk_plan(const dynts_config &c, int n_tokens, int slots, bool far_cap = false, bool codes = false, bool tree = false) {
+// Groups of waves (drafts, chunks on codes): one workgroup a compute unit, and no two shares of many units, which are bound by HBM, before the slots pay for
+// the joint.  us by the number of shares: W = 128, 32 units of 2500 slots 1 / 2: 39.1 / 35.1, 128 units 44.2 / 47.0, 64 units of 4500 71.4 / 55.2; W = 16, 8 units of
+// 16400 8 / 16 / 32: 40.3 / 33.9 / 47.1; W = 64, 64 units of 9000 2 / 4 / 8: 81.7 / 70.1 / 83.6.
+ChunkPlan chunk_plan(const dynts_config &c, int n_tokens, int slots, bool far_cap = false, bool codes = false, bool tree = false, bool shaped = false) {
   ChunkPlan pl;
   const long long R = (long long)n_tokens * (c.n_q_heads / c.n_kv_heads), units = (long long)c.batch * c.n_kv_heads;
   const long long F = units * ((R + dynts::kFewRows - 1) / dynts::kFewRows), W = units * ((R + dynts::kChRows - 1) / dynts::kChRows);
@@ -80,6 +82,7 @@ ChunkPlan chunk_plan(const dynts_config &c, int n_tokens, int slots, bool far_ca
     const double many = 18 + all * c.head_dim * 1.7e-6 + all * R * (c.head_dim == 128 ? 3e-7 : 2e-7);
     pl.few = few < many;
   }
+  pl.groups = !pl.few && W <= 256 && (tree || (codes && !shaped));
   pl.token = codes && !tree && R <= dynts::kTokRows;
   pl.rows = pl.token ? dynts::kTokRows : pl.few ? dynts::kFewRows : dynts::kChRows;
   pl.blocks = (int)((R + pl.rows - 1) / pl.rows);
@@ -95,7 +98,10 @@ ChunkPlan chunk_plan(const dynts_config &c, int n_tokens, int slots, bool far_ca
   } else {
     shares = shares < 32 ? shares : 32;
     shares = shares < 512 / W ? shares : 512 / W;
-    if (tree && W * shares > 256 && slots / shares < 1536) shares = 256 / W;
+    if (pl.groups) {
+      shares = shares < 256 / W ? shares : 256 / W;
+      if (units > 64 && slots < 3500) shares = 1;
+    }
   }
   if (slots < 1536) shares = 1;
   while (shares > 1 && units * pl.Rpad * shares > kMostPartials) --shares;
@@ -116,6 +122,7 @@ ChunkPlan chunk_plan(const dynts_config &c, int n_tokens, int slots, bool far_ca
   return pl;
 }
 
+bool shaped(const dynts_shaping *s) { return s && (s->softcap > 0.f || s->window > 0 || s->slope || s->first || s->last); }
 // a cap that takes the longer form of soft_caps
 bool far_cap(const dynts_shaping *s) { return s && s->softcap * kLog2E > dynts::kCapNear; }
 
@@ -128,7 +135,7 @@ dynts_config config_of(const ChunkCache &c) {
 ChunkPlan chunk_plan(const ChunkCache &c, int n_tokens, const dynts_shaping *shaping, bool tree) {
   // (slots of a window: no more than its positions, those of the chunk's other tokens beside them)
   const long long seen = shaping && shaping->window > 0 ? (long long)shaping->window + n_tokens : c.cap;
-  return chunk_plan(config_of(c), n_tokens, (int)(seen < c.cap ? seen : c.cap), far_cap(shaping), c.code != 0, tree);
+  return chunk_plan(config_of(c), n_tokens, (int)(seen < c.cap ? seen : c.cap), far_cap(shaping), c.code != 0, tree, shaped(shaping));
 }
 
 // Room behind a chunk's scratch where the layer's codes lie as bf16, for the kernel of many rows.
@@ -153,7 +160,6 @@ int check_shaping(const dynts_shaping *s, float scale) {
 
 uint32_t group_magic(int G) { return G == 1 ? 0u : (uint32_t)(((1ull << 32) + G - 1) / G); }
 
-bool shaped(const dynts_shaping *s) { return s && (s->softcap > 0.f || s->window > 0 || s->slope || s->first || s->last); }
 bool shaped(const dynts::ChunkShape &s) { return s.cap > 0.f || s.window > 0 || s.slope || s.first || s.last; }
 dynts::ChunkShape chunk_shape(const dynts_shaping *s, float scale) {
   dynts::ChunkShape out{};
@@ -219,7 +225,7 @@ unsigned chunk_grid(const ChunkCache &c, long long blocks, int threads) {
   return wgs >= (1LL << 32) / threads ? 0u : (unsigned)wgs;
 }
 unsigned attend_grid(const ChunkCache &c, const ChunkPlan &pl) {
-  return chunk_grid(c, (long long)pl.blocks * pl.n_split, pl.token ? dynts::kTokWaves * 64 : pl.few ? dynts::kFewThreads : dynts::kChThreads);
+  return chunk_grid(c, (long long)pl.blocks * pl.n_split, pl.token ? dynts::kTokWaves * 64 : pl.few ? dynts::kFewThreads : pl.groups ? dynts::kGroups * dynts::kChThreads : dynts::kChThreads);
 }
 // Which kernel of chunk_scores.hpp.  C: chunks of 32 rows of a unit, W: workgroups of 64 slots, one a compute unit.  Few slots: 7 + C / 4 us a round of 256 of
 // them; many: 4 + 0.8 C us while its W / 4 workgroups have a compute unit each.  us, few / many:
@@ -246,6 +252,7 @@ template <int D, bool SHAPED>
 void launch_attend_d(const dynts::ChunkAttendParams &p, const ChunkPlan &pl, unsigned grid, hipStream_t st) {
   if (pl.token) dynts::launch_coded_token(p, SHAPED, grid, st);
   else if (pl.few && (p.seen || p.c.code)) dynts::launch_few_form(p, p.seen ? dynts::kTree : SHAPED ? dynts::kShaped : dynts::kPlain, grid, st);
+  else if (pl.groups) dynts::launch_attend_groups(p, p.seen ? dynts::kTree : dynts::kPlain, grid, st);
   else if (p.seen) dynts::launch_tree_attend(p, grid, st);
   else if (pl.few) hipLaunchKernelGGL((dynts::chunk_attend_few_kernel<D, SHAPED>), dim3(grid), dim3(dynts::kFewThreads), 0, st, p);
   else if (SHAPED && p.shape.slope) hipLaunchKernelGGL((dynts::chunk_attend_kernel<D, SHAPED, SHAPED, false>), dim3(grid), dim3(dynts::kChThreads), 0, st, p);

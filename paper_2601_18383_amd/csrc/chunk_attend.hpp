@@ -281,15 +281,18 @@ __device__ __forceinline__ int chunk_lds_v(int row, int piece) {
 // form): the chunk's own rows are not in the cache yet; they are read where the caller has them, and every workgroup copies those of its tokens at its
 // end.  (Copied by a launch of their own before, 512 tokens of 64 sequences, 32 heads on 8: 244 us a step instead of 236, heads of 64 134 instead of
 // 123, 28 on 4 of 32 sequences, 600 tokens, 122 instead of 123.)
-template <int D, int MASK, bool BIASED, bool APPEND>
+// GROUPS: of four waves, that share out the tiles of the same rows and are joined through LDS (see forms_attend_groups_kernel; not with APPEND or SHAPED).
+template <int D, int MASK, bool BIASED, bool APPEND, int GROUPS = 1>
 __device__ __forceinline__ void chunk_attend_rows(const ChunkAttendParams &p) {
   constexpr bool SHAPED = MASK == kShaped, TREE = MASK == kTree;
   using Lds = ChunkLds<D>;
   const ChunkCache &c = p.c;
   // Three tiles' places: one is worked on, one is on its way, one is being asked for.
-  __shared__ __attribute__((aligned(1024))) char sm[Lds::kPlaces * Lds::kPlace];
+  __shared__ __attribute__((aligned(1024))) char sm[GROUPS * Lds::kPlaces * Lds::kPlace];
   __shared__ int sm_range[2 * kChWaves];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int tid = threadIdx.x, lane = tid & 63, whole = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wave = GROUPS > 1 ? whole % kChWaves : whole, group = GROUPS > 1 ? whole / kChWaves : 0;
+  constexpr int kRound = GROUPS * kChTile;  // slots from a wave's tile to its next one
   const int col = lane & 31, hf = lane >> 5, r16 = lane & 15;
   int unit, blk;
   const int n_blk = (p.T * c.G + kChRows - 1) / kChRows;
@@ -375,7 +378,7 @@ __device__ __forceinline__ void chunk_attend_rows(const ChunkAttendParams &p) {
   // Staging, past the registers: a wave brings kInstr parts of 1 KB of either operand.  A lane's piece of a part is the one that belongs at byte
   // 16 * lane of it; its place in the row is the same for all of a lane's parts.  Rows past the cache's end repeat the last one.
   constexpr int PPR = D / 8, kInstr = Lds::kTileBytes / 1024 / kChWaves, kRowsPart = 1024 / (2 * D);
-  const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)sm;
+  const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)sm + group * (Lds::kPlaces * Lds::kPlace);
   const int my_row = wave * kRowsPart + lane / PPR;
   const uint32_t k_off = chunk_lds<D>(my_row, lane % PPR), v_off = chunk_lds_v<D>(my_row, lane % PPR);
   constexpr int kNext = kRowsPart * kChWaves;  // rows from a lane's part to its next one
@@ -396,7 +399,7 @@ __device__ __forceinline__ void chunk_attend_rows(const ChunkAttendParams &p) {
     }
   };
   // (the page of the next tile to bring: looked up a tile ahead)
-  int page = c.block_table ? chunk_page(c, unit, t0) : 0;
+  int page = c.block_table ? chunk_page(c, unit, t0 + group * kChTile) : 0;
   auto bring = [&](int t, uint32_t place) {
     if (t >= t1) return;
     const int this_page = page;
@@ -408,7 +411,7 @@ __device__ __forceinline__ void chunk_attend_rows(const ChunkAttendParams &p) {
       rows = cached < rows ? cached : rows;
     }
     const size_t at = chunk_tile<D>(c, unit, t, this_page);
-    if (c.block_table) page = chunk_page(c, unit, t + kChTile);
+    if (c.block_table) page = chunk_page(c, unit, t + kRound);
     const RowBuffer kb = row_buffer<D>(c.K + at, rows), vb = row_buffer<D>(c.V + at, rows);
 #pragma unroll
     for (int i = 0; i < kInstr; ++i) {
@@ -564,13 +567,14 @@ __device__ __forceinline__ void chunk_attend_rows(const ChunkAttendParams &p) {
   constexpr int kWait = 0x0070;  // s_waitcnt of lgkmcnt(0) and vmcnt(0)
   auto tile = [&](int t, auto PLACE, auto FREE, auto FIRST) {
     constexpr uint32_t place = decltype(PLACE)::value * Lds::kPlace, free = decltype(FREE)::value * Lds::kPlace;
-    if (t + kChTile >= t1) __builtin_amdgcn_s_waitcnt(kWait);
+    if (t + kRound >= t1) __builtin_amdgcn_s_waitcnt(kWait);
     else if (SHAPED && wave == 0) __builtin_amdgcn_s_waitcnt(kWait + 2 * kInstr + 1);
     else __builtin_amdgcn_s_waitcnt(kWait + 2 * kInstr);
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    bring(t + 2 * kChTile, lds + free);
+    if (GROUPS > 1 && t >= t1) return;  // (this group's last round)
+    bring(t + 2 * kRound, lds + free);
     f32x16 s;
     products(s, place);
     const int *tp = reinterpret_cast<const int *>(sm + place + 2 * Lds::kTileBytes);
@@ -579,19 +583,21 @@ __device__ __forceinline__ void chunk_attend_rows(const ChunkAttendParams &p) {
     weigh(s, pf, FIRST);
     add_values(pf, place);
   };
-  bring(t0, lds);
-  bring(t0 + kChTile, lds + Lds::kPlace);
+  const int own0 = t0 + group * kChTile, more = own0 - t0;  // this group's first tile
+  bring(own0, lds);
+  bring(own0 + kRound, lds + Lds::kPlace);
   // (the queries are waited for here: in the loop, every third tile would wait for all loads)
 #pragma unroll
   for (int ks = 0; ks < D / 16; ++ks) asm volatile("" : "+v"(qf[ks]));
   constexpr std::integral_constant<int, 0> kA{};
   constexpr std::integral_constant<int, 1> kB{};
   constexpr std::integral_constant<int, 2> kC{};
-  if (t0 < t1) tile(t0, kA, kC, std::true_type{});
-  for (int t = t0 + kChTile; t < t1; t += 3 * kChTile) {
-    tile(t, kB, kA, std::false_type{});
-    if (t + kChTile < t1) tile(t + kChTile, kC, kB, std::false_type{});
-    if (t + 2 * kChTile < t1) tile(t + 2 * kChTile, kA, kC, std::false_type{});
+  // (rounds are counted by the first group's tiles: every wave meets every barrier)
+  if (t0 < t1) tile(own0, kA, kC, std::true_type{});
+  for (int t = t0 + kRound; t < t1; t += 3 * kRound) {
+    tile(t + more, kB, kA, std::false_type{});
+    if (t + kRound < t1) tile(t + kRound + more, kC, kB, std::false_type{});
+    if (t + 2 * kRound < t1) tile(t + 2 * kRound + more, kA, kC, std::false_type{});
   }
 
   if (APPEND && split == 0) {  // the tokens whose first row is one of this workgroup's
@@ -601,7 +607,38 @@ __device__ __forceinline__ void chunk_attend_rows(const ChunkAttendParams &p) {
 
   // sums of the two halves' keys; outputs row by row through LDS
   __syncthreads();
-  const float sum = l + __shfl_xor(l, 32);
+  float sum = l + __shfl_xor(l, 32);
+  if (GROUPS > 1) {  // the other groups', one after the other and lane by lane, through what the first does not use for its outputs
+    __shared__ float sm_stats[2][kChWaves][64];
+    static_assert(GROUPS == 1 || (kChWaves * 32 * 2 * D + kChWaves * 64 * 2 * D <= GROUPS * Lds::kPlaces * Lds::kPlace && !APPEND && !SHAPED), "room for a group's outputs");
+    f32x4 *const theirs = reinterpret_cast<f32x4 *>(sm + kChWaves * 32 * 2 * D + wave * (64 * 2 * D)) + lane;
+#pragma unroll
+    for (int g = 1; g < GROUPS; ++g) {
+      if (g > 1) __syncthreads();
+      if (group == g) {
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+          for (int e = 0; e < 16; e += 4) theirs[64 * (4 * dt + e / 4)] = f32x4{acc[dt][e], acc[dt][e + 1], acc[dt][e + 2], acc[dt][e + 3]};
+        sm_stats[0][wave][lane] = nm;
+        sm_stats[1][wave][lane] = sum;
+      }
+      __syncthreads();
+      if (group > 0) continue;
+      const float nm2 = sm_stats[0][wave][lane], next = fminf(nm, nm2), f = fast_exp2(next - nm), f2 = fast_exp2(next - nm2);
+      nm = next;
+      sum = sum * f + sm_stats[1][wave][lane] * f2;
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+          const f32x4 x = theirs[64 * (4 * dt + e / 4)];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) acc[dt][e + k] = acc[dt][e + k] * f + x[k] * f2;
+        }
+    }
+    if (group > 0) return;
+  }
   if (shares > 1) {
     if (row0 + col >= R) return;
     const size_t prow = ((size_t)unit * p.n_split + split) * p.Rpad + row0 + col;
@@ -650,6 +687,14 @@ __global__ __launch_bounds__(kChThreads, D == 128 ? 3 : 4) void chunk_attend_ker
 template <int D>
 __global__ __launch_bounds__(kChThreads, D == 128 ? 3 : 4) void tree_attend_kernel(const ChunkAttendParams p) {
   chunk_attend_rows<D, kTree, false, false>(p);
+}
+// Drafts, and chunks on unpacked codes, of few row blocks: as many waves a compute unit as three workgroups have, on the same rows, which saves partial outputs
+// in memory and their merge (us, three workgroups / three groups, with the better number of shares each: 32 tokens of 32 sequences, 28 heads on 4, on 2464 slots 65 / 54, of
+// 8 sequences 64 tokens 37 / 35 and on 4500 slots, 32 on 8, 58 / 55, 64 tokens of one on 16384 37 / 34; two groups 56 in place of 54).
+constexpr int kGroups = 3;
+template <int D, int MASK>
+__global__ __launch_bounds__(kGroups * kChThreads, kGroups) void forms_attend_groups_kernel(const ChunkAttendParams p) {
+  chunk_attend_rows<D, MASK, false, false, kGroups>(p);
 }
 
 // ---- few rows: 32 of them a workgroup, its eight waves share out the keys --------------------------------------------------

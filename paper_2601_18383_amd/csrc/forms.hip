@@ -58,6 +58,15 @@ void launch_tree_attend(const ChunkAttendParams &p, unsigned grid, hipStream_t s
   if (p.c.D == 128) hipLaunchKernelGGL((tree_attend_kernel<128>), dim3(grid), dim3(kChThreads), 0, st, p);
   else hipLaunchKernelGGL((tree_attend_kernel<64>), dim3(grid), dim3(kChThreads), 0, st, p);
 }
+template <int D>
+static void attend_groups(const ChunkAttendParams &p, int mask, unsigned grid, hipStream_t st) {
+  if (mask == kTree) hipLaunchKernelGGL((forms_attend_groups_kernel<D, kTree>), dim3(grid), dim3(kGroups * kChThreads), 0, st, p);
+  else hipLaunchKernelGGL((forms_attend_groups_kernel<D, kPlain>), dim3(grid), dim3(kGroups * kChThreads), 0, st, p);
+}
+void launch_attend_groups(const ChunkAttendParams &p, int mask, unsigned grid, hipStream_t st) {
+  if (p.c.D == 128) attend_groups<128>(p, mask, grid, st);
+  else attend_groups<64>(p, mask, grid, st);
+}
 
 template <int D, int CODE, bool SHAPED, bool BIASED>
 static void coded_scores_form(const ChunkScoreParams &p, bool few, unsigned grid, hipStream_t st) {
