@@ -528,30 +528,57 @@ def _on_device(owner, *tensors):
         raise ValueError("the cache's arrays or the tables are not on the current GPU (%d, not %d)" % (dev, bound))
 
 
-def _chunk_sizes(ctx, q, n_new, shaping, lse, *others):
-    """n_new, shaping and lse fit a chunk of queries q [Nb][T][Hq][d], and all lie on the current GPU, `others` too."""
+def _here(owner, t):
+    """The current GPU, which a call's first tensor lies on, and what is bound to the context."""
+    dev = t.get_device()
+    if dev < 0 or dev != _device() or getattr(owner, "gpu", None) not in (None, dev):
+        _on_device(owner, t)
+    return dev
+
+
+def _at(t, dtype, dev):
+    """_ptr of a tensor that has to lie on GPU `dev`, or of None."""
+    if t is None:
+        return None
+    if t.get_device() != dev:
+        _on_device(None, t)
+    assert t.is_contiguous(), "tensors crossing the C ABI must be contiguous"
+    assert t.dtype is dtype, "expected %s, got %s" % (dtype, t.dtype)
+    return t.data_ptr()
+
+
+_BF16, _F32, _I32 = torch.bfloat16, torch.float32, torch.int32
+
+
+def _chunk_sizes(ctx, q, n_new, shaping, lse):
+    """n_new, shaping and lse fit a chunk of queries q [Nb][T][Hq][d], which lies on the current GPU; shaping's tensors too.
+    -> the chunk's tokens, that GPU"""
     Nb, T, Hq, d = q.shape
     dims = getattr(ctx, "dims", None)
-    assert dims is None or (Nb, Hq, d) == (dims[0], dims[1], dims[3]), "the context's batch, query heads and head_dim"
+    assert dims is None or (Nb == dims[0] and Hq == dims[1] and d == dims[3]), "the context's batch, query heads and head_dim"
     assert n_new is None or n_new.numel() == Nb, "n_new holds one number a sequence"
     assert lse is None or lse.numel() == Nb * T * Hq, "lse holds one number a token and query head"
-    if shaping is None:
-        _on_device(ctx, q, n_new, lse, *others)
-    else:
+    if shaping is not None:
         assert shaping.heads is None or shaping.heads == Hq, "slope holds one number a query head"
         assert not shaping.tokens or shaping.tokens == {Nb * T}, "first and last hold one position a token"
-        _on_device(ctx, q, n_new, lse, *others, *shaping.t)
-    return T
+        _on_device(ctx, q, *shaping.t)
+    return T, _here(ctx, q)
 
 
 def _chunk_rows(ctx, k_new, v_new, s_new):
     """k_new, v_new [Nb][T][Hkv][d] and s_new [Nb][T][Hkv] are of one chunk."""
     Nb, T, Hkv, d = k_new.shape
     dims = getattr(ctx, "dims", None)
-    assert dims is None or (Nb, Hkv, d) == (dims[0], dims[2], dims[3]), "the context's batch, KV heads and head_dim"
+    assert dims is None or (Nb == dims[0] and Hkv == dims[2] and d == dims[3]), "the context's batch, KV heads and head_dim"
     assert v_new.numel() == Nb * T * Hkv * d, "k_new and v_new are of one shape"
     assert s_new is None or s_new.numel() == Nb * T * Hkv, "s_new holds one number a token and KV head"
     return Nb, T
+
+
+def _scratch(t, dev):
+    if t.get_device() != dev:
+        _on_device(None, t)
+    return t.data_ptr(), t.numel() * t.element_size()
 
 
 def dynts_chunk_append(ctx, layer, k_new, v_new, scratch, n_new=None, s_new=None, question=False, stream=None):
@@ -559,43 +586,37 @@ def dynts_chunk_append(ctx, layer, k_new, v_new, scratch, n_new=None, s_new=None
     dynts_chunk_scratch_bytes bytes."""
     Nb, T = _chunk_rows(ctx, k_new, v_new, s_new)
     assert n_new is None or n_new.numel() == Nb, "n_new holds one number a sequence"
-    _on_device(ctx, k_new, v_new, s_new, n_new, scratch)
-    _check(lib.dynts_chunk_append(ctx, layer, _ptr(k_new, torch.bfloat16), _ptr(v_new, torch.bfloat16),
-                                  _ptr(s_new, torch.float32), T, _ptr(n_new, torch.int32),
-                                  1 if question else 0, scratch.data_ptr(), scratch.numel() * scratch.element_size(),
-                                  _stream(stream)), "dynts_chunk_append")
+    dev = _here(ctx, k_new)
+    _check(lib.dynts_chunk_append(ctx, layer, _at(k_new, _BF16, dev), _at(v_new, _BF16, dev), _at(s_new, _F32, dev), T,
+                                  _at(n_new, _I32, dev), 1 if question else 0, *_scratch(scratch, dev), _stream(stream)),
+           "dynts_chunk_append")
 
 
 def dynts_chunk_attend(ctx, layer, q, out, scratch, lse=None, n_new=None, shaping=None, stream=None):
     """q, out bf16 [Nb][T][Hq][d], lse fp32 [Nb][T][Hq] or None, shaping: Shaping or None."""
-    T = _chunk_sizes(ctx, q, n_new, shaping, lse, out, scratch)
+    T, dev = _chunk_sizes(ctx, q, n_new, shaping, lse)
     assert out.numel() == q.numel(), "out has the shape of q"
-    _check(lib.dynts_chunk_attend(ctx, layer, _ptr(q, torch.bfloat16), T, _ptr(n_new, torch.int32),
-                                  _shaping(shaping), _ptr(out, torch.bfloat16), _ptr(lse, torch.float32),
-                                  scratch.data_ptr(), scratch.numel() * scratch.element_size(), _stream(stream)),
-           "dynts_chunk_attend")
+    _check(lib.dynts_chunk_attend(ctx, layer, _at(q, _BF16, dev), T, _at(n_new, _I32, dev), _shaping(shaping), _at(out, _BF16, dev),
+                                  _at(lse, _F32, dev), *_scratch(scratch, dev), _stream(stream)), "dynts_chunk_attend")
 
 
 def dynts_chunk_scores(ctx, layer, q, lse, dst=None, accumulate=True, n_new=None, shaping=None, stream=None):
     """q and lse as in dynts_chunk_attend; dst fp32 [Nb][Hkv][cap] or None (= the layer's S)."""
     dims = getattr(ctx, "dims", None)
     assert dst is None or dims is None or dst.numel() == dims[0] * dims[2] * dims[4], "dst holds one number a slot"
-    T = _chunk_sizes(ctx, q, n_new, shaping, lse, dst)
-    _check(lib.dynts_chunk_scores(ctx, layer, _ptr(q, torch.bfloat16), T, _ptr(n_new, torch.int32),
-                                  _shaping(shaping), _ptr(lse, torch.float32), _ptr(dst, torch.float32),
-                                  1 if accumulate else 0, _stream(stream)), "dynts_chunk_scores")
+    T, dev = _chunk_sizes(ctx, q, n_new, shaping, lse)
+    _check(lib.dynts_chunk_scores(ctx, layer, _at(q, _BF16, dev), T, _at(n_new, _I32, dev), _shaping(shaping), _at(lse, _F32, dev),
+                                  _at(dst, _F32, dev), 1 if accumulate else 0, _stream(stream)), "dynts_chunk_scores")
 
 
 def dynts_chunk_step(ctx, layer, q, k_new, v_new, out, scratch, lse=None, n_new=None, s_new=None, question=False,
                      shaping=None, stream=None):
     """dynts_chunk_append, dynts_chunk_attend and dynts_chunk_scores into S in one call; arguments as there."""
-    T = _chunk_sizes(ctx, q, n_new, shaping, lse, k_new, v_new, s_new, out, scratch)
+    T, dev = _chunk_sizes(ctx, q, n_new, shaping, lse)
     assert _chunk_rows(ctx, k_new, v_new, s_new) == (q.shape[0], T) and out.numel() == q.numel(), "q, k_new, v_new and out are of one chunk"
-    _check(lib.dynts_chunk_step(ctx, layer, _ptr(q, torch.bfloat16), _ptr(k_new, torch.bfloat16),
-                                _ptr(v_new, torch.bfloat16), _ptr(s_new, torch.float32), T,
-                                _ptr(n_new, torch.int32), 1 if question else 0, _shaping(shaping),
-                                _ptr(out, torch.bfloat16), _ptr(lse, torch.float32), scratch.data_ptr(),
-                                scratch.numel() * scratch.element_size(), _stream(stream)), "dynts_chunk_step")
+    _check(lib.dynts_chunk_step(ctx, layer, _at(q, _BF16, dev), _at(k_new, _BF16, dev), _at(v_new, _BF16, dev), _at(s_new, _F32, dev), T,
+                                _at(n_new, _I32, dev), 1 if question else 0, _shaping(shaping), _at(out, _BF16, dev), _at(lse, _F32, dev),
+                                *_scratch(scratch, dev), _stream(stream)), "dynts_chunk_step")
 
 
 class Rotary:
@@ -648,11 +669,11 @@ def dynts_read_rows(ctx, layer, K_out, V_out, first=None, stream=None):
     """K_out, V_out bf16 [Nb][Hkv][n_rows][d]; first int32 [Nb] or None."""
     Nb, Hkv, n_rows, d = K_out.shape
     dims = getattr(ctx, "dims", None)
-    assert dims is None or (Nb, Hkv, d) == (dims[0], dims[2], dims[3]), "the context's batch, KV heads and head_dim"
-    assert V_out.numel() == K_out.numel() and (first is None or first.numel() == Nb), "V_out as K_out, first one number a sequence"
-    _on_device(ctx, K_out, V_out, first)
-    _check(lib.dynts_read_rows(ctx, layer, _ptr(first, torch.int32), n_rows, _ptr(K_out, torch.bfloat16), _ptr(V_out, torch.bfloat16),
-                               _stream(stream)), "dynts_read_rows")
+    assert dims is None or (Nb == dims[0] and Hkv == dims[2] and d == dims[3]), "the context's batch, KV heads and head_dim"
+    assert V_out.numel() == Nb * Hkv * n_rows * d and (first is None or first.numel() == Nb), "V_out as K_out, first one number a sequence"
+    dev = _here(ctx, K_out)
+    _check(lib.dynts_read_rows(ctx, layer, _at(first, _I32, dev), n_rows, _at(K_out, _BF16, dev), _at(V_out, _BF16, dev), _stream(stream)),
+           "dynts_read_rows")
 
 
 def tree_words(n_tokens):
@@ -663,56 +684,52 @@ def tree_words(n_tokens):
 def dynts_tree_build(parents, seen, depth=None, n_new=None, stream=None):
     """parents, depth int32 [Nb][T]; seen int32 [Nb][T][tree_words(T)]; n_new int32 [Nb]."""
     Nb, T = parents.shape
-    assert seen.numel() == Nb * T * tree_words(T), "seen holds tree_words(T) words a token"
+    assert seen.numel() == Nb * T * ((T + 31) // 32), "seen holds tree_words(T) words a token"
     assert depth is None or depth.numel() == Nb * T, "depth holds one number a token"
     assert n_new is None or n_new.numel() == Nb, "n_new holds one number a sequence"
-    _on_device(None, parents, seen, depth, n_new)
-    _check(lib.dynts_tree_build(_ptr(parents, torch.int32), _ptr(n_new, torch.int32), Nb, T, _ptr(seen, torch.int32), _ptr(depth, torch.int32),
+    dev = _here(None, parents)
+    _check(lib.dynts_tree_build(_at(parents, _I32, dev), _at(n_new, _I32, dev), Nb, T, _at(seen, _I32, dev), _at(depth, _I32, dev),
                                 _stream(stream)), "dynts_tree_build")
-
-
-def _draft(q, seen):
-    Nb, T = q.shape[:2]
-    assert seen.numel() == Nb * T * tree_words(T), "seen holds tree_words(T) words a token"
 
 
 def dynts_tree_attend(ctx, layer, q, seen, out, scratch, lse=None, n_new=None, stream=None):
     """q, out bf16 [Nb][T][Hq][d], lse fp32 [Nb][T][Hq] or None, seen int32 [Nb][T][tree_words(T)]."""
-    T = _chunk_sizes(ctx, q, n_new, None, lse, seen, out, scratch)
-    _draft(q, seen)
+    T, dev = _chunk_sizes(ctx, q, n_new, None, lse)
+    assert seen.numel() == q.shape[0] * T * ((T + 31) // 32), "seen holds tree_words(T) words a token"
     assert out.numel() == q.numel(), "out has the shape of q"
-    _check(lib.dynts_tree_attend(ctx, layer, _ptr(q, torch.bfloat16), T, _ptr(n_new, torch.int32), _ptr(seen, torch.int32),
-                                 _ptr(out, torch.bfloat16), _ptr(lse, torch.float32), scratch.data_ptr(),
-                                 scratch.numel() * scratch.element_size(), _stream(stream)), "dynts_tree_attend")
+    _check(lib.dynts_tree_attend(ctx, layer, _at(q, _BF16, dev), T, _at(n_new, _I32, dev), _at(seen, _I32, dev), _at(out, _BF16, dev),
+                                 _at(lse, _F32, dev), *_scratch(scratch, dev), _stream(stream)), "dynts_tree_attend")
 
 
 def dynts_tree_step(ctx, layer, q, k_new, v_new, seen, n_taken, out, scratch, lse=None, n_new=None, s_new=None, stream=None):
     """k_new, v_new bf16 [Nb][T][Hkv][d], s_new fp32 [Nb][T][Hkv], n_taken int32 [Nb]; the rest as in dynts_tree_attend."""
-    T = _chunk_sizes(ctx, q, n_new, None, lse, k_new, v_new, s_new, seen, n_taken, out, scratch)
-    assert _chunk_rows(ctx, k_new, v_new, s_new) == (q.shape[0], T) and out.numel() == q.numel(), "q, k_new, v_new and out are of one draft"
-    _draft(q, seen)
-    assert n_taken.numel() == q.shape[0], "n_taken holds one number a sequence"
-    _check(lib.dynts_tree_step(ctx, layer, _ptr(q, torch.bfloat16), _ptr(k_new, torch.bfloat16), _ptr(v_new, torch.bfloat16),
-                               _ptr(s_new, torch.float32), T, _ptr(n_new, torch.int32), _ptr(seen, torch.int32), _ptr(n_taken, torch.int32),
-                               _ptr(out, torch.bfloat16), _ptr(lse, torch.float32), scratch.data_ptr(),
-                               scratch.numel() * scratch.element_size(), _stream(stream)), "dynts_tree_step")
+    T, dev = _chunk_sizes(ctx, q, n_new, None, lse)
+    Nb = q.shape[0]
+    assert _chunk_rows(ctx, k_new, v_new, s_new) == (Nb, T) and out.numel() == q.numel(), "q, k_new, v_new and out are of one draft"
+    assert seen.numel() == Nb * T * ((T + 31) // 32), "seen holds tree_words(T) words a token"
+    assert n_taken.numel() == Nb, "n_taken holds one number a sequence"
+    _check(lib.dynts_tree_step(ctx, layer, _at(q, _BF16, dev), _at(k_new, _BF16, dev), _at(v_new, _BF16, dev), _at(s_new, _F32, dev), T,
+                               _at(n_new, _I32, dev), _at(seen, _I32, dev), _at(n_taken, _I32, dev), _at(out, _BF16, dev),
+                               _at(lse, _F32, dev), *_scratch(scratch, dev), _stream(stream)), "dynts_tree_step")
 
 
 def dynts_tree_keep(ctx, layer, seen, leaf, n_taken, n_kept, q=None, lse=None, q_kept=None, lse_kept=None, stream=None):
     """seen int32 [Nb][T][tree_words(T)]; leaf, n_taken (or None), n_kept int32 [Nb]; q, q_kept bf16 [Nb][T][Hq][d], lse, lse_kept fp32 [Nb][T][Hq]."""
-    Nb, T = seen.shape[:2]
+    Nb, T, W = seen.shape
     dims = getattr(ctx, "dims", None)
     assert dims is None or Nb == dims[0], "the context's batch"
-    assert seen.numel() == Nb * T * tree_words(T), "seen holds tree_words(T) words a token"
-    assert all(t is None or t.numel() == Nb for t in (leaf, n_taken, n_kept)), "leaf, n_taken and n_kept hold one number a sequence"
-    assert q_kept is None or (q is not None and q_kept.numel() == q.numel()), "q_kept has the shape of q"
-    assert lse_kept is None or (lse is not None and lse_kept.numel() == lse.numel()), "lse_kept has the shape of lse"
-    assert dims is None or q_kept is None or q.numel() == Nb * T * dims[1] * dims[3], "q is of the draft"
-    assert dims is None or lse_kept is None or lse.numel() == Nb * T * dims[1], "lse is of the draft"
-    _on_device(ctx, seen, leaf, n_taken, n_kept, q, lse, q_kept, lse_kept)
-    _check(lib.dynts_tree_keep(ctx, layer, T, _ptr(n_taken, torch.int32), _ptr(seen, torch.int32), _ptr(leaf, torch.int32),
-                               _ptr(q, torch.bfloat16), _ptr(lse, torch.float32), _ptr(q_kept, torch.bfloat16), _ptr(lse_kept, torch.float32),
-                               _ptr(n_kept, torch.int32), _stream(stream)), "dynts_tree_keep")
+    assert W == (T + 31) // 32, "seen holds tree_words(T) words a token"
+    assert leaf.numel() == Nb and n_kept.numel() == Nb and (n_taken is None or n_taken.numel() == Nb), "leaf, n_taken and n_kept hold one number a sequence"
+    if q_kept is not None:
+        size = q.numel()
+        assert q_kept.numel() == size and (dims is None or size == Nb * T * dims[1] * dims[3]), "q and q_kept are of the draft"
+    if lse_kept is not None:
+        size = lse.numel()
+        assert lse_kept.numel() == size and (dims is None or size == Nb * T * dims[1]), "lse and lse_kept are of the draft"
+    dev = _here(ctx, seen)
+    _check(lib.dynts_tree_keep(ctx, layer, T, _at(n_taken, _I32, dev), _at(seen, _I32, dev), _at(leaf, _I32, dev), _at(q, _BF16, dev),
+                               _at(lse, _F32, dev), _at(q_kept, _BF16, dev), _at(lse_kept, _F32, dev), _at(n_kept, _I32, dev),
+                               _stream(stream)), "dynts_tree_keep")
 
 
 class CodedCache:
