@@ -550,18 +550,25 @@ def run_score_block(args, wl):
 def run_chunk(args, wl):
     """A chunk of T new tokens of every sequence on a generator-made steady-state cache of layer 0: rotary positions of its
     queries and keys, then append, attention and score accumulation.  A step is one such chunk; lengths are set back in
-    between."""
+    between.  --codes: on a cache of 8-bit codes.  --draft: the T tokens are drafted ones that branch; a step finds out who sees whom,
+    appends them, attends, keeps the path to the last token and accumulates its scores."""
     import torch
     from paper_2601_18383_amd import binding as B, synth
 
     dev = torch.device("cuda:0")
     gen = synth.Synth(wl, dev)
-    T, n0, Nb, d = args.chunk, wl.steady_len + wl.evict_every // 2, wl.batch, wl.head_dim
-    cache = B.Cache(1, Nb, wl.n_q_heads, wl.n_kv_heads, d, max(n0 + T, wl.capacity), wl.budget, wl.window, wl.evict_every,
-                    device=dev)
+    T, n0, Nb, d = args.draft or args.chunk, wl.steady_len + wl.evict_every // 2, wl.batch, wl.head_dim
+    shape = (1, Nb, wl.n_q_heads, wl.n_kv_heads, d, max(n0 + T, wl.capacity), wl.budget, wl.window, wl.evict_every)
     st = gen.steady_state(0, n0)
-    cache.K[0, :, :, :n0] = st["K"]
-    cache.V[0, :, :, :n0] = st["V"]
+    if args.codes:
+        cache = B.CodedCache(*shape, code=B.DYNTS_CODE_E4M3 if args.codes == "e4m3" else B.DYNTS_CODE_INT8, device=dev)
+        scratch = torch.empty(B.dynts_codes_scratch_bytes(cache.cfg, max(n0, T)), dtype=torch.uint8, device=dev)
+        B.dynts_chunk_append(cache.ctx, 0, *(st[x].permute(0, 2, 1, 3).contiguous() for x in "KV"), scratch)
+    else:
+        cache = B.Cache(*shape, device=dev)
+        scratch = torch.empty(B.dynts_chunk_scratch_bytes(cache.cfg, T), dtype=torch.uint8, device=dev)
+        cache.K[0, :, :, :n0] = st["K"]
+        cache.V[0, :, :, :n0] = st["V"]
     cache.S[0, :, :, :n0] = st["S"]
     cache.pos[0, :, :, :n0] = torch.arange(n0, device=dev, dtype=torch.int32)
     cache.n_prompt.fill_(wl.prompt)
@@ -571,14 +578,30 @@ def run_chunk(args, wl):
     qr, kr, out = torch.empty_like(q), torch.empty_like(k), torch.zeros_like(q)
     rotary = B.Rotary(d, (10000.0 ** (-torch.arange(d // 2, device=dev, dtype=torch.float64) / (d // 2))).to(torch.float32))
     positions = (n0 + torch.arange(T, device=dev, dtype=torch.int32)).expand(1, Nb, T).contiguous()
-    scratch = torch.empty(B.dynts_chunk_scratch_bytes(cache.cfg, T), dtype=torch.uint8, device=dev)
+    if args.draft:
+        z = lambda *size: torch.zeros(size, dtype=torch.int32, device=dev)
+        seen, taken, kept, leaf = z(Nb, T, B.tree_words(T)), z(Nb), z(Nb), z(Nb).fill_(T - 1)
+        # every token follows one of those before it, or the cache
+        parents = torch.tensor([(7 * i) % (i + 1) - 1 for i in range(T)], dtype=torch.int32, device=dev).expand(Nb, T).contiguous()
+        lse, q_kept = torch.zeros((Nb, T, wl.n_q_heads), dtype=torch.float32, device=dev), torch.zeros_like(q)
+        lse_kept = torch.zeros_like(lse)
+
+    def chunk():
+        if not args.draft:
+            B.dynts_chunk_step(cache.ctx, 0, qr, kr, v, out, scratch)
+            return
+        B.dynts_tree_build(parents, seen)
+        B.dynts_tree_step(cache.ctx, 0, qr, kr, v, seen, taken, out, scratch, lse=lse)
+        B.dynts_tree_keep(cache.ctx, 0, seen, leaf, taken, kept, q=qr, lse=lse, q_kept=q_kept, lse_kept=lse_kept)
+        B.dynts_chunk_scores(cache.ctx, 0, q_kept, lse_kept, n_new=kept)
+
     parts = [torch.cuda.Event(enable_timing=True) for _ in range(3)]
 
     def step():
         cache.seq_len.fill_(n0)
         cache.next_pos.fill_(n0)
         B.dynts_rotate(rotary, q, k, positions, qr, kr)
-        B.dynts_chunk_step(cache.ctx, 0, qr, kr, v, out, scratch)
+        chunk()
 
     for _ in range(args.warmup):
         step()
@@ -594,24 +617,28 @@ def run_chunk(args, wl):
     parts[1].record()
     for _ in range(20):
         cache.seq_len.fill_(n0)
-        B.dynts_chunk_step(cache.ctx, 0, qr, kr, v, out, scratch)
+        chunk()
     parts[2].record()
     torch.cuda.synchronize()
     assert int(cache.status.item()) == 0
     ms = dt / args.steps * 1e3
     pairs = Nb * wl.n_q_heads * (T * n0 + T * (T + 1) / 2.0)
-    flops = 6.0 * d * pairs   # logits and outputs, and the logits once more for the scores
-    nbytes = Nb * (wl.n_kv_heads * (4.0 * d * n0 + 12.0 * d * T + 8.0 * (n0 + T)) + 8.0 * wl.n_q_heads * d * T)
+    flops = (4.0 if args.draft else 6.0) * d * pairs   # logits and outputs, and the logits once more for the scores (of few tokens of a draft)
+    nbytes = Nb * (wl.n_kv_heads * ((2.0 * 33 / 32 if args.codes else 4.0) * d * n0 + 12.0 * d * T + 8.0 * (n0 + T)) + 8.0 * wl.n_q_heads * d * T)
     mfma, hbm = flops / (ms * 1e-3) / 1e12, nbytes / (ms * 1e-3) / 1e9
     bound = ("mfma", mfma, 2500.0, "TFLOP/s") if mfma / 2500.0 > hbm / 8000.0 else ("hbm", hbm, 8000.0, "GB/s")
-    roofline = {"bound": bound[0], "kernel": "rotate_kernel + chunk_attend_kernel or chunk_attend_few_kernel + chunk_scores_kernel",
+    kernels = "rotate_kernel + chunk_attend_kernel or chunk_attend_few_kernel + chunk_scores_kernel"
+    if args.codes or args.draft:
+        kernels = "rotate_kernel + the kernels of %s" % " and ".join(["codes"] * bool(args.codes) + ["drafts"] * bool(args.draft))
+    roofline = {"bound": bound[0], "kernel": kernels,
                 "achieved": round(bound[1], 1), "peak": bound[2], "unit": bound[3], "frac": round(bound[1] / bound[2], 4),
                 "traffic": None, "algorithmic_flops_per_call": flops, "algorithmic_bytes_per_call": nbytes,
                 "rotate_us": round(parts[0].elapsed_time(parts[1]) / 20 * 1e3, 1),
                 "chunk_step_us": round(parts[1].elapsed_time(parts[2]) / 20 * 1e3, 1)}
     return dict(value=args.steps / dt, ms_per_step=ms, roofline=roofline, whole_step_gbs=hbm,
                 seq_steps_per_s=args.steps * Nb / dt, evictions_timed=0, first_timed_step=0, active_min=Nb, active_max=Nb,
-                mode="chunks of %d new tokens a sequence on a steady-state cache" % T)
+                mode="%s of %d new tokens a sequence on a steady-state cache%s" % (
+                    "drafts" if args.draft else "chunks", T, " of codes (%s)" % args.codes if args.codes else ""))
 
 
 def run_predictor(args, wl):
@@ -721,10 +748,11 @@ def result_line(args, wl, r, cpu):
     """The one JSON object bench.py prints."""
     line = {
         "metric": "predictor calls/sec, 1 MI355X" if getattr(args, "predictor", False) else
+                  "draft steps/sec (rotate+append+attn+keep+score), 1 MI355X" if getattr(args, "draft", 0) else
                   "chunk steps/sec (rotate+append+attn+score), 1 MI355X" if getattr(args, "chunk", 0) else
                   "block-scoring calls/sec, 1 MI355X" if getattr(args, "score_block", 0) else
                   "decode steps/sec (attn+score+evict), 1 MI355X", "value": round(r["value"], 2),
-        "unit": "calls/s" if getattr(args, "score_block", 0) or getattr(args, "predictor", False) or getattr(args, "chunk", 0) else "decode steps/s", "n_gpus": 1, "steps": args.steps, "warmup": args.warmup,
+        "unit": "calls/s" if getattr(args, "score_block", 0) or getattr(args, "predictor", False) or getattr(args, "chunk", 0) or getattr(args, "draft", 0) else "decode steps/s", "n_gpus": 1, "steps": args.steps, "warmup": args.warmup,
         "ms_per_step": round(r["ms_per_step"], 5), "higher_is_better": True, "scaling": "weak",
         "vs_baseline": None, "dtype": "bf16", "data": "synthetic",
         "config": {"workload": "%s: %d layer(s), batch %d, %d q / %d kv heads, head_dim %d, prompt %d, budget %d, "
@@ -769,6 +797,9 @@ def main():
     ap.add_argument("--chunk", type=int, default=0, metavar="T",
                     help="time chunks of T new tokens a sequence (rotary positions, append, attention, scores) on a "
                          "steady-state cache instead of the decode path")
+    ap.add_argument("--draft", type=int, default=0, metavar="T",
+                    help="the same for T drafted tokens a sequence that branch, of which a path is kept")
+    ap.add_argument("--codes", choices=("e4m3", "int8"), default=None, help="with --chunk or --draft: on a cache of 8-bit codes")
     ap.add_argument("--paged", action="store_true",
                     help="steady-state run on the paged (block-table) cache layout instead of the dense one")
     ap.add_argument("--predictor", action="store_true",
@@ -806,7 +837,7 @@ def main():
     elif args.score_block:
         r = run_score_block(args, wl)
         args.no_cpu_baseline = True
-    elif args.chunk:
+    elif args.chunk or args.draft:
         r = run_chunk(args, wl)
         args.no_cpu_baseline = True
     elif args.trajectory:
