@@ -32,6 +32,7 @@ struct ChunkPlan {
   bool few;          // chunk_attend_few_kernel
   bool token;        // coded_token_kernel
   bool groups;       // forms_attend_groups_kernel
+  bool unpack;       // codes are made bf16 in scratch beforehand
   int rows, blocks;  // query rows of a workgroup, row blocks of a unit
   int n_split, Rpad;
   size_t off_lse = 0, off_n = 0, off_ml = 0, off_o = 0, bytes = 0;
@@ -60,30 +61,29 @@ constexpr long long kMostPartials = 65536;
 //   many rows, W = 64, 4500 slots 1 / 4 / 8 / 16: 94.9 / 41.6 / 37.3 / 37.1, 1000 1 / 2: 24.8 / 28.1; W = 128 of 1000 1 / 2 / 4: 25.4 / 30.5 / 31.4; W = 256 of 4500
 //     1 / 2 / 4: 97.8 / 84.7 / 84.4, of 1000 25.6 / 33.2 / 33.2; W = 16 of 16000 8 / 16 / 31: 50.9 / 35.4 / 36.4
 //
-// Caches of codes (the kernel for many rows then has them unpacked before, 0.22 us per 1000 slots of a unit): by the estimates below, in us.  Few / many, both as
-// measured:
-//   head_dim 128, 8 units: 4500 slots R = 512 27.5 / 37.3 (e4m3), 32.9 / 37.5 (whole numbers); 16000 slots R = 256 - / 57, R = 512 92 / 71; 32 units: 1500 slots
-//     R = 512 44.8 / 39.8, 4500 R = 256 53 / 64, R = 512 70 / 77 and 89 / 77; 128 units: 500 slots R = 128 20 / 27, R = 256 44 / 29, 4500 R = 128 79 / 158, R = 256
-//     202 / 175
-//   head_dim 64, 8 units: 4500 slots R = 1024 28 / 31 and 35 / 31; 32 units: 500 slots R = 1024 19 / 20 and 23 / 20, R = 2048 38 / 25, 4500 R = 512 45 / 46, R = 1024
-//     82 / 68
+// Caches of codes by the same rule.  us, few / many (e4m3; whole numbers up to a fourth more):
+//   head_dim 128, 8 units: 4500 slots R = 512 27.2 / 28.3, R = 1024 38.1 / 36.8; 16000 slots R = 128 25.9 / 28.8, R = 256 37.3 / 34.3; 32 units: 1500 slots R = 256 17.4 /
+//     24.1, R = 512 32.8 / 30.3, 4500 R = 256 36.2 / 35.2, 16000 R = 64 39.8 / 50.6, R = 128 66.4 / 56.0; 128 units: 500 slots R = 64 10.9 / 16.2, R = 128 19.9 / 17.1, 4500
+//     R = 64 42.5 / 54.2, R = 128 77.6 / 60.4; 512 units: 500 slots R = 64 37.1 / 26.8, 1500 70.5 / 69.4, 4500 163 / 185
+//   head_dim 64, 8 units: 16000 slots R = 128 19.8 / 21.7, R = 256 27.3 / 24.5; 32 units: 1500 slots R = 512 18.8 / 22.3, 4500 43.2 / 38.3; 128 units: 1500 slots R = 96
+//     17.6 / 23.6, 4500 41.4 / 36.8
 // Groups of waves (drafts, chunks on codes): one workgroup a compute unit, and no two shares of many units, which are bound by HBM, before the slots pay for
 // the joint.  us by the number of shares: W = 128, 32 units of 2500 slots 1 / 2: 39.1 / 35.1, 128 units 44.2 / 47.0, 64 units of 4500 71.4 / 55.2; W = 16, 8 units of
 // 16400 8 / 16 / 32: 40.3 / 33.9 / 47.1; W = 64, 64 units of 9000 2 / 4 / 8: 81.7 / 70.1 / 83.6.
-ChunkPlan chunk_plan(const dynts_config &c, int n_tokens, int slots, bool far_cap = false, bool codes = false, bool tree = false, bool shaped = false) {
+ChunkPlan chunk_plan(const dynts_config &c, int n_tokens, int slots, bool far_cap = false, int code = 0, bool tree = false, bool shaped = false) {
   ChunkPlan pl;
   const long long R = (long long)n_tokens * (c.n_q_heads / c.n_kv_heads), units = (long long)c.batch * c.n_kv_heads;
   const long long F = units * ((R + dynts::kFewRows - 1) / dynts::kFewRows), W = units * ((R + dynts::kChRows - 1) / dynts::kChRows);
   const int room = c.head_dim == 128 ? 256 : 512;  // workgroups of few rows that the chip holds
   pl.few = far_cap || R <= dynts::kFewRows || (F <= room && (R <= 2 * dynts::kFewRows || F * slots <= 1 << 20));
-  if (codes && !far_cap && R > dynts::kFewRows) {
-    const double all = (double)units * slots, cut = F < room ? (room / F < 16 ? room / F : 16) : 1;
-    const double few = (F > room ? (double)F / room : 1.0) * (6.5 + 0.0087 * slots / cut) + (cut > 1 ? 4 : 0);
-    const double many = 18 + all * c.head_dim * 1.7e-6 + all * R * (c.head_dim == 128 ? 3e-7 : 2e-7);
-    pl.few = few < many;
-  }
-  pl.groups = !pl.few && W <= 256 && (tree || (codes && !shaped));
-  pl.token = codes && !tree && R <= dynts::kTokRows;
+  // Codes become bf16 in every row block anew; shaped, or of more blocks than this, they are unpacked before.  us by the blocks of a unit, unpacked / not: e4m3, head_dim 128,
+  // 128 units of 2500 slots 8 / 12 / 16 / 24: 217 291 374 554 / 186 273 361 556, 8 units of 16000 8 / 24 / 64: 98 238 523 / 80 243 578; whole numbers 128 units 8 / 12 / 16: 217
+  // 293 376 / 201 295 396; head_dim 64, 32 units of 2500 8 / 12: 43.5 55.9 / 36.3 62.2, 128 of 1000 8 / 12 / 24: 54.9 77.4 140 / 49.5 75.4 143, whole numbers 55 79 141 / 55
+  // 79 158.
+  const int most_blocks = c.head_dim == 128 ? (code == DYNTS_CODE_E4M3 ? 20 : 10) : code == DYNTS_CODE_E4M3 ? 10 : 8;
+  pl.unpack = code && !pl.few && (shaped || W > units * most_blocks);
+  pl.groups = !pl.few && W <= 256 && (tree || (code && !pl.unpack));
+  pl.token = code && !tree && R <= dynts::kTokRows;
   pl.rows = pl.token ? dynts::kTokRows : pl.few ? dynts::kFewRows : dynts::kChRows;
   pl.blocks = (int)((R + pl.rows - 1) / pl.rows);
   pl.Rpad = pl.blocks * pl.rows;
@@ -135,7 +135,7 @@ dynts_config config_of(const ChunkCache &c) {
 ChunkPlan chunk_plan(const ChunkCache &c, int n_tokens, const dynts_shaping *shaping, bool tree) {
   // (slots of a window: no more than its positions, those of the chunk's other tokens beside them)
   const long long seen = shaping && shaping->window > 0 ? (long long)shaping->window + n_tokens : c.cap;
-  return chunk_plan(config_of(c), n_tokens, (int)(seen < c.cap ? seen : c.cap), far_cap(shaping), c.code != 0, tree, shaped(shaping));
+  return chunk_plan(config_of(c), n_tokens, (int)(seen < c.cap ? seen : c.cap), far_cap(shaping), c.code, tree, shaped(shaping));
 }
 
 // Room behind a chunk's scratch where the layer's codes lie as bf16, for the kernel of many rows.
@@ -253,6 +253,7 @@ void launch_attend_d(const dynts::ChunkAttendParams &p, const ChunkPlan &pl, uns
   if (pl.token) dynts::launch_coded_token(p, SHAPED, grid, st);
   else if (pl.few && (p.seen || p.c.code)) dynts::launch_few_form(p, p.seen ? dynts::kTree : SHAPED ? dynts::kShaped : dynts::kPlain, grid, st);
   else if (pl.groups) dynts::launch_attend_groups(p, p.seen ? dynts::kTree : dynts::kPlain, grid, st);
+  else if (!pl.few && p.c.code) dynts::launch_coded_attend(p, p.seen ? dynts::kTree : dynts::kPlain, grid, st);
   else if (p.seen) dynts::launch_tree_attend(p, grid, st);
   else if (pl.few) hipLaunchKernelGGL((dynts::chunk_attend_few_kernel<D, SHAPED>), dim3(grid), dim3(dynts::kFewThreads), 0, st, p);
   else if (SHAPED && p.shape.slope) hipLaunchKernelGGL((dynts::chunk_attend_kernel<D, SHAPED, SHAPED, false>), dim3(grid), dim3(dynts::kChThreads), 0, st, p);
@@ -279,7 +280,7 @@ int launch_attend(ChunkCache c, const uint16_t *q, int n_tokens, const int32_t *
                   float *lse, void *scratch, const Fresh &fresh, hipStream_t st) {
   const ChunkPlan pl = chunk_plan(c, n_tokens, shaping, seen != nullptr);
   char *const base = static_cast<char *>(scratch);
-  if (c.code && !pl.few) {  // the codes as bf16, in a dense cache in scratch
+  if (pl.unpack) {  // in a dense cache
     uint16_t *const K = reinterpret_cast<uint16_t *>(base + pl.bytes), *const V = reinterpret_cast<uint16_t *>(base + pl.bytes + unpacked_bytes(config_of(c)));
     dynts::launch_read_rows(c, nullptr, c.cap, K, V, false, st);
     c.K = K;

@@ -282,13 +282,16 @@ __device__ __forceinline__ int chunk_lds_v(int row, int piece) {
 // end.  (Copied by a launch of their own before, 512 tokens of 64 sequences, 32 heads on 8: 244 us a step instead of 236, heads of 64 134 instead of
 // 123, 28 on 4 of 32 sequences, 600 tokens, 122 instead of 123.)
 // GROUPS: of four waves, that share out the tiles of the same rows and are joined through LDS (see forms_attend_groups_kernel; not with APPEND or SHAPED).
-template <int D, int MASK, bool BIASED, bool APPEND, int GROUPS = 1>
+// CODE: the cache holds codes, which go through registers, where they become bf16 once for the four waves (not with APPEND or SHAPED).
+template <int D, int MASK, bool BIASED, bool APPEND, int GROUPS = 1, int CODE = 0>
 __device__ __forceinline__ void chunk_attend_rows(const ChunkAttendParams &p) {
   constexpr bool SHAPED = MASK == kShaped, TREE = MASK == kTree;
   using Lds = ChunkLds<D>;
   const ChunkCache &c = p.c;
   // Three tiles' places: one is worked on, one is on its way, one is being asked for.
-  __shared__ __attribute__((aligned(1024))) char sm[GROUPS * Lds::kPlaces * Lds::kPlace];
+  // (Codes: two, one is worked on, the other is written; what comes after is on its way in registers.)
+  constexpr int kGroupLds = CODE ? 4 * Lds::kTileBytes : Lds::kPlaces * Lds::kPlace;
+  __shared__ __attribute__((aligned(1024))) char sm[GROUPS * kGroupLds];
   __shared__ int sm_range[2 * kChWaves];
   const int tid = threadIdx.x, lane = tid & 63, whole = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wave = GROUPS > 1 ? whole % kChWaves : whole, group = GROUPS > 1 ? whole / kChWaves : 0;
@@ -378,7 +381,7 @@ __device__ __forceinline__ void chunk_attend_rows(const ChunkAttendParams &p) {
   // Staging, past the registers: a wave brings kInstr parts of 1 KB of either operand.  A lane's piece of a part is the one that belongs at byte
   // 16 * lane of it; its place in the row is the same for all of a lane's parts.  Rows past the cache's end repeat the last one.
   constexpr int PPR = D / 8, kInstr = Lds::kTileBytes / 1024 / kChWaves, kRowsPart = 1024 / (2 * D);
-  const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)sm + group * (Lds::kPlaces * Lds::kPlace);
+  const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)sm + group * kGroupLds;
   const int my_row = wave * kRowsPart + lane / PPR;
   const uint32_t k_off = chunk_lds<D>(my_row, lane % PPR), v_off = chunk_lds_v<D>(my_row, lane % PPR);
   constexpr int kNext = kRowsPart * kChWaves;  // rows from a lane's part to its next one
@@ -584,20 +587,87 @@ __device__ __forceinline__ void chunk_attend_rows(const ChunkAttendParams &p) {
     add_values(pf, place);
   };
   const int own0 = t0 + group * kChTile, more = own0 - t0;  // this group's first tile
-  bring(own0, lds);
-  bring(own0 + kRound, lds + Lds::kPlace);
-  // (the queries are waited for here: in the loop, every third tile would wait for all loads)
+  if constexpr (CODE != 0) {
+    // a thread's piece of a tile: an eighth of a row of K, and of V, with their scales
+    constexpr int kPiece = D / 8;
+    const int prow = (wave * 64 + lane) >> 3, piece = lane & 7;
+    u32x4 kc{}, vc{};
+    uint32_t k_scale = 0, v_scale = 0;
+    auto fetch = [&](int t) {
+      const size_t row = chunk_tile<1>(c, unit, t, page);
+      if (c.block_table) page = chunk_page(c, unit, t + kRound);
+      const int rows = n - t < kChTile ? n - t : kChTile;  // (rows past the cache's end: zeros)
+      const RowBuffer kb = row_buffer<D / 2>(c.K + row * (D / 2), rows), vb = row_buffer<D / 2>(c.V + row * (D / 2), rows);
+      const RowBuffer ks = scale_buffer<D>(c.K_scale + row * (D / kCodeBlock), rows), vs = scale_buffer<D>(c.V_scale + row * (D / kCodeBlock), rows);
+      const int at = prow * D + piece * kPiece, s_at = at / kCodeBlock;
+      if constexpr (D == 128) {
+        kc = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(kb, at, 0, 0));
+        vc = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(vb, at, 0, 0));
+      } else {
+        const uint2 k2 = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(kb, at, 0, 0)), v2 = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(vb, at, 0, 0));
+        kc[0] = k2.x;
+        kc[1] = k2.y;
+        vc[0] = v2.x;
+        vc[1] = v2.y;
+      }
+      k_scale = __builtin_amdgcn_raw_buffer_load_b8(ks, s_at, 0, 0);
+      v_scale = __builtin_amdgcn_raw_buffer_load_b8(vs, s_at, 0, 0);
+    };
+    char *const mine = sm + group * kGroupLds;
+    auto put = [&](int place) {
+      u32x4 lo, hi;
+      decode16<CODE>(kc, k_scale, lo, hi);  // (head_dim 64: the first eight)
+      *reinterpret_cast<u32x4 *>(mine + place + chunk_lds<D>(prow, D == 128 ? 2 * piece : piece)) = lo;
+      if (D == 128) *reinterpret_cast<u32x4 *>(mine + place + chunk_lds<D>(prow, 2 * piece + 1)) = hi;
+      decode16<CODE>(vc, v_scale, lo, hi);
+      *reinterpret_cast<u32x4 *>(mine + place + Lds::kTileBytes + chunk_lds_v<D>(prow, D == 128 ? 2 * piece : piece)) = lo;
+      if (D == 128) *reinterpret_cast<u32x4 *>(mine + place + Lds::kTileBytes + chunk_lds_v<D>(prow, 2 * piece + 1)) = hi;
+    };
+    // One tile out of its place; the next one goes to the other place, which every wave has left before the barrier.
+    auto tile = [&](int t, auto PLACE, auto FIRST) {
+      constexpr uint32_t place = decltype(PLACE)::value * 2 * Lds::kTileBytes, other = 2 * Lds::kTileBytes - place;
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (this wave's part of the tile is written)
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      if (GROUPS > 1 && t >= t1) return;  // (this group's last round)
+      if (t + kRound < t1) put(other);
+      if (t + 2 * kRound < t1) fetch(t + 2 * kRound);
+      f32x16 s;
+      products(s, place);
+      shape(s, t, nullptr);
+      bf16x8 pf[2];
+      weigh(s, pf, FIRST);
+      add_values(pf, place);
+    };
+    if (own0 < t1) {
+      fetch(own0);
+      put(0);
+      if (own0 + kRound < t1) fetch(own0 + kRound);
+    }
+    constexpr std::integral_constant<int, 0> kA{};
+    constexpr std::integral_constant<int, 1> kB{};
+    // (rounds are counted by the first group's tiles: every wave meets every barrier)
+    if (t0 < t1) tile(own0, kA, std::true_type{});
+    for (int t = t0 + kRound; t < t1; t += 2 * kRound) {
+      tile(t + more, kB, std::false_type{});
+      if (t + kRound < t1) tile(t + kRound + more, kA, std::false_type{});
+    }
+  } else {
+    bring(own0, lds);
+    bring(own0 + kRound, lds + Lds::kPlace);
+    // (the queries are waited for here: in the loop, every third tile would wait for all loads)
 #pragma unroll
-  for (int ks = 0; ks < D / 16; ++ks) asm volatile("" : "+v"(qf[ks]));
-  constexpr std::integral_constant<int, 0> kA{};
-  constexpr std::integral_constant<int, 1> kB{};
-  constexpr std::integral_constant<int, 2> kC{};
-  // (rounds are counted by the first group's tiles: every wave meets every barrier)
-  if (t0 < t1) tile(own0, kA, kC, std::true_type{});
-  for (int t = t0 + kRound; t < t1; t += 3 * kRound) {
-    tile(t + more, kB, kA, std::false_type{});
-    if (t + kRound < t1) tile(t + kRound + more, kC, kB, std::false_type{});
-    if (t + 2 * kRound < t1) tile(t + 2 * kRound + more, kA, kC, std::false_type{});
+    for (int ks = 0; ks < D / 16; ++ks) asm volatile("" : "+v"(qf[ks]));
+    constexpr std::integral_constant<int, 0> kA{};
+    constexpr std::integral_constant<int, 1> kB{};
+    constexpr std::integral_constant<int, 2> kC{};
+    // (rounds are counted by the first group's tiles: every wave meets every barrier)
+    if (t0 < t1) tile(own0, kA, kC, std::true_type{});
+    for (int t = t0 + kRound; t < t1; t += 3 * kRound) {
+      tile(t + more, kB, kA, std::false_type{});
+      if (t + kRound < t1) tile(t + kRound + more, kC, kB, std::false_type{});
+      if (t + 2 * kRound < t1) tile(t + 2 * kRound + more, kA, kC, std::false_type{});
+    }
   }
 
   if (APPEND && split == 0) {  // the tokens whose first row is one of this workgroup's
@@ -610,7 +680,7 @@ __device__ __forceinline__ void chunk_attend_rows(const ChunkAttendParams &p) {
   float sum = l + __shfl_xor(l, 32);
   if (GROUPS > 1) {  // the other groups', one after the other and lane by lane, through what the first does not use for its outputs
     __shared__ float sm_stats[2][kChWaves][64];
-    static_assert(GROUPS == 1 || (kChWaves * 32 * 2 * D + kChWaves * 64 * 2 * D <= GROUPS * Lds::kPlaces * Lds::kPlace && !APPEND && !SHAPED), "room for a group's outputs");
+    static_assert(GROUPS == 1 || (kChWaves * 32 * 2 * D + kChWaves * 64 * 2 * D <= GROUPS * kGroupLds && !APPEND && !SHAPED), "room for a group's outputs");
     f32x4 *const theirs = reinterpret_cast<f32x4 *>(sm + kChWaves * 32 * 2 * D + wave * (64 * 2 * D)) + lane;
 #pragma unroll
     for (int g = 1; g < GROUPS; ++g) {
@@ -692,9 +762,15 @@ __global__ __launch_bounds__(kChThreads, D == 128 ? 3 : 4) void tree_attend_kern
 // in memory and their merge (us, three workgroups / three groups, with the better number of shares each: 32 tokens of 32 sequences, 28 heads on 4, on 2464 slots 65 / 54, of
 // 8 sequences 64 tokens 37 / 35 and on 4500 slots, 32 on 8, 58 / 55, 64 tokens of one on 16384 37 / 34; two groups 56 in place of 54).
 constexpr int kGroups = 3;
-template <int D, int MASK>
+template <int D, int MASK, int CODE>
 __global__ __launch_bounds__(kGroups * kChThreads, kGroups) void forms_attend_groups_kernel(const ChunkAttendParams p) {
-  chunk_attend_rows<D, MASK, false, false, kGroups>(p);
+  chunk_attend_rows<D, MASK, false, false, kGroups, CODE>(p);
+}
+// Many rows on a cache of codes: 512 tokens of 16 sequences on 2656 slots, 32 heads on 8, e4m3, 377 us (with the codes unpacked before, 49 us of it, 391), 64 of 64 sequences
+// on 600 58 (102), 64 of 32 on 2464, 28 on 4, 94 (122).
+template <int D, int MASK, int CODE>
+__global__ __launch_bounds__(kChThreads, D == 128 ? 3 : 4) void coded_attend_kernel(const ChunkAttendParams p) {
+  chunk_attend_rows<D, MASK, false, false, 1, CODE>(p);
 }
 
 // ---- few rows: 32 of them a workgroup, its eight waves share out the keys --------------------------------------------------

@@ -58,14 +58,35 @@ void launch_tree_attend(const ChunkAttendParams &p, unsigned grid, hipStream_t s
   if (p.c.D == 128) hipLaunchKernelGGL((tree_attend_kernel<128>), dim3(grid), dim3(kChThreads), 0, st, p);
   else hipLaunchKernelGGL((tree_attend_kernel<64>), dim3(grid), dim3(kChThreads), 0, st, p);
 }
-template <int D>
+template <int D, int CODE>
 static void attend_groups(const ChunkAttendParams &p, int mask, unsigned grid, hipStream_t st) {
-  if (mask == kTree) hipLaunchKernelGGL((forms_attend_groups_kernel<D, kTree>), dim3(grid), dim3(kGroups * kChThreads), 0, st, p);
-  else hipLaunchKernelGGL((forms_attend_groups_kernel<D, kPlain>), dim3(grid), dim3(kGroups * kChThreads), 0, st, p);
+  if (mask == kTree) hipLaunchKernelGGL((forms_attend_groups_kernel<D, kTree, CODE>), dim3(grid), dim3(kGroups * kChThreads), 0, st, p);
+  else if (CODE) hipLaunchKernelGGL((forms_attend_groups_kernel<D, kPlain, CODE ? CODE : DYNTS_CODE_E4M3>), dim3(grid), dim3(kGroups * kChThreads), 0, st, p);
 }
 void launch_attend_groups(const ChunkAttendParams &p, int mask, unsigned grid, hipStream_t st) {
-  if (p.c.D == 128) attend_groups<128>(p, mask, grid, st);
-  else attend_groups<64>(p, mask, grid, st);
+  if (p.c.D == 128) {
+    if (p.c.code == DYNTS_CODE_E4M3) attend_groups<128, DYNTS_CODE_E4M3>(p, mask, grid, st);
+    else if (p.c.code == DYNTS_CODE_INT8) attend_groups<128, DYNTS_CODE_INT8>(p, mask, grid, st);
+    else attend_groups<128, 0>(p, mask, grid, st);
+  } else {
+    if (p.c.code == DYNTS_CODE_E4M3) attend_groups<64, DYNTS_CODE_E4M3>(p, mask, grid, st);
+    else if (p.c.code == DYNTS_CODE_INT8) attend_groups<64, DYNTS_CODE_INT8>(p, mask, grid, st);
+    else attend_groups<64, 0>(p, mask, grid, st);
+  }
+}
+template <int D, int CODE>
+static void coded_attend(const ChunkAttendParams &p, int mask, unsigned grid, hipStream_t st) {
+  if (mask == kTree) hipLaunchKernelGGL((coded_attend_kernel<D, kTree, CODE>), dim3(grid), dim3(kChThreads), 0, st, p);
+  else hipLaunchKernelGGL((coded_attend_kernel<D, kPlain, CODE>), dim3(grid), dim3(kChThreads), 0, st, p);
+}
+void launch_coded_attend(const ChunkAttendParams &p, int mask, unsigned grid, hipStream_t st) {
+  if (p.c.D == 128) {
+    if (p.c.code == DYNTS_CODE_E4M3) coded_attend<128, DYNTS_CODE_E4M3>(p, mask, grid, st);
+    else coded_attend<128, DYNTS_CODE_INT8>(p, mask, grid, st);
+  } else {
+    if (p.c.code == DYNTS_CODE_E4M3) coded_attend<64, DYNTS_CODE_E4M3>(p, mask, grid, st);
+    else coded_attend<64, DYNTS_CODE_INT8>(p, mask, grid, st);
+  }
 }
 
 template <int D, int CODE, bool SHAPED, bool BIASED>

@@ -11,6 +11,8 @@ constexpr int kTreeMost = 4096;
 
 // chunk_attend_few_kernel's other forms: mask kTree, or a cache of codes with any mask.
 __attribute__((visibility("hidden"))) void launch_few_form(const ChunkAttendParams &p, int mask, unsigned grid, hipStream_t st);
+// many rows on a cache of codes, mask kPlain or kTree
+__attribute__((visibility("hidden"))) void launch_coded_attend(const ChunkAttendParams &p, int mask, unsigned grid, hipStream_t st);
 // up to kTokRows rows on a cache of codes
 __attribute__((visibility("hidden"))) void launch_coded_token(const ChunkAttendParams &p, bool shaped, unsigned grid, hipStream_t st);
 __attribute__((visibility("hidden"))) void launch_coded_token_scores(const ChunkScoreParams &p, bool shaped, unsigned grid, hipStream_t st);
