@@ -400,8 +400,8 @@ int dynts_chunk_step(dynts_ctx *ctx, int32_t layer, const uint16_t *q, const uin
  * A block with an infinity, a NaN or a magnitude of 2^126 and more has s = 255 and reads as NaN.
  *
  * dynts_bind_codes takes such a cache in place of dynts_bind's or (block_table not NULL) dynts_bind_paged's: K, V uint8 [L][Nb][Hkv][cap][d] with scales
- * [L][Nb][Hkv][cap][d / 32], or pools [n_pages][64][d] with scales [n_pages][64][d / 32]; everything else as there.  16-byte aligned; pools zero-filled
- * before first use.  Chunks (dynts_chunk_append, _attend, _scores, _step; n_tokens = 1 is the form for single tokens, question = 1 fills a prompt), drafts
+ * [L][Nb][Hkv][cap][d / 32], or pools [n_pages][64][d] with scales [n_pages][64][d / 32]; everything else as there.
+ * 16-byte aligned; pools zero-filled before first use.  Chunks (dynts_chunk_append, _attend, _scores, _step; n_tokens = 1 is the form for single tokens, question = 1 fills a prompt), drafts
  * (dynts_tree_*), dynts_read_rows, dynts_select_evict, dynts_compact and dynts_update_scores (which has nothing to do) serve it; the new tokens of a
  * chunk see each other's rows as the cache holds them.  The other calls on rows return DYNTS_ECODES: dynts_prefill, dynts_append, dynts_decode_attend,
  * dynts_decode_attend_update, dynts_decode_step, dynts_decode_step_static, dynts_hint_trigger, dynts_score_block, dynts_decode_loop. */

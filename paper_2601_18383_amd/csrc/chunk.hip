@@ -192,7 +192,8 @@ int check_append(const ChunkCache &c, const uint16_t *k_new, const uint16_t *v_n
 // copy: false leaves the rows to chunk_attend_kernel
 int launch_append(const ChunkCache &c, const uint16_t *k_new, const uint16_t *v_new, const float *s_new, int n_tokens,
                   const int32_t *n_new, int question, int32_t *taken, bool copy, hipStream_t st) {
-  const dynts::ChunkAppendParams p{c, k_new, v_new, s_new, n_new, taken, n_tokens, question, group_magic(c.Hkv)};
+  const dynts::ChunkAppendParams p{c, k_new, v_new, s_new, n_new, taken, n_tokens, question,
+                                  ((1ull << 36) + c.Hkv - 1) / c.Hkv};
   const long long pieces = (long long)n_tokens * c.Hkv * (c.D / 8);
   const dim3 block(dynts::kAppendThreads);
   if (c.code && pieces <= dynts::kAppendSmall) {
@@ -204,8 +205,7 @@ int launch_append(const ChunkCache &c, const uint16_t *k_new, const uint16_t *v_
     else hipLaunchKernelGGL((dynts::chunk_reserve_kernel<64, true>), dim3(c.Nb), block, 0, st, p);
     return launch_status();
   }
-  constexpr int kPer = dynts::kAppendThreads * dynts::kAppendAtOnce;
-  const dim3 grid((unsigned)((pieces + kPer - 1) / kPer), c.Nb);
+  const dim3 grid((unsigned)((pieces + dynts::kAppendThreads - 1) / dynts::kAppendThreads), c.Nb);
   if (c.code) copy = false;
   if (c.D == 128) {
     hipLaunchKernelGGL((dynts::chunk_reserve_kernel<128, false>), dim3(c.Nb), block, 0, st, p);

@@ -19,31 +19,33 @@ struct ChunkAppendParams {
   int32_t *taken;                 // [Nb], out: tokens of each sequence that were appended
   int T;
   int question;                   // the tokens are question slots
-  uint32_t hkv_magic;             // ceil(2^32 / Hkv), 0 for Hkv = 1
+  uint64_t hkv_magic;             // ceil(2^36 / Hkv)
 };
 
 constexpr int kAppendThreads = 256;
 // Pieces of 16 bytes, K's, that the first launch copies itself: a workgroup has 16 a thread then.
 constexpr int kAppendSmall = 16 * kAppendThreads;
 
-// Pieces [from, ...) of sequence b, `step` apart: piece p is part p % (D / 8) of head (p / (D / 8)) % Hkv of token p / (D / 8) / Hkv.  Four of them are asked for at a
-// time: behind the stores of one the next would wait for a trip to memory (16 tokens of 32 sequences, 4 heads of 128, by one workgroup a sequence 5.0 us instead
+// Pieces [from, ...) of sequence b, `step` apart: piece p is part p % (D / 8) of head (p / (D / 8)) % Hkv of token p / (D / 8) / Hkv.  AT_ONCE: four of them are asked for at a
+// time where one workgroup has all: behind the stores of one the next would wait for a trip to memory (16 tokens of 32 sequences, 4 heads of 128, by one workgroup a sequence 5.0 us instead
 // of 7.9).  CODE: the cache holds codes (codes.hpp).
 constexpr int kAppendAtOnce = 4;
-template <int D, int CODE = 0>
+// Row `src` of a sequence's [T][Hkv]: its token.  (Below 2^27 rows, 2^20 tokens of 128 heads: the magic number is off by less than 2^7 / 2^36 of the quotient's step a row.)
+__device__ __forceinline__ int append_token(int src, uint64_t magic) { return (int)((uint64_t)(uint32_t)src * magic >> 36); }
+template <int D, int CODE, int AT_ONCE>
 __device__ __forceinline__ void chunk_copy(const ChunkAppendParams &p, int b, int n, int m, int pos0, int from, int step) {
   constexpr int LPR = D / 8;
   const ChunkCache &c = p.c;
   const int end = m * c.Hkv * LPR;
   const size_t row0 = (size_t)b * p.T * c.Hkv;
-  for (int first = from; first < end; first += kAppendAtOnce * step) {
-    u32x4 k[kAppendAtOnce], v[kAppendAtOnce];
-    float score[kAppendAtOnce];
-    size_t row[kAppendAtOnce];  // in the cache
+  for (int first = from; first < end; first += AT_ONCE * step) {
+    u32x4 k[AT_ONCE], v[AT_ONCE];
+    float score[AT_ONCE];
+    size_t row[AT_ONCE];  // in the cache
 #pragma unroll
-    for (int u = 0; u < kAppendAtOnce; ++u) {
+    for (int u = 0; u < AT_ONCE; ++u) {
       const int at = first + u * step < end ? first + u * step : first;
-      const int piece = at % LPR, src = at / LPR, i = p.hkv_magic ? (int)__umulhi((uint32_t)src, p.hkv_magic) : src, h = src - i * c.Hkv;
+      const int piece = at % LPR, src = at / LPR, i = append_token(src, p.hkv_magic), h = src - i * c.Hkv;
       k[u] = load_u32x4(p.k_new + (row0 + src) * D + 8 * piece);
       v[u] = load_u32x4(p.v_new + (row0 + src) * D + 8 * piece);
       score[u] = p.question ? INFINITY : 0.f;
@@ -52,10 +54,10 @@ __device__ __forceinline__ void chunk_copy(const ChunkAppendParams &p, int b, in
       row[u] = c.block_table ? paged_row<1>(c.block_table + unit * c.max_pages, n + i, c.max_pages, c.n_pages) : unit * (size_t)c.cap + (n + i);
     }
 #pragma unroll
-    for (int u = 0; u < kAppendAtOnce; ++u) {
+    for (int u = 0; u < AT_ONCE; ++u) {
       const int at = first + u * step;
       if (at >= end) break;
-      const int piece = at % LPR, src = at / LPR, i = p.hkv_magic ? (int)__umulhi((uint32_t)src, p.hkv_magic) : src, h = src - i * c.Hkv;
+      const int piece = at % LPR, src = at / LPR, i = append_token(src, p.hkv_magic), h = src - i * c.Hkv;
       const size_t dst = row[u] * D + 8 * piece;
       if (CODE) {
         encode8<CODE>(k[u], reinterpret_cast<uint8_t *>(c.K), c.K_scale, dst, piece);
@@ -146,7 +148,7 @@ __device__ __forceinline__ void chunk_reserve(const ChunkAppendParams &p) {
   }
   if (COPY) {
     __syncthreads();  // (the pages above)
-    chunk_copy<D, CODE>(p, b, n, m, pos0, tid, kAppendThreads);
+    chunk_copy<D, CODE, kAppendAtOnce>(p, b, n, m, pos0, tid, kAppendThreads);
   }
 }
 template <int D, bool COPY>
@@ -158,11 +160,11 @@ __global__ __launch_bounds__(kAppendThreads) void coded_reserve_kernel(const Chu
   chunk_reserve<D, true, CODE>(p);
 }
 
-// grid (ceil(T * Hkv * D / 8 / 256 / 4), Nb), behind chunk_reserve_kernel
+// grid (ceil(T * Hkv * D / 8 / 256), Nb), behind chunk_reserve_kernel
 template <int D>
 __global__ __launch_bounds__(kAppendThreads) void chunk_copy_kernel(const ChunkAppendParams p) {
   const int b = blockIdx.y, m = p.taken[b];
-  chunk_copy<D>(p, b, p.c.seq_len[b] - m, m, p.c.next_pos[b] - m, blockIdx.x * kAppendThreads + threadIdx.x, gridDim.x * kAppendThreads);
+  chunk_copy<D, 0, 1>(p, b, p.c.seq_len[b] - m, m, p.c.next_pos[b] - m, blockIdx.x * kAppendThreads + threadIdx.x, gridDim.x * kAppendThreads);
 }
 // The same for a cache of codes, a workgroup for kCodedTokens neighbouring tokens of one head: scales, scores and positions of 32 rows share a line, and are to leave
 // from one L2 (token by token over the heads, as above, 512 of 64 sequences, 8 heads of 128, 54 us instead of 43: 203 MB read and written).

@@ -266,3 +266,12 @@ def test_tensors_elsewhere_or_of_other_sizes_are_refused(B, monkeypatch):
     assert len(called) == 5
     B.dynts_destroy(ctx)
     B.dynts_destroy(there)
+
+
+def test_a_row_finds_its_token():
+    """The multiplication that stands for the division of rows by heads: exact at every border of up to 2^20 tokens of up to 128 heads."""
+    for heads in range(1, 129):
+        magic = ((1 << 36) + heads - 1) // heads
+        for token in [0, 1, 2, 1000, 304000, 304001, (1 << 19) + 1, (1 << 20) - 1]:
+            for row in (token * heads, token * heads + heads - 1):
+                assert row < 1 << 27 and row * magic >> 36 == token and row * magic < 1 << 64

@@ -464,3 +464,19 @@ def test_two_streams(B):
         torch.cuda.synchronize()
         results.append([t.clone() for i in range(2) for t in (outs[i], caches[i].S, caches[i].K_codes, caches[i].K_scale)])
     assert all(torch.equal(x, y) for x, y in zip(*results))
+
+
+def test_rows_of_many_heads(B):
+    """More rows than 2^25 in one chunk, of a number of heads that is no power of two, on a bf16 cache: every row where it belongs."""
+    Hkv, d, T = 127, 64, 330000
+    c = B.Cache(1, 1, Hkv, Hkv, d, T + 64, 0, 0, 1)
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    k = torch.randint(-30000, 30000, (1, T, Hkv, d), generator=gen, device=DEV, dtype=torch.int16).view(torch.bfloat16)
+    scratch = torch.empty(B.dynts_chunk_scratch_bytes(c.cfg, T), dtype=torch.uint8, device=DEV)
+    B.dynts_chunk_append(c.ctx, 0, k, k, scratch)
+    assert int(c.status.item()) == 0 and int(c.seq_len.item()) == T
+    for h in list(range(0, Hkv, 9)) + [Hkv - 1]:
+        assert torch.equal(c.K[0, 0, h, :T].view(torch.int16), k[0, :, h].view(torch.int16)), h
+        assert torch.equal(c.V[0, 0, h, :T].view(torch.int16), k[0, :, h].view(torch.int16)), h
+        assert torch.equal(c.pos[0, 0, h, :T], torch.arange(T, dtype=torch.int32, device=DEV))
+    assert not c.K[0, 0, :, T:].any()
