@@ -88,27 +88,45 @@ __device__ __forceinline__ void decode16(u32x4 x, uint32_t s, u32x4 &lo, u32x4 &
   }
 }
 
-// load_row_frags for a row of codes.
+// load_row_frags for a row of codes: 16 bytes a lane, the halves of the wave then change what the other's operands want.  (Scores of 35 rows of 128 units on 2464
+// slots 15.5 us instead of 16.9 with eight bytes a lane.  With head_dim 64 eight bytes are taken: 10.2 instead of 11.4, 40 rows of 128 units on 2500.)
 template <int D, int CODE>
 __device__ __forceinline__ void decode_row_frags(bf16x8 (&f)[D / 16], const uint8_t *row, const uint8_t *scales, int hf) {
-  uint2 x[D / 16];
+  u32x4 x[D / 32];
 #pragma unroll
-  for (int ks = 0; ks < D / 16; ++ks) x[ks] = *reinterpret_cast<const uint2 *>(row + 16 * ks + 8 * hf);
+  for (int j = 0; j < D / 32; ++j) {
+    if (D == 128) {
+      x[j] = *reinterpret_cast<const u32x4 *>(row + 32 * j + 16 * hf);
+    } else {
+      const uint2 a = *reinterpret_cast<const uint2 *>(row + 32 * j + 8 * hf), z = *reinterpret_cast<const uint2 *>(row + 32 * j + 16 + 8 * hf);
+      x[j] = u32x4{a.x, a.y, z.x, z.y};
+    }
+  }
   uint32_t s;
   if (D == 128) s = *reinterpret_cast<const uint32_t *>(scales);
   else s = *reinterpret_cast<const uint16_t *>(scales);
 #pragma unroll
-  for (int ks = 0; ks < D / 16; ++ks) {
-    const float scale = __uint_as_float((s >> (8 * (ks / 2)) & 255u) << 23);
-    u32x4 w;
-    uint32_t a, b;
-    decode4<CODE>(x[ks].x, scale, a, b);
-    w[0] = a;
-    w[1] = b;
-    decode4<CODE>(x[ks].y, scale, a, b);
-    w[2] = a;
-    w[3] = b;
-    f[ks] = __builtin_bit_cast(bf16x8, w);
+  for (int j = 0; j < D / 32; ++j) {
+    const float scale = __uint_as_float((s >> (8 * j) & 255u) << 23);
+    u32x4 w[2];  // elements 32 j + 8 hf .. +7 and 32 j + 16 + 8 hf .. +7
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      uint32_t y[2] = {x[j][k], x[j][2 + k]};
+      if (D == 128) {
+        const auto swapped = __builtin_amdgcn_permlane32_swap(y[0], y[1], false, false);
+        y[0] = swapped[0];
+        y[1] = swapped[1];
+      }
+#pragma unroll
+      for (int o = 0; o < 2; ++o) {
+        uint32_t lo, hi;
+        decode4<CODE>(y[o], scale, lo, hi);
+        w[o][2 * k] = lo;
+        w[o][2 * k + 1] = hi;
+      }
+    }
+    f[2 * j] = __builtin_bit_cast(bf16x8, w[0]);
+    f[2 * j + 1] = __builtin_bit_cast(bf16x8, w[1]);
   }
 }
 
