@@ -262,7 +262,8 @@ void launch_attend_d(const dynts::ChunkAttendParams &p, const ChunkPlan &pl, uns
   if (p.n_split > 1) {
     constexpr int rows = dynts::kMergeThreads / (D / 8);
     const dim3 merge((p.T * p.c.G + rows - 1) / rows, p.c.Nb * p.c.Hkv), threads(dynts::kMergeThreads);
-    if (p.n_split > 4) hipLaunchKernelGGL((dynts::chunk_merge_kernel<D, 16>), merge, threads, 0, st, p, pl.rows);
+    if (p.n_split > 4 && (p.seen || p.c.code)) dynts::launch_merge_form(p, pl.rows, st);
+    else if (p.n_split > 4) hipLaunchKernelGGL((dynts::chunk_merge_kernel<D, 16>), merge, threads, 0, st, p, pl.rows);
     else if (p.n_split > 2) hipLaunchKernelGGL((dynts::chunk_merge_kernel<D, 4>), merge, threads, 0, st, p, pl.rows);
     else hipLaunchKernelGGL((dynts::chunk_merge_kernel<D, 2>), merge, threads, 0, st, p, pl.rows);
   }

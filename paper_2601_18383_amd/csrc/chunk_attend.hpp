@@ -758,7 +758,7 @@ template <int D>
 __global__ __launch_bounds__(kChThreads, D == 128 ? 3 : 4) void tree_attend_kernel(const ChunkAttendParams p) {
   chunk_attend_rows<D, kTree, false, false>(p);
 }
-// Drafts, and chunks on unpacked codes, of few row blocks: as many waves a compute unit as three workgroups have, on the same rows, which saves partial outputs
+// Drafts, and chunks on codes, of few row blocks: as many waves a compute unit as three workgroups have, on the same rows, which saves partial outputs
 // in memory and their merge (us, three workgroups / three groups, with the better number of shares each: 32 tokens of 32 sequences, 28 heads on 4, on 2464 slots 65 / 54, of
 // 8 sequences 64 tokens 37 / 35 and on 4500 slots, 32 on 8, 58 / 55, 64 tokens of one on 16384 37 / 34; two groups 56 in place of 54).
 constexpr int kGroups = 3;
@@ -1065,7 +1065,7 @@ __global__ __launch_bounds__(kFewThreads, D == 64 && MASK != kShaped ? 4 : 2) vo
 }
 
 // The shares of a row together.  grid (ceil(T * G / kMergeRows), units), D / 8 threads a row.  AT_ONCE: shares that are asked for at a time, the first ones
-// before it is known how many there are (16 of single tokens of 8 units: 3.1 us instead of 5.4 with four).
+// before it is known how many there are (with four, and their number first, 16 shares of 8 units take 2 us longer).
 constexpr int kMergeThreads = 256;
 template <int D, int AT_ONCE>
 __global__ __launch_bounds__(kMergeThreads) void chunk_merge_kernel(const ChunkAttendParams p, int block_rows) {
@@ -1106,6 +1106,62 @@ __global__ __launch_bounds__(kMergeThreads) void chunk_merge_kernel(const ChunkA
       }
     }
   }
+  const int i = chunk_token(r, p.g_magic);
+  chunk_write<D>(p, ((size_t)b * p.T + i) * c.Hq + (size_t)h * c.G + (r - i * c.G), d0, o, top, sum);
+}
+
+// The same for more than four shares of drafts and of caches of codes: a wave a row, its lanes share out the shares as well, all of them asked for at once.
+// (Whole calls, with this one / with the one above: single tokens of 8 units of 16400 slots, 32 shares, 14.5 / 16.9 us; 256 rows of them, 16 shares, 33.3 / 34.1; of 128 units of
+// 2464 slots, two shares, 20.1 / 19.6.)
+constexpr int kMergeMost = 32;  // shares
+template <int D>
+__global__ __launch_bounds__(kMergeThreads) void forms_merge_kernel(const ChunkAttendParams p, int block_rows) {
+  const ChunkCache &c = p.c;
+  constexpr int LPR = D / 8, PARTS = 64 / LPR, EACH = kMergeMost / PARTS;
+  const int unit = blockIdx.y, b = unit / c.Hkv, h = unit - b * c.Hkv, lane = threadIdx.x & 63;
+  const int r = blockIdx.x * (kMergeThreads / 64) + threadIdx.x / 64, part = lane / LPR, d0 = 8 * (lane % LPR);
+  if (r >= p.T * c.G) return;
+  const size_t first = (size_t)unit * p.n_split * p.Rpad + r;
+  float2 ml[EACH];
+  f32x4 a[EACH], z[EACH];
+#pragma unroll
+  for (int s = 0; s < EACH; ++s) {
+    const int share = PARTS * s + part;
+    ml[s] = float2{0.f, 0.f};
+    if (share >= p.n_split) continue;
+    const size_t prow = first + (size_t)share * p.Rpad;
+    ml[s] = *reinterpret_cast<const float2 *>(p.part_ml + 2 * prow);
+    a[s] = *reinterpret_cast<const f32x4 *>(p.part_o + prow * D + d0);
+    z[s] = *reinterpret_cast<const f32x4 *>(p.part_o + prow * D + d0 + 4);
+  }
+  const int shares = p.part_n[unit * (p.Rpad / block_rows) + r / block_rows];
+  int n;
+  const int m = chunk_tokens(c, p.n_new, p.T, b, n);
+  if (r >= m * c.G || shares == 1) return;
+  float top = -INFINITY, sum = 0.f, o[8] = {};
+#pragma unroll
+  for (int s = 0; s < EACH; ++s)
+    if (PARTS * s + part < shares && ml[s].y > 0.f) top = fmaxf(top, ml[s].x);  // (else a share without a key that the row sees)
+#pragma unroll
+  for (int d = LPR; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+#pragma unroll
+  for (int s = 0; s < EACH; ++s) {
+    if (PARTS * s + part >= shares || !(ml[s].y > 0.f)) continue;
+    const float w = fast_exp2(ml[s].x - top);
+    sum += ml[s].y * w;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      o[j] += a[s][j] * w;
+      o[4 + j] += z[s][j] * w;
+    }
+  }
+#pragma unroll
+  for (int d = LPR; d < 64; d *= 2) {
+    sum += __shfl_xor(sum, d);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o[j] += __shfl_xor(o[j], d);
+  }
+  if (part > 0) return;
   const int i = chunk_token(r, p.g_magic);
   chunk_write<D>(p, ((size_t)b * p.T + i) * c.Hq + (size_t)h * c.G + (r - i * c.G), d0, o, top, sum);
 }

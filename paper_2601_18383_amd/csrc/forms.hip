@@ -7,11 +7,15 @@
 
 namespace dynts {
 
+// (a cache that is not of codes comes with mask kTree)
 template <int D, int CODE>
 static void few_form(const ChunkAttendParams &p, int mask, unsigned grid, hipStream_t st) {
-  if (mask == kTree) hipLaunchKernelGGL((forms_attend_few_kernel<D, kTree, CODE>), dim3(grid), dim3(kFewThreads), 0, st, p);
-  else if (mask == kShaped) hipLaunchKernelGGL((forms_attend_few_kernel<D, kShaped, CODE == 0 ? DYNTS_CODE_E4M3 : CODE>), dim3(grid), dim3(kFewThreads), 0, st, p);
-  else hipLaunchKernelGGL((forms_attend_few_kernel<D, kPlain, CODE == 0 ? DYNTS_CODE_E4M3 : CODE>), dim3(grid), dim3(kFewThreads), 0, st, p);
+  auto *kernel = forms_attend_few_kernel<D, kTree, CODE>;
+  if constexpr (CODE != 0) {
+    if (mask == kShaped) kernel = forms_attend_few_kernel<D, kShaped, CODE>;
+    else if (mask == kPlain) kernel = forms_attend_few_kernel<D, kPlain, CODE>;
+  }
+  hipLaunchKernelGGL(kernel, dim3(grid), dim3(kFewThreads), 0, st, p);
 }
 void launch_few_form(const ChunkAttendParams &p, int mask, unsigned grid, hipStream_t st) {
   if (p.c.D == 128) {
@@ -60,8 +64,11 @@ void launch_tree_attend(const ChunkAttendParams &p, unsigned grid, hipStream_t s
 }
 template <int D, int CODE>
 static void attend_groups(const ChunkAttendParams &p, int mask, unsigned grid, hipStream_t st) {
-  if (mask == kTree) hipLaunchKernelGGL((forms_attend_groups_kernel<D, kTree, CODE>), dim3(grid), dim3(kGroups * kChThreads), 0, st, p);
-  else if (CODE) hipLaunchKernelGGL((forms_attend_groups_kernel<D, kPlain, CODE ? CODE : DYNTS_CODE_E4M3>), dim3(grid), dim3(kGroups * kChThreads), 0, st, p);
+  auto *kernel = forms_attend_groups_kernel<D, kTree, CODE>;
+  if constexpr (CODE != 0) {
+    if (mask == kPlain) kernel = forms_attend_groups_kernel<D, kPlain, CODE>;
+  }
+  hipLaunchKernelGGL(kernel, dim3(grid), dim3(kGroups * kChThreads), 0, st, p);
 }
 void launch_attend_groups(const ChunkAttendParams &p, int mask, unsigned grid, hipStream_t st) {
   if (p.c.D == 128) {
@@ -73,6 +80,11 @@ void launch_attend_groups(const ChunkAttendParams &p, int mask, unsigned grid, h
     else if (p.c.code == DYNTS_CODE_INT8) attend_groups<64, DYNTS_CODE_INT8>(p, mask, grid, st);
     else attend_groups<64, 0>(p, mask, grid, st);
   }
+}
+void launch_merge_form(const ChunkAttendParams &p, int block_rows, hipStream_t st) {
+  const dim3 grid((p.T * p.c.G + kMergeThreads / 64 - 1) / (kMergeThreads / 64), p.c.Nb * p.c.Hkv), block(kMergeThreads);
+  if (p.c.D == 128) hipLaunchKernelGGL((forms_merge_kernel<128>), grid, block, 0, st, p, block_rows);
+  else hipLaunchKernelGGL((forms_merge_kernel<64>), grid, block, 0, st, p, block_rows);
 }
 template <int D, int CODE>
 static void coded_attend(const ChunkAttendParams &p, int mask, unsigned grid, hipStream_t st) {

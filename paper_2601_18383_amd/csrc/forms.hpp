@@ -19,6 +19,8 @@ __attribute__((visibility("hidden"))) void launch_coded_token_scores(const Chunk
 // many rows: a draft's tokens; kGroups groups of waves, with mask kPlain or kTree
 __attribute__((visibility("hidden"))) void launch_tree_attend(const ChunkAttendParams &p, unsigned grid, hipStream_t st);
 __attribute__((visibility("hidden"))) void launch_attend_groups(const ChunkAttendParams &p, int mask, unsigned grid, hipStream_t st);
+// the shares of either together, more than four
+__attribute__((visibility("hidden"))) void launch_merge_form(const ChunkAttendParams &p, int block_rows, hipStream_t st);
 __attribute__((visibility("hidden"))) void launch_coded_scores(const ChunkScoreParams &p, bool few, bool shaped, bool biased, unsigned grid, hipStream_t st);
 // small: one launch that makes room and writes; else one (behind chunk_reserve_kernel) that writes
 __attribute__((visibility("hidden"))) void launch_coded_append(const ChunkAppendParams &p, bool small, hipStream_t st);
