@@ -32,6 +32,7 @@ struct ChunkPlan {
   bool few;          // chunk_attend_few_kernel
   bool token;        // coded_token_kernel
   bool groups;       // forms_attend_groups_kernel
+  bool half;         // forms_attend_half_kernel
   bool unpack;       // codes are made bf16 in scratch beforehand
   int rows, blocks;  // query rows of a workgroup, row blocks of a unit
   int n_split, Rpad;
@@ -70,6 +71,11 @@ constexpr long long kMostPartials = 65536;
 // Groups of waves (drafts, chunks on codes): one workgroup a compute unit, and no two shares of many units, which are bound by HBM, before the slots pay for
 // the joint.  us by the number of shares: W = 128, 32 units of 2500 slots 1 / 2: 39.1 / 35.1, 128 units 44.2 / 47.0, 64 units of 4500 71.4 / 55.2; W = 16, 8 units of
 // 16400 8 / 16 / 32: 40.3 / 33.9 / 47.1; W = 64, 64 units of 9000 2 / 4 / 8: 81.7 / 70.1 / 83.6.
+// Where they have no shares and half as many rows a workgroup, H of them, still have a compute unit each: half.  us, 128 rows / 64 (bf16 | e4m3 | whole numbers):
+//   head_dim 128, 500 slots: 64 units R = 256 17.2 / 14.6 | 18.5 / 15.8 | 19.6 / 16.7, 128 of R = 128 16.1 / 14.6 | 18.0 / 15.2 | 18.9 / 16.0, 256 of R = 64 18.7 / 17.1 | 18.0 / 16.2 |
+//     19.2 / 16.9; 2464 slots: 128 of R = 112 45.7 / 41.6 | 47.1 / 42.4 | 51.4 / 45.8, 256 of R = 64 63.5 / 61.1 | 56.1 / 50.1 | 61.4 / 52.3, H = 512 53.3 / 56.9 | 55.9 / 56.8 | 61.9 / 61.0
+//   head_dim 64, 2464 slots: 128 of R = 128 27.8 / 25.1 | 35.4 / 29.1 | 37.1 / 30.9
+//   instead of shares: 64 units of 4500 slots R = 128 45.8 / 47.2 | 38.5 / 44.1 | 40.7 / 48.1, 32 of 16000 R = 256 88.0 / 112 | 87.3 / 123 | 97.2 / 135
 ChunkPlan chunk_plan(const dynts_config &c, int n_tokens, int slots, bool far_cap = false, int code = 0, bool tree = false, bool shaped = false) {
   ChunkPlan pl;
   const long long R = (long long)n_tokens * (c.n_q_heads / c.n_kv_heads), units = (long long)c.batch * c.n_kv_heads;
@@ -85,8 +91,6 @@ ChunkPlan chunk_plan(const dynts_config &c, int n_tokens, int slots, bool far_ca
   pl.groups = !pl.few && W <= 256 && (tree || (code && !pl.unpack));
   pl.token = code && !tree && R <= dynts::kTokRows;
   pl.rows = pl.token ? dynts::kTokRows : pl.few ? dynts::kFewRows : dynts::kChRows;
-  pl.blocks = (int)((R + pl.rows - 1) / pl.rows);
-  pl.Rpad = pl.blocks * pl.rows;
   long long shares = slots / (32 * dynts::kShareTiles);
   if (pl.token) {
     shares = shares < 32 ? shares : 32;
@@ -104,6 +108,10 @@ ChunkPlan chunk_plan(const dynts_config &c, int n_tokens, int slots, bool far_ca
     }
   }
   if (slots < 1536) shares = 1;
+  pl.half = pl.groups && shares < 2 && units * ((R + dynts::kHalfRows - 1) / dynts::kHalfRows) <= 256;
+  if (pl.half) pl.rows = dynts::kHalfRows;
+  pl.blocks = (int)((R + pl.rows - 1) / pl.rows);
+  pl.Rpad = pl.blocks * pl.rows;
   while (shares > 1 && units * pl.Rpad * shares > kMostPartials) --shares;
   pl.n_split = shares < 1 ? 1 : (int)shares;
   size_t off = align_up((size_t)c.batch * sizeof(int32_t));
@@ -225,7 +233,7 @@ unsigned chunk_grid(const ChunkCache &c, long long blocks, int threads) {
   return wgs >= (1LL << 32) / threads ? 0u : (unsigned)wgs;
 }
 unsigned attend_grid(const ChunkCache &c, const ChunkPlan &pl) {
-  return chunk_grid(c, (long long)pl.blocks * pl.n_split, pl.token ? dynts::kTokWaves * 64 : pl.few ? dynts::kFewThreads : pl.groups ? dynts::kGroups * dynts::kChThreads : dynts::kChThreads);
+  return chunk_grid(c, (long long)pl.blocks * pl.n_split, pl.token ? dynts::kTokWaves * 64 : pl.few ? dynts::kFewThreads : pl.half ? dynts::kHalfGroups<1> * dynts::kHalfWaves * 64 : pl.groups ? dynts::kGroups * dynts::kChThreads : dynts::kChThreads);
 }
 // Which kernel of chunk_scores.hpp.  C: chunks of 32 rows of a unit, W: workgroups of 64 slots, one a compute unit.  Few slots: 7 + C / 4 us a round of 256 of
 // them; many: 4 + 0.8 C us while its W / 4 workgroups have a compute unit each.  us, few / many:
@@ -252,6 +260,7 @@ template <int D, bool SHAPED>
 void launch_attend_d(const dynts::ChunkAttendParams &p, const ChunkPlan &pl, unsigned grid, hipStream_t st) {
   if (pl.token) dynts::launch_coded_token(p, SHAPED, grid, st);
   else if (pl.few && (p.seen || p.c.code)) dynts::launch_few_form(p, p.seen ? dynts::kTree : SHAPED ? dynts::kShaped : dynts::kPlain, grid, st);
+  else if (pl.half) dynts::launch_attend_half(p, p.seen ? dynts::kTree : dynts::kPlain, grid, st);
   else if (pl.groups) dynts::launch_attend_groups(p, p.seen ? dynts::kTree : dynts::kPlain, grid, st);
   else if (!pl.few && p.c.code) dynts::launch_coded_attend(p, p.seen ? dynts::kTree : dynts::kPlain, grid, st);
   else if (p.seen) dynts::launch_tree_attend(p, grid, st);

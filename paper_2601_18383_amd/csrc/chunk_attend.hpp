@@ -281,24 +281,25 @@ __device__ __forceinline__ int chunk_lds_v(int row, int piece) {
 // form): the chunk's own rows are not in the cache yet; they are read where the caller has them, and every workgroup copies those of its tokens at its
 // end.  (Copied by a launch of their own before, 512 tokens of 64 sequences, 32 heads on 8: 244 us a step instead of 236, heads of 64 134 instead of
 // 123, 28 on 4 of 32 sequences, 600 tokens, 122 instead of 123.)
-// GROUPS: of four waves, that share out the tiles of the same rows and are joined through LDS (see forms_attend_groups_kernel; not with APPEND or SHAPED).
-// CODE: the cache holds codes, which go through registers, where they become bf16 once for the four waves (not with APPEND or SHAPED).
-template <int D, int MASK, bool BIASED, bool APPEND, int GROUPS = 1, int CODE = 0>
+// GROUPS: of WAVES waves, that share out the tiles of the same rows and are joined through LDS (see forms_attend_groups_kernel; not with APPEND or SHAPED).
+// CODE: the cache holds codes, which go through registers, where they become bf16 once for a group's waves (not with APPEND or SHAPED).
+template <int D, int MASK, bool BIASED, bool APPEND, int GROUPS = 1, int CODE = 0, int WAVES = kChWaves>
 __device__ __forceinline__ void chunk_attend_rows(const ChunkAttendParams &p) {
   constexpr bool SHAPED = MASK == kShaped, TREE = MASK == kTree;
   using Lds = ChunkLds<D>;
+  constexpr int kRows = 32 * WAVES;  // query rows of the workgroup
   const ChunkCache &c = p.c;
   // Three tiles' places: one is worked on, one is on its way, one is being asked for.
   // (Codes: two, one is worked on, the other is written; what comes after is on its way in registers.)
   constexpr int kGroupLds = CODE ? 4 * Lds::kTileBytes : Lds::kPlaces * Lds::kPlace;
   __shared__ __attribute__((aligned(1024))) char sm[GROUPS * kGroupLds];
-  __shared__ int sm_range[2 * kChWaves];
+  __shared__ int sm_range[2 * WAVES];
   const int tid = threadIdx.x, lane = tid & 63, whole = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wave = GROUPS > 1 ? whole % kChWaves : whole, group = GROUPS > 1 ? whole / kChWaves : 0;
+  const int wave = GROUPS > 1 ? whole % WAVES : whole, group = GROUPS > 1 ? whole / WAVES : 0;
   constexpr int kRound = GROUPS * kChTile;  // slots from a wave's tile to its next one
   const int col = lane & 31, hf = lane >> 5, r16 = lane & 15;
   int unit, blk;
-  const int n_blk = (p.T * c.G + kChRows - 1) / kChRows;
+  const int n_blk = (p.T * c.G + kRows - 1) / kRows;
   // (documents: which rows see most is not known, and units at once cost: means of eight draws, 470 tokens of 21 sequences on 1571 slots, 28 heads on 4, in
   // documents 71 us unit by unit, 90 four at a time, 75 two; 4096 of 2, 32 on 8, 102 / 102 / 101; first rows first 76 and 110)
   if (!chunk_map(SHAPED && p.shape.first ? 1 : 4, n_blk * p.n_split, c.Nb * c.Hkv, unit, blk)) return;
@@ -309,10 +310,10 @@ __device__ __forceinline__ void chunk_attend_rows(const ChunkAttendParams &p) {
   const int m = chunk_tokens(c, p.n_new, p.T, b, n);
   const int R = m * c.G;
   blk = n_blk - 1 - blk;  // (the last rows see most)
-  if (blk * kChRows >= R) return;
+  if (blk * kRows >= R) return;
   const int base = n - m;  // the chunk's first slot
 
-  const int row0 = blk * kChRows + wave * 32;
+  const int row0 = blk * kRows + wave * 32;
   const int r = row0 + col < R ? row0 + col : R - 1;
   const int tok = chunk_token(r, p.g_magic), g = r - tok * c.G;
   bf16x8 qf[D / 16];
@@ -324,8 +325,8 @@ __device__ __forceinline__ void chunk_attend_rows(const ChunkAttendParams &p) {
   const int32_t *pos = c.pos + (size_t)unit * c.cap;
   int lim, own = 0, t_lo = 0, t_hi, all_lo = 0, all_hi, own_lo = 0;  // (own_lo: of the wave's first row)
   uint32_t span = 0;
-  const int r1 = blk * kChRows + kChRows - 1;
-  const int i0 = chunk_token(blk * kChRows, p.g_magic), i1 = chunk_token(r1 < R ? r1 : R - 1, p.g_magic);
+  const int r1 = blk * kRows + kRows - 1;
+  const int i0 = chunk_token(blk * kRows, p.g_magic), i1 = chunk_token(r1 < R ? r1 : R - 1, p.g_magic);
   if (SHAPED) {
     own = pos[base + tok];
     const int head = pos[0], tail = pos[n - 1];
@@ -343,13 +344,13 @@ __device__ __forceinline__ void chunk_attend_rows(const ChunkAttendParams &p) {
     }
     if (lane == 0) {
       sm_range[wave] = first;
-      sm_range[kChWaves + wave] = last;
+      sm_range[WAVES + wave] = last;
     }
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < kChWaves; ++w) {
+    for (int w = 0; w < WAVES; ++w) {
       first = sm_range[w] < first ? sm_range[w] : first;
-      last = sm_range[kChWaves + w] > last ? sm_range[kChWaves + w] : last;
+      last = sm_range[WAVES + w] > last ? sm_range[WAVES + w] : last;
     }
     chunk_range(p.shape, pos, n, base, i0, i1, __builtin_amdgcn_readfirstlane(first), __builtin_amdgcn_readfirstlane(last), __builtin_amdgcn_readfirstlane(head),
                 __builtin_amdgcn_readfirstlane(tail), lane, t_lo, t_hi);
@@ -379,12 +380,18 @@ __device__ __forceinline__ void chunk_attend_rows(const ChunkAttendParams &p) {
     for (int e = 0; e < 16; ++e) acc[dt][e] = 0.f;
 
   // Staging, past the registers: a wave brings kInstr parts of 1 KB of either operand.  A lane's piece of a part is the one that belongs at byte
-  // 16 * lane of it; its place in the row is the same for all of a lane's parts.  Rows past the cache's end repeat the last one.
-  constexpr int PPR = D / 8, kInstr = Lds::kTileBytes / 1024 / kChWaves, kRowsPart = 1024 / (2 * D);
+  // 16 * lane of it; its place in the row comes again every kSets parts.  Rows past the cache's end repeat the last one.
+  constexpr int PPR = D / 8, kInstr = Lds::kTileBytes / 1024 / WAVES, kRowsPart = 1024 / (2 * D);
   const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)sm + group * kGroupLds;
   const int my_row = wave * kRowsPart + lane / PPR;
-  const uint32_t k_off = chunk_lds<D>(my_row, lane % PPR), v_off = chunk_lds_v<D>(my_row, lane % PPR);
-  constexpr int kNext = kRowsPart * kChWaves;  // rows from a lane's part to its next one
+  constexpr int kNext = kRowsPart * WAVES;  // rows from a lane's part to its next one
+  constexpr int kSets = kChWaves / WAVES;   // parts after which a piece's place in its row comes again
+  uint32_t k_off[kSets], v_off[kSets];
+#pragma unroll
+  for (int j = 0; j < kSets; ++j) {
+    k_off[j] = chunk_lds<D>(my_row + j * kNext, lane % PPR) - j * kNext * 2 * D;
+    v_off[j] = chunk_lds_v<D>(my_row + j * kNext, lane % PPR) - j * kNext * 2 * D;
+  }
   // rows `cached` and on of a tile: from k_new and v_new, where a token's heads lie side by side
   auto bring_fresh = [&](int t, int rows, int cached, uint32_t place) {
     const uint32_t pitch = (uint32_t)c.Hkv * 2 * D;
@@ -396,9 +403,9 @@ __device__ __forceinline__ void chunk_attend_rows(const ChunkAttendParams &p) {
     for (int i = 0; i < kInstr; ++i) {
       const int row = my_row + i * kNext;
       if (row < cached) continue;
-      const uint32_t off = (row < rows ? row : rows - 1) * pitch - my_row * (2 * D), to = place + 1024 * (wave + i * kChWaves);
-      lds_bring16(kb, off + k_off, 0, to);
-      lds_bring16(vb, off + v_off, 0, to + Lds::kTileBytes);
+      const uint32_t off = (row < rows ? row : rows - 1) * pitch - my_row * (2 * D), to = place + 1024 * (wave + i * WAVES);
+      lds_bring16(kb, off + k_off[i % kSets], 0, to);
+      lds_bring16(vb, off + v_off[i % kSets], 0, to + Lds::kTileBytes);
     }
   };
   // (the page of the next tile to bring: looked up a tile ahead)
@@ -418,16 +425,16 @@ __device__ __forceinline__ void chunk_attend_rows(const ChunkAttendParams &p) {
     const RowBuffer kb = row_buffer<D>(c.K + at, rows), vb = row_buffer<D>(c.V + at, rows);
 #pragma unroll
     for (int i = 0; i < kInstr; ++i) {
-      const uint32_t to = place + 1024 * (wave + i * kChWaves);
+      const uint32_t to = place + 1024 * (wave + i * WAVES);
       if (rows == kChTile) {
-        lds_bring16(kb, k_off, i * kNext * 2 * D, to);
-        lds_bring16(vb, v_off, i * kNext * 2 * D, to + Lds::kTileBytes);
+        lds_bring16(kb, k_off[i % kSets], i * kNext * 2 * D, to);
+        lds_bring16(vb, v_off[i % kSets], i * kNext * 2 * D, to + Lds::kTileBytes);
       } else {
         const int over = my_row + i * kNext - (rows - 1);
         if (APPEND && over > 0) continue;
         const uint32_t back = (over > 0 ? over : 0) * (2 * D);
-        lds_bring16(kb, k_off + i * kNext * 2 * D - back, 0, to);
-        lds_bring16(vb, v_off + i * kNext * 2 * D - back, 0, to + Lds::kTileBytes);
+        lds_bring16(kb, k_off[i % kSets] + i * kNext * 2 * D - back, 0, to);
+        lds_bring16(vb, v_off[i % kSets] + i * kNext * 2 * D - back, 0, to + Lds::kTileBytes);
       }
     }
     if (SHAPED && wave == 0 && lane < kChTile) {
@@ -588,40 +595,45 @@ __device__ __forceinline__ void chunk_attend_rows(const ChunkAttendParams &p) {
   };
   const int own0 = t0 + group * kChTile, more = own0 - t0;  // this group's first tile
   if constexpr (CODE != 0) {
-    // a thread's piece of a tile: an eighth of a row of K, and of V, with their scales
-    constexpr int kPiece = D / 8;
+    // a thread's pieces of a tile: an eighth of a row of K, and of V, with their scales, of one row or two
+    constexpr int kPiece = D / 8, kEach = kChWaves / WAVES, kApart = 8 * WAVES;
     const int prow = (wave * 64 + lane) >> 3, piece = lane & 7;
-    u32x4 kc{}, vc{};
-    uint32_t k_scale = 0, v_scale = 0;
+    u32x4 kc[kEach], vc[kEach];
+    uint32_t k_scale[kEach], v_scale[kEach];
     auto fetch = [&](int t) {
       const size_t row = chunk_tile<1>(c, unit, t, page);
       if (c.block_table) page = chunk_page(c, unit, t + kRound);
       const int rows = n - t < kChTile ? n - t : kChTile;  // (rows past the cache's end: zeros)
       const RowBuffer kb = row_buffer<D / 2>(c.K + row * (D / 2), rows), vb = row_buffer<D / 2>(c.V + row * (D / 2), rows);
       const RowBuffer ks = scale_buffer<D>(c.K_scale + row * (D / kCodeBlock), rows), vs = scale_buffer<D>(c.V_scale + row * (D / kCodeBlock), rows);
-      const int at = prow * D + piece * kPiece, s_at = at / kCodeBlock;
-      if constexpr (D == 128) {
-        kc = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(kb, at, 0, 0));
-        vc = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(vb, at, 0, 0));
-      } else {
-        const uint2 k2 = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(kb, at, 0, 0)), v2 = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(vb, at, 0, 0));
-        kc[0] = k2.x;
-        kc[1] = k2.y;
-        vc[0] = v2.x;
-        vc[1] = v2.y;
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) {
+        const int at = (prow + e * kApart) * D + piece * kPiece, s_at = at / kCodeBlock;
+        if constexpr (D == 128) {
+          kc[e] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(kb, at, 0, 0));
+          vc[e] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(vb, at, 0, 0));
+        } else {
+          const uint2 k2 = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(kb, at, 0, 0)), v2 = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(vb, at, 0, 0));
+          kc[e] = u32x4{k2.x, k2.y, 0, 0};
+          vc[e] = u32x4{v2.x, v2.y, 0, 0};
+        }
+        k_scale[e] = __builtin_amdgcn_raw_buffer_load_b8(ks, s_at, 0, 0);
+        v_scale[e] = __builtin_amdgcn_raw_buffer_load_b8(vs, s_at, 0, 0);
       }
-      k_scale = __builtin_amdgcn_raw_buffer_load_b8(ks, s_at, 0, 0);
-      v_scale = __builtin_amdgcn_raw_buffer_load_b8(vs, s_at, 0, 0);
     };
     char *const mine = sm + group * kGroupLds;
     auto put = [&](int place) {
-      u32x4 lo, hi;
-      decode16<CODE>(kc, k_scale, lo, hi);  // (head_dim 64: the first eight)
-      *reinterpret_cast<u32x4 *>(mine + place + chunk_lds<D>(prow, D == 128 ? 2 * piece : piece)) = lo;
-      if (D == 128) *reinterpret_cast<u32x4 *>(mine + place + chunk_lds<D>(prow, 2 * piece + 1)) = hi;
-      decode16<CODE>(vc, v_scale, lo, hi);
-      *reinterpret_cast<u32x4 *>(mine + place + Lds::kTileBytes + chunk_lds_v<D>(prow, D == 128 ? 2 * piece : piece)) = lo;
-      if (D == 128) *reinterpret_cast<u32x4 *>(mine + place + Lds::kTileBytes + chunk_lds_v<D>(prow, 2 * piece + 1)) = hi;
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) {
+        const int to = prow + e * kApart;
+        u32x4 lo, hi;
+        decode16<CODE>(kc[e], k_scale[e], lo, hi);  // (head_dim 64: the first eight)
+        *reinterpret_cast<u32x4 *>(mine + place + chunk_lds<D>(to, D == 128 ? 2 * piece : piece)) = lo;
+        if (D == 128) *reinterpret_cast<u32x4 *>(mine + place + chunk_lds<D>(to, 2 * piece + 1)) = hi;
+        decode16<CODE>(vc[e], v_scale[e], lo, hi);
+        *reinterpret_cast<u32x4 *>(mine + place + Lds::kTileBytes + chunk_lds_v<D>(to, D == 128 ? 2 * piece : piece)) = lo;
+        if (D == 128) *reinterpret_cast<u32x4 *>(mine + place + Lds::kTileBytes + chunk_lds_v<D>(to, 2 * piece + 1)) = hi;
+      }
     };
     // One tile out of its place; the next one goes to the other place, which every wave has left before the barrier.
     auto tile = [&](int t, auto PLACE, auto FIRST) {
@@ -671,7 +683,7 @@ __device__ __forceinline__ void chunk_attend_rows(const ChunkAttendParams &p) {
   }
 
   if (APPEND && split == 0) {  // the tokens whose first row is one of this workgroup's
-    const int first = (blk * kChRows + c.G - 1) / c.G, last = (blk * kChRows + kChRows + c.G - 1) / c.G;
+    const int first = (blk * kRows + c.G - 1) / c.G, last = (blk * kRows + kRows + c.G - 1) / c.G;
     chunk_copy_head<D>(c, p.k_new, p.v_new, p.s_new, p.T, p.question, b, h, base, first, last < m ? last : m, c.next_pos[b] - m, tid, kChThreads);
   }
 
@@ -679,9 +691,9 @@ __device__ __forceinline__ void chunk_attend_rows(const ChunkAttendParams &p) {
   __syncthreads();
   float sum = l + __shfl_xor(l, 32);
   if (GROUPS > 1) {  // the other groups', one after the other and lane by lane, through what the first does not use for its outputs
-    __shared__ float sm_stats[2][kChWaves][64];
-    static_assert(GROUPS == 1 || (kChWaves * 32 * 2 * D + kChWaves * 64 * 2 * D <= GROUPS * kGroupLds && !APPEND && !SHAPED), "room for a group's outputs");
-    f32x4 *const theirs = reinterpret_cast<f32x4 *>(sm + kChWaves * 32 * 2 * D + wave * (64 * 2 * D)) + lane;
+    __shared__ float sm_stats[2][WAVES][64];
+    static_assert(GROUPS == 1 || (WAVES * 32 * 2 * D + WAVES * 64 * 2 * D <= GROUPS * kGroupLds && !APPEND && !SHAPED), "room for a group's outputs");
+    f32x4 *const theirs = reinterpret_cast<f32x4 *>(sm + WAVES * 32 * 2 * D + wave * (64 * 2 * D)) + lane;
 #pragma unroll
     for (int g = 1; g < GROUPS; ++g) {
       if (g > 1) __syncthreads();
@@ -765,6 +777,15 @@ constexpr int kGroups = 3;
 template <int D, int MASK, int CODE>
 __global__ __launch_bounds__(kGroups * kChThreads, kGroups) void forms_attend_groups_kernel(const ChunkAttendParams p) {
   chunk_attend_rows<D, MASK, false, false, kGroups, CODE>(p);
+}
+// The same with half of the rows, for as few units as leave compute units idle otherwise: two waves a group, and groups as LDS has room for (sides by size
+// beside the rule that chooses; 16 tokens of 32 sequences, 28 heads on 4, 2464 slots, 142 MB: 41.6 us instead of 45.7).
+constexpr int kHalfWaves = 2, kHalfRows = 32 * kHalfWaves;
+template <int CODE>
+constexpr int kHalfGroups = CODE ? 4 : 3;
+template <int D, int MASK, int CODE>
+__global__ __launch_bounds__(kHalfGroups<CODE> * kHalfWaves * 64, 2) void forms_attend_half_kernel(const ChunkAttendParams p) {
+  chunk_attend_rows<D, MASK, false, false, kHalfGroups<CODE>, CODE, kHalfWaves>(p);
 }
 // Many rows on a cache of codes: 512 tokens of 16 sequences on 2656 slots, 32 heads on 8, e4m3, 377 us (with the codes unpacked before, 49 us of it, 391), 64 of 64 sequences
 // on 600 58 (102), 64 of 32 on 2464, 28 on 4, 94 (122).

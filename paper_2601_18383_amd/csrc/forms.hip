@@ -7,7 +7,7 @@
 
 namespace dynts {
 
-// (a cache that is not of codes comes with mask kTree)
+// (here and below: a cache that is not of codes comes with mask kTree)
 template <int D, int CODE>
 static void few_form(const ChunkAttendParams &p, int mask, unsigned grid, hipStream_t st) {
   auto *kernel = forms_attend_few_kernel<D, kTree, CODE>;
@@ -69,6 +69,25 @@ static void attend_groups(const ChunkAttendParams &p, int mask, unsigned grid, h
     if (mask == kPlain) kernel = forms_attend_groups_kernel<D, kPlain, CODE>;
   }
   hipLaunchKernelGGL(kernel, dim3(grid), dim3(kGroups * kChThreads), 0, st, p);
+}
+template <int D, int CODE>
+static void attend_half(const ChunkAttendParams &p, int mask, unsigned grid, hipStream_t st) {
+  auto *kernel = forms_attend_half_kernel<D, kTree, CODE>;
+  if constexpr (CODE != 0) {
+    if (mask == kPlain) kernel = forms_attend_half_kernel<D, kPlain, CODE>;
+  }
+  hipLaunchKernelGGL(kernel, dim3(grid), dim3(kHalfGroups<CODE> * kHalfWaves * 64), 0, st, p);
+}
+void launch_attend_half(const ChunkAttendParams &p, int mask, unsigned grid, hipStream_t st) {
+  if (p.c.D == 128) {
+    if (p.c.code == DYNTS_CODE_E4M3) attend_half<128, DYNTS_CODE_E4M3>(p, mask, grid, st);
+    else if (p.c.code == DYNTS_CODE_INT8) attend_half<128, DYNTS_CODE_INT8>(p, mask, grid, st);
+    else attend_half<128, 0>(p, mask, grid, st);
+  } else {
+    if (p.c.code == DYNTS_CODE_E4M3) attend_half<64, DYNTS_CODE_E4M3>(p, mask, grid, st);
+    else if (p.c.code == DYNTS_CODE_INT8) attend_half<64, DYNTS_CODE_INT8>(p, mask, grid, st);
+    else attend_half<64, 0>(p, mask, grid, st);
+  }
 }
 void launch_attend_groups(const ChunkAttendParams &p, int mask, unsigned grid, hipStream_t st) {
   if (p.c.D == 128) {

@@ -16,8 +16,9 @@ __attribute__((visibility("hidden"))) void launch_coded_attend(const ChunkAttend
 // up to kTokRows rows on a cache of codes
 __attribute__((visibility("hidden"))) void launch_coded_token(const ChunkAttendParams &p, bool shaped, unsigned grid, hipStream_t st);
 __attribute__((visibility("hidden"))) void launch_coded_token_scores(const ChunkScoreParams &p, bool shaped, unsigned grid, hipStream_t st);
-// many rows: a draft's tokens; kGroups groups of waves, with mask kPlain or kTree
+// many rows: a draft's tokens; groups of waves, with mask kPlain (caches of codes) or kTree, for kChRows rows a workgroup, or kHalfRows (unsplit)
 __attribute__((visibility("hidden"))) void launch_tree_attend(const ChunkAttendParams &p, unsigned grid, hipStream_t st);
+__attribute__((visibility("hidden"))) void launch_attend_half(const ChunkAttendParams &p, int mask, unsigned grid, hipStream_t st);
 __attribute__((visibility("hidden"))) void launch_attend_groups(const ChunkAttendParams &p, int mask, unsigned grid, hipStream_t st);
 // the shares of either together, more than four
 __attribute__((visibility("hidden"))) void launch_merge_form(const ChunkAttendParams &p, int block_rows, hipStream_t st);

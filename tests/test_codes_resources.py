@@ -35,3 +35,8 @@ def test_scores_keep_three_workgroups_a_compute_unit(kernels):  # noqa: F811
         assert k["vgpr_count"] <= 168 and k["vgpr_spill_count"] <= 2 and 3 * k["group_segment_fixed_size"] <= LDS, name
     for name, k in _named(kernels, r"coded_scores_few_kernelILi(64|128)E", 12).items():
         assert k["vgpr_count"] <= 256 and k["vgpr_spill_count"] == 0, name
+
+
+def test_half_of_the_rows_keep_two_waves_a_vector_unit(kernels):  # noqa: F811
+    for name, k in _named(kernels, r"forms_attend_half_kernel", 10).items():
+        assert k["vgpr_count"] <= 256 and k["vgpr_spill_count"] == 0 and k["group_segment_fixed_size"] <= LDS, name
