@@ -434,7 +434,7 @@ int dynts_read_rows(dynts_ctx *ctx, int32_t layer, const int32_t *first, int32_t
  *   n_tokens: tokens of the largest draft, 1 <= n_tokens <= 4096; n_new int32 [Nb] or NULL as for chunks, the rest of the arrays is padding.
  *   seen uint32 [Nb][n_tokens][ceil(n_tokens / 32)]: bit j % 32 of word j / 32 of token i says that it sees token j of the draft.  What
  *     dynts_tree_build writes, or any other pattern; bits of tokens behind the sequence's last count as 0.
- * Arrays that are written overlap no other argument. */
+ * Arrays that are written overlap no other argument.  Rows of V that a token of the draft does not see have to be finite, rows of K need not. */
 
 /* seen, and depth int32 [Nb][n_tokens] (0 for a token whose parent is the cache; may be NULL), from parents int32 [Nb][n_tokens]: the draft's
  * token before it that a token follows, or -1, the cache (as does any number that is not of a token before it).  Padding gets zeros. */

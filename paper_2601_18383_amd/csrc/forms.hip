@@ -222,6 +222,8 @@ int dynts_tree_keep(dynts_ctx *ctx, int32_t layer, int32_t n_tokens, const int32
   if (!seen || !leaf || !n_kept || (q_kept && !q) || (lse_kept && !lse)) return DYNTS_ENULL;
   if (n_tokens <= 0 || n_tokens > dynts::kTreeMost) return DYNTS_EINVAL;
   if (misaligned(q, 16) || misaligned(q_kept, 16) || misaligned(lse, 4) || misaligned(lse_kept, 4) || misaligned(seen, 4)) return DYNTS_EINVAL;
+  const size_t each = (size_t)c.Nb * 4;  // (other workgroups read leaf and n_taken while n_kept is written)
+  if (overlap(n_kept, each, leaf, each) || (n_taken && overlap(n_kept, each, n_taken, each))) return DYNTS_EINVAL;
   const size_t rows = (size_t)c.Nb * n_tokens * c.Hq;
   if ((q_kept && overlap(q_kept, rows * c.D * 2, q, rows * c.D * 2)) || (lse_kept && overlap(lse_kept, rows * 4, lse, rows * 4))) return DYNTS_EINVAL;
   const dynts::TreeKeepParams p{c, seen, leaf, n_taken, n_kept, q, lse, q_kept, lse_kept, n_tokens, (n_tokens + 31) / 32};

@@ -149,7 +149,7 @@ def test_draft_refusals(B, coded):
     T = 16
     need = B.dynts_codes_scratch_bytes(cfg, T)
     base = dict(ctx=ctx, layer=0, q=ONE, T=T, n=None, seen=ONE, out=FAR, lse=None, scratch=ONE, size=need, k=ONE, v=ONE, s=None, taken=ONE, leaf=ONE,
-                kept=ONE, q_kept=None, lse_kept=None)
+                kept=C.c_void_p(512), q_kept=None, lse_kept=None)
 
     def attend(**kw):
         x = dict(base, **kw)
@@ -181,6 +181,7 @@ def test_draft_refusals(B, coded):
     assert keep(q_kept=FAR, q=None) == B.DYNTS_ENULL and keep(lse_kept=FAR, lse=None) == B.DYNTS_ENULL
     assert keep(q_kept=ONE) == B.DYNTS_EINVAL and keep(lse_kept=ONE, lse=ONE) == B.DYNTS_EINVAL
     assert keep(q_kept=C.c_void_p((1 << 40) + 8)) == B.DYNTS_EINVAL
+    assert keep(kept=ONE) == B.DYNTS_EINVAL and keep(leaf=FAR, n=ONE, kept=C.c_void_p(264)) == B.DYNTS_EINVAL  # over leaf, over n_taken
     B.dynts_destroy(ctx)
     ctx = B.dynts_create(cfg)
     assert attend(ctx=ctx) == B.DYNTS_ENOTBOUND and step(ctx=ctx) == B.DYNTS_ENOTBOUND and keep(ctx=ctx) == B.DYNTS_ENOTBOUND
