@@ -167,7 +167,7 @@ __global__ __launch_bounds__(kAppendThreads) void chunk_copy_kernel(const ChunkA
   chunk_copy<D, 0, 1>(p, b, p.c.seq_len[b] - m, m, p.c.next_pos[b] - m, blockIdx.x * kAppendThreads + threadIdx.x, gridDim.x * kAppendThreads);
 }
 // The same for a cache of codes, a workgroup for kCodedTokens neighbouring tokens of one head: scales, scores and positions of 32 rows share a line, and are to leave
-// from one L2 (token by token over the heads, as above, 512 of 64 sequences, 8 heads of 128, 54 us instead of 43: 203 MB read and written).
+// from one L2 (token by token over the heads, as above, 512 of 64 sequences, 8 heads of 128, 54 us instead of 43, on other arrays in turn).
 // grid (ceil(T / kCodedTokens) * Hkv, Nb).
 template <int D>
 constexpr int kCodedTokens = kAppendAtOnce * kAppendThreads / (D / 8);

@@ -271,7 +271,7 @@ __global__ __launch_bounds__(WAVES * 64, MASK == kShaped && D == 128 ? 2 : 4) vo
 }
 
 // The weight that slots receive from up to 16 rows: 64 of them a wave, all asked for at once, rows in the registers of the quads.  grid as chunk_scores_kernel's:
-// ceil(cap / 256) workgroups a unit.
+// ceil(cap / 256) workgroups a unit.  Bound by HBM: 512 units of 2657 slots, 180 MB, 32 us, 5.6 TB/s.
 constexpr int kTsWaves = 4, kTsKeys = 64 * kTsWaves;
 template <int D, bool SHAPED, int CODE>
 __global__ __launch_bounds__(kTsWaves * 64) void coded_token_scores_kernel(const ChunkScoreParams p) {

@@ -27,7 +27,7 @@ __device__ __forceinline__ uint32_t code_scale(uint32_t most) {  // most: the la
 }
 
 // Eight neighbouring elements, x, to `codes + at`, and their block's scale, by four neighbouring lanes that have a block between them; piece: which eighth of
-// elements of the row.
+// elements of the row.  (512 tokens of 64 sequences, 8 heads of 128, 203 MB read and written: 37 us, 5.5 TB/s; a large copy reaches 5.1.)
 template <int CODE>
 __device__ __forceinline__ void encode8(u32x4 x, uint8_t *codes, uint8_t *scales, size_t at, int piece) {
   uint32_t most = 0;
@@ -147,7 +147,8 @@ struct ReadParams {
 constexpr int kReadThreads = 256;
 
 // Slots first[b] + i of every unit to row i, those that the sequence has; a copy, bound by HBM.  grid (ceil(n_rows * D / 8 / 256 / 2), Hkv, Nb), eight elements of
-// K and V a thread, so that a wave's stores are whole lines, and twice.
+// K and V a thread, so that a wave's stores are whole lines, and twice.  PAST: stores go past the caches, for a reader that comes later.  (1900 rows of 128 units, 189 MB: 28 us,
+// 6.7 TB/s, part of it from the memory-side cache; before a long chunk, 2764 rows of them, 274 MB, 44 us.)
 constexpr int kReadAtOnce = 2;
 template <int D, int CODE, bool PAST>
 __global__ __launch_bounds__(kReadThreads) void read_rows_kernel(const ReadParams p) {
@@ -208,7 +209,8 @@ __global__ __launch_bounds__(kReadThreads) void read_rows_kernel(const ReadParam
 }
 
 // ---- eviction: as compact_kernel, rows of D bytes and their scales --------------------------------------------------------
-// grid (6, Hkv, Nb): K's codes, V's, K's scales, V's, S, pos.  PAGED leaves seq_len to paged_trim_kernel.
+// grid (6, Hkv, Nb): K's codes, V's, K's scales, V's, S, pos.  PAGED leaves seq_len to paged_trim_kernel.  Bound by HBM: 128 units, 1920 of 2432 rows kept, 130 MB, 22.5 us
+// (compact_kernel on the same rows in bf16 46).
 template <int D, bool PAGED, int THREADS>
 __global__ __launch_bounds__(THREADS) void coded_compact_kernel(const CompactParams p, const ChunkCache c) {
   const int tid = threadIdx.x, what = blockIdx.x, h = blockIdx.y, b = blockIdx.z;

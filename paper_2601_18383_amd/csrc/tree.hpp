@@ -21,7 +21,8 @@ struct TreeBuildParams {
 };
 
 // A token's ancestors and itself as bits: seen_i = {i} + seen_parent(i), followed upwards from every token by a thread of its own (parents lie before their
-// children, so a token's words are complete from the last to the first).  grid (ceil(T / 256), Nb), LDS for T words.
+// children, so a token's words are complete from the last to the first).  grid (ceil(T / 256), Nb), LDS for T words.  Once a draft, for all layers: 3.0 us for 16 tokens of
+// 32 sequences, which is a launch; a chain of T tokens is T steps of its last thread.
 __global__ __launch_bounds__(kTreeThreads) void tree_build_kernel(const TreeBuildParams p) {
   extern __shared__ int32_t sm_parent[];
   const int b = blockIdx.y, tid = threadIdx.x;
@@ -90,7 +91,8 @@ __device__ __forceinline__ int tree_path(const TreeKeepParams &p, int b, int m, 
 
 // grid (1 + gathering workgroups, Nb).  Workgroup 0 of a sequence moves its rows: destinations in ascending order, a batch's sources read before its
 // destinations are written; a kept token's source lies at or behind its destination, so no later batch's source is overwritten (as in compact_kernel).
-// Positions stay: the slot of the k-th kept token had the k-th position already.  The others gather q and lse.
+// Positions stay: the slot of the k-th kept token had the k-th position already.  The others gather q and lse.  Bound by the chain leaf, words, rows: 5.2 us for 16 tokens of
+// 32 sequences, 4 heads of 128, any of them the last that stays.
 template <int D>
 __global__ __launch_bounds__(kKeepThreads) void tree_keep_kernel(const TreeKeepParams p) {
   const ChunkCache &c = p.c;
