@@ -71,7 +71,8 @@ constexpr long long kMostPartials = 65536;
 // Groups of waves (drafts, chunks on codes): one workgroup a compute unit, and no two shares of many units, which are bound by HBM, before the slots pay for
 // the joint.  us by the number of shares: W = 128, 32 units of 2500 slots 1 / 2: 39.1 / 35.1, 128 units 44.2 / 47.0, 64 units of 4500 71.4 / 55.2; W = 16, 8 units of
 // 16400 8 / 16 / 32: 40.3 / 33.9 / 47.1; W = 64, 64 units of 9000 2 / 4 / 8: 81.7 / 70.1 / 83.6.
-// Where they have no shares and half as many rows a workgroup, H of them, still have a compute unit each: half.  us, 128 rows / 64 (bf16 | e4m3 | whole numbers):
+// Where they have no shares and half as many rows a workgroup, H of them, still have a compute unit each: half.  us, 128 rows / 64 (bf16 | e4m3 | whole numbers; on codes
+// measured with one barrier for all groups: 64 rows have become up to 5 us faster since, 128 up to 2):
 //   head_dim 128, 500 slots: 64 units R = 256 17.2 / 14.6 | 18.5 / 15.8 | 19.6 / 16.7, 128 of R = 128 16.1 / 14.6 | 18.0 / 15.2 | 18.9 / 16.0, 256 of R = 64 18.7 / 17.1 | 18.0 / 16.2 |
 //     19.2 / 16.9; 2464 slots: 128 of R = 112 45.7 / 41.6 | 47.1 / 42.4 | 51.4 / 45.8, 256 of R = 64 63.5 / 61.1 | 56.1 / 50.1 | 61.4 / 52.3, H = 512 53.3 / 56.9 | 55.9 / 56.8 | 61.9 / 61.0
 //   head_dim 64, 2464 slots: 128 of R = 128 27.8 / 25.1 | 35.4 / 29.1 | 37.1 / 30.9
