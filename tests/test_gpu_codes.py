@@ -228,6 +228,23 @@ def test_attend_and_scores(B, layout, code, Hq, Hkv, d, n_old, n_new):
     Case(B, layout, code, Hq, Hkv, d, n_old, n_new, gaps=50).run().check()
 
 
+MANY = [  # as many units as it takes for workgroups of 64 and of 128 rows, in groups of waves and not, and for codes that are unpacked beforehand
+    (16, 8, 128, [0, 1, 31, 32, 33, 63, 64, 65, 96, 97] * 2, [30, 30, 1, 29, 0, 17, 32, 30, 16, 30] * 2),
+    (28, 4, 128, [0, 300, 64, 95] * 4, [30, 30, 11, 0] * 4),
+    (16, 8, 64, [2100, 0, 1, 130] * 4, [64, 64, 33, 5] * 4),
+    (16, 8, 64, [0, 33, 64, 190] * 2, [150, 149, 64, 1] * 2),
+    (20, 10, 128, [0, 31, 64, 129] * 4, [130, 64, 129, 3] * 4),
+    (16, 4, 64, [90, 0, 1, 33], [700, 650, 1, 129]),
+]
+
+
+@pytest.mark.parametrize("layout", LAYOUTS)
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("Hq,Hkv,d,n_old,n_new", MANY)
+def test_many_rows_of_many_units(B, layout, code, Hq, Hkv, d, n_old, n_new):
+    Case(B, layout, code, Hq, Hkv, d, n_old, n_new, gaps=20, seed=5).run().check()
+
+
 def _shapings(c, kind):
     Nb = len(c.n_old)
     own = torch.stack([c.pos[b][0, c.n_old[b]:][:1].expand(1) if c.n_new[b] else torch.zeros(1, dtype=torch.int32) for b in range(Nb)]) + torch.arange(c.T)

@@ -173,6 +173,21 @@ def test_attend(B, kind, Hq, Hkv, d, n_old, n_new):
     assert int(x.c.status.item()) == 0
 
 
+MANY = [  # as many units as it takes for workgroups of 64 and of 128 rows, in groups of waves and not
+    (16, 8, 128, [0, 1, 31, 32, 33, 63, 64, 65, 96, 97] * 2, [30, 30, 1, 29, 0, 17, 32, 30, 16, 30] * 2),
+    (28, 4, 128, [0, 300, 64, 95] * 4, [30, 30, 11, 0] * 4),
+    (16, 8, 64, [2100, 0, 1, 130] * 4, [64, 64, 33, 5] * 4),
+    (16, 8, 64, [0, 33, 64, 190] * 2, [150, 149, 64, 1] * 2),
+    (20, 10, 128, [0, 31, 64, 129] * 4, [130, 64, 129, 3] * 4),
+]
+
+
+@pytest.mark.parametrize("kind", ["dense", "paged", "e4m3", "int8_paged"])
+@pytest.mark.parametrize("Hq,Hkv,d,n_old,n_new", MANY)
+def test_attend_many_units(B, kind, Hq, Hkv, d, n_old, n_new):
+    Draft(B, kind, Hq, Hkv, d, n_old, n_new, how="deep" if d == 64 else "any", seed=7).attend().check()
+
+
 @pytest.mark.parametrize("kind", ["dense", "int8_paged"])
 @pytest.mark.parametrize("how", ["flat", "deep"])
 @pytest.mark.parametrize("Hq,Hkv,d,n_old,n_new", [SHAPES[1], SHAPES[5], SHAPES[7], SHAPES[8]])
