@@ -269,13 +269,12 @@ void launch_attend_d(const dynts::ChunkAttendParams &p, const ChunkPlan &pl, uns
   else if (SHAPED && p.shape.slope) hipLaunchKernelGGL((dynts::chunk_attend_kernel<D, SHAPED, SHAPED, false>), dim3(grid), dim3(dynts::kChThreads), 0, st, p);
   else if (!SHAPED && p.k_new) hipLaunchKernelGGL((dynts::chunk_attend_kernel<D, false, false, !SHAPED>), dim3(grid), dim3(dynts::kChThreads), 0, st, p);
   else hipLaunchKernelGGL((dynts::chunk_attend_kernel<D, SHAPED, false, false>), dim3(grid), dim3(dynts::kChThreads), 0, st, p);
-  if (p.n_split > 1) {
+  if (p.n_split > 1 && (p.seen || p.c.code)) {
+    dynts::launch_merge_form(p, pl.rows, st);
+  } else if (p.n_split > 1) {
     constexpr int rows = dynts::kMergeThreads / (D / 8);
-    const dim3 merge((p.T * p.c.G + rows - 1) / rows, p.c.Nb * p.c.Hkv), threads(dynts::kMergeThreads);
-    if (p.n_split > 4 && (p.seen || p.c.code)) dynts::launch_merge_form(p, pl.rows, st);
-    else if (p.n_split > 4) hipLaunchKernelGGL((dynts::chunk_merge_kernel<D, 16>), merge, threads, 0, st, p, pl.rows);
-    else if (p.n_split > 2) hipLaunchKernelGGL((dynts::chunk_merge_kernel<D, 4>), merge, threads, 0, st, p, pl.rows);
-    else hipLaunchKernelGGL((dynts::chunk_merge_kernel<D, 2>), merge, threads, 0, st, p, pl.rows);
+    hipLaunchKernelGGL(dynts::chunk_merge_kernel<D>, dim3((p.T * p.c.G + rows - 1) / rows, p.c.Nb * p.c.Hkv), dim3(dynts::kMergeThreads), 0, st, p,
+                       pl.rows);
   }
 }
 

@@ -1107,37 +1107,32 @@ __global__ __launch_bounds__(kFewThreads, D == 64 && MASK != kShaped ? 4 : 2) vo
   chunk_attend_few<D, MASK, CODE>(p);
 }
 
-// The shares of a row together.  grid (ceil(T * G / kMergeRows), units), D / 8 threads a row.  AT_ONCE: shares that are asked for at a time, the first ones
-// before it is known how many there are (with four, and their number first, 16 shares of 8 units take 2 us longer).
+// The shares of a row together.  grid (ceil(T * G / kMergeRows), units), D / 8 threads a row.
 constexpr int kMergeThreads = 256;
-template <int D, int AT_ONCE>
+template <int D>
 __global__ __launch_bounds__(kMergeThreads) void chunk_merge_kernel(const ChunkAttendParams p, int block_rows) {
   const ChunkCache &c = p.c;
   const int unit = blockIdx.y, b = unit / c.Hkv, h = unit - b * c.Hkv;
+  int n;
+  const int m = chunk_tokens(c, p.n_new, p.T, b, n);
   const int r = blockIdx.x * (kMergeThreads / (D / 8)) + threadIdx.x / (D / 8), d0 = 8 * (threadIdx.x % (D / 8));
-  if (r >= p.T * c.G) return;
+  if (r >= m * c.G) return;
+  const int shares = p.part_n[unit * (p.Rpad / block_rows) + r / block_rows];
+  if (shares == 1) return;
   const size_t first = (size_t)unit * p.n_split * p.Rpad + r;
-  float2 ml[AT_ONCE];
-  f32x4 a[AT_ONCE], z[AT_ONCE];
-  auto fetch = [&](int s0) {
+  float top = -INFINITY, sum = 0.f, o[8] = {};
+  for (int s0 = 0; s0 < shares; s0 += 4) {  // four shares' loads at a time
+    float2 ml[4];
+    f32x4 a[4], z[4];
 #pragma unroll
-    for (int s = 0; s < AT_ONCE; ++s) {
-      const size_t prow = first + (size_t)(s0 + s < p.n_split ? s0 + s : s0) * p.Rpad;
+    for (int s = 0; s < 4; ++s) {
+      const size_t prow = first + (size_t)(s0 + s < shares ? s0 + s : s0) * p.Rpad;
       ml[s] = *reinterpret_cast<const float2 *>(p.part_ml + 2 * prow);
       a[s] = *reinterpret_cast<const f32x4 *>(p.part_o + prow * D + d0);
       z[s] = *reinterpret_cast<const f32x4 *>(p.part_o + prow * D + d0 + 4);
     }
-  };
-  fetch(0);
-  const int shares = p.part_n[unit * (p.Rpad / block_rows) + r / block_rows];
-  int n;
-  const int m = chunk_tokens(c, p.n_new, p.T, b, n);
-  if (r >= m * c.G || shares == 1) return;
-  float top = -INFINITY, sum = 0.f, o[8] = {};
-  for (int s0 = 0; s0 < shares; s0 += AT_ONCE) {
-    if (s0 > 0) fetch(s0);
 #pragma unroll
-    for (int s = 0; s < AT_ONCE; ++s) {
+    for (int s = 0; s < 4; ++s) {
       if (s0 + s >= shares || !(ml[s].y > 0.f)) continue;  // (a share without a key that the row sees)
       const float next = fmaxf(top, ml[s].x), f = fast_exp2(top - next), w = fast_exp2(ml[s].x - next);
       top = next;
@@ -1153,9 +1148,46 @@ __global__ __launch_bounds__(kMergeThreads) void chunk_merge_kernel(const ChunkA
   chunk_write<D>(p, ((size_t)b * p.T + i) * c.Hq + (size_t)h * c.G + (r - i * c.G), d0, o, top, sum);
 }
 
-// The same for more than four shares of drafts and of caches of codes: a wave a row, its lanes share out the shares as well, all of them asked for at once.
-// (Whole calls, with this one / with the one above: single tokens of 8 units of 16400 slots, 32 shares, 14.5 / 16.9 us; 256 rows of them, 16 shares, 33.3 / 34.1; of 128 units of
-// 2464 slots, two shares, 20.1 / 19.6.)
+// The same for up to four shares of drafts and of caches of codes: all are asked for at once, before it is known how many there are.
+template <int D>
+__global__ __launch_bounds__(kMergeThreads) void forms_merge_few_kernel(const ChunkAttendParams p, int block_rows) {
+  const ChunkCache &c = p.c;
+  const int unit = blockIdx.y, b = unit / c.Hkv, h = unit - b * c.Hkv;
+  const int r = blockIdx.x * (kMergeThreads / (D / 8)) + threadIdx.x / (D / 8), d0 = 8 * (threadIdx.x % (D / 8));
+  if (r >= p.T * c.G) return;
+  float2 ml[4];
+  f32x4 a[4], z[4];
+#pragma unroll
+  for (int s = 0; s < 4; ++s) {
+    const size_t prow = ((size_t)unit * p.n_split + (s < p.n_split ? s : 0)) * p.Rpad + r;
+    ml[s] = *reinterpret_cast<const float2 *>(p.part_ml + 2 * prow);
+    a[s] = *reinterpret_cast<const f32x4 *>(p.part_o + prow * D + d0);
+    z[s] = *reinterpret_cast<const f32x4 *>(p.part_o + prow * D + d0 + 4);
+  }
+  const int shares = p.part_n[unit * (p.Rpad / block_rows) + r / block_rows];
+  int n;
+  const int m = chunk_tokens(c, p.n_new, p.T, b, n);
+  if (r >= m * c.G || shares == 1) return;
+  float top = -INFINITY, sum = 0.f, o[8] = {};
+#pragma unroll
+  for (int s = 0; s < 4; ++s) {
+    if (s >= shares || !(ml[s].y > 0.f)) continue;  // (a share without a key that the row sees)
+    const float next = fmaxf(top, ml[s].x), f = fast_exp2(top - next), w = fast_exp2(ml[s].x - next);
+    top = next;
+    sum = sum * f + ml[s].y * w;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      o[j] = o[j] * f + a[s][j] * w;
+      o[4 + j] = o[4 + j] * f + z[s][j] * w;
+    }
+  }
+  const int i = chunk_token(r, p.g_magic);
+  chunk_write<D>(p, ((size_t)b * p.T + i) * c.Hq + (size_t)h * c.G + (r - i * c.G), d0, o, top, sum);
+}
+
+// And for more than four: a wave a row, its lanes share out the shares as well, all of them asked for at once.
+// (Whole calls, with this one / with threads that take 16 shares at a time: single tokens of 8 units of 16400 slots, 32 shares, 14.5 / 16.9 us; 256 rows of them, 16 shares, 33.3 / 34.1; of 128 units of
+// 2464 slots, two shares, with this one / with the one above 20.1 / 19.6.)
 constexpr int kMergeMost = 32;  // shares
 template <int D>
 __global__ __launch_bounds__(kMergeThreads) void forms_merge_kernel(const ChunkAttendParams p, int block_rows) {

@@ -100,10 +100,16 @@ void launch_attend_groups(const ChunkAttendParams &p, int mask, unsigned grid, h
     else attend_groups<64, 0>(p, mask, grid, st);
   }
 }
+template <int D>
+static void merge_form(const ChunkAttendParams &p, int block_rows, hipStream_t st) {
+  const int rows = p.n_split > 4 ? kMergeThreads / 64 : kMergeThreads / (D / 8);
+  const dim3 grid((p.T * p.c.G + rows - 1) / rows, p.c.Nb * p.c.Hkv), block(kMergeThreads);
+  if (p.n_split > 4) hipLaunchKernelGGL(forms_merge_kernel<D>, grid, block, 0, st, p, block_rows);
+  else hipLaunchKernelGGL(forms_merge_few_kernel<D>, grid, block, 0, st, p, block_rows);
+}
 void launch_merge_form(const ChunkAttendParams &p, int block_rows, hipStream_t st) {
-  const dim3 grid((p.T * p.c.G + kMergeThreads / 64 - 1) / (kMergeThreads / 64), p.c.Nb * p.c.Hkv), block(kMergeThreads);
-  if (p.c.D == 128) hipLaunchKernelGGL((forms_merge_kernel<128>), grid, block, 0, st, p, block_rows);
-  else hipLaunchKernelGGL((forms_merge_kernel<64>), grid, block, 0, st, p, block_rows);
+  if (p.c.D == 128) merge_form<128>(p, block_rows, st);
+  else merge_form<64>(p, block_rows, st);
 }
 template <int D, int CODE>
 static void coded_attend(const ChunkAttendParams &p, int mask, unsigned grid, hipStream_t st) {

@@ -20,7 +20,7 @@ __attribute__((visibility("hidden"))) void launch_coded_token_scores(const Chunk
 __attribute__((visibility("hidden"))) void launch_tree_attend(const ChunkAttendParams &p, unsigned grid, hipStream_t st);
 __attribute__((visibility("hidden"))) void launch_attend_half(const ChunkAttendParams &p, int mask, unsigned grid, hipStream_t st);
 __attribute__((visibility("hidden"))) void launch_attend_groups(const ChunkAttendParams &p, int mask, unsigned grid, hipStream_t st);
-// the shares of either together, more than four
+// the shares of a draft's rows, or of rows on a cache of codes, together
 __attribute__((visibility("hidden"))) void launch_merge_form(const ChunkAttendParams &p, int block_rows, hipStream_t st);
 __attribute__((visibility("hidden"))) void launch_coded_scores(const ChunkScoreParams &p, bool few, bool shaped, bool biased, unsigned grid, hipStream_t st);
 // small: one launch that makes room and writes; else one (behind chunk_reserve_kernel) that writes
