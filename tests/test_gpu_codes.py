@@ -245,6 +245,14 @@ def test_many_rows_of_many_units(B, layout, code, Hq, Hkv, d, n_old, n_new):
     Case(B, layout, code, Hq, Hkv, d, n_old, n_new, gaps=20, seed=5).run().check()
 
 
+@pytest.mark.parametrize("layout", LAYOUTS)
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("Hq,Hkv,d,n_old,n_new", [(8, 1, 128, [2100, 10, 700], [2, 1, 0]), (8, 2, 64, [1700, 3], [1, 1]), (8, 1, 128, [2100, 10], [20, 4]),
+                                                  (8, 1, 64, [1, 1600], [3, 9]), (16, 1, 128, [1600, 50, 0, 1], [131, 130, 131, 1])])
+def test_two_to_four_shares(B, layout, code, Hq, Hkv, d, n_old, n_new):
+    Case(B, layout, code, Hq, Hkv, d, n_old, n_new, gaps=20, seed=6).run().check()
+
+
 def _shapings(c, kind):
     Nb = len(c.n_old)
     own = torch.stack([c.pos[b][0, c.n_old[b]:][:1].expand(1) if c.n_new[b] else torch.zeros(1, dtype=torch.int32) for b in range(Nb)]) + torch.arange(c.T)

@@ -188,6 +188,13 @@ def test_attend_many_units(B, kind, Hq, Hkv, d, n_old, n_new):
     Draft(B, kind, Hq, Hkv, d, n_old, n_new, how="deep" if d == 64 else "any", seed=7).attend().check()
 
 
+@pytest.mark.parametrize("kind", ["dense", "paged", "e4m3", "int8_paged"])
+@pytest.mark.parametrize("Hq,Hkv,d,n_old,n_new", [(8, 1, 128, [2100, 10, 700], [2, 1, 0]), (8, 1, 128, [2100, 10], [20, 4]), (8, 1, 64, [1, 1600], [3, 9]),
+                                                  (16, 1, 128, [1600, 50, 0, 1], [131, 130, 131, 1])])
+def test_attend_two_to_four_shares(B, kind, Hq, Hkv, d, n_old, n_new):
+    Draft(B, kind, Hq, Hkv, d, n_old, n_new, seed=8).attend().check()
+
+
 @pytest.mark.parametrize("kind", ["dense", "int8_paged"])
 @pytest.mark.parametrize("how", ["flat", "deep"])
 @pytest.mark.parametrize("Hq,Hkv,d,n_old,n_new", [SHAPES[1], SHAPES[5], SHAPES[7], SHAPES[8]])
