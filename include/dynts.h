@@ -367,7 +367,8 @@ int dynts_chunk_append(dynts_ctx *ctx, int32_t layer, const uint16_t *k_new, con
 /* Attention of the LAST n_new[b] tokens in the cache (at most seq_len[b]): token i of them sees the slots up to its own, or what
  * `shaping` (host struct of device pointers, or NULL) says.  q bf16 [Nb][n_tokens][Hq][d]; out bf16 [Nb][n_tokens][Hq][d];
  * lse fp32 [Nb][n_tokens][Hq] or NULL: log of the softmax denominators.  Reads the cache only; what dynts_update_scores owes is
- * not touched. */
+ * not touched.  A NaN in a row of K makes out and lse of the tokens and heads that see the row NaN, and so what the slots that they see receive
+ * (dynts_chunk_scores). */
 int dynts_chunk_attend(dynts_ctx *ctx, int32_t layer, const uint16_t *q, int32_t n_tokens, const int32_t *n_new,
                        const dynts_shaping *shaping, uint16_t *out, float *lse, void *scratch, size_t scratch_bytes,
                        void *stream);

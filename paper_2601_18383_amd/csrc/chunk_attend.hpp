@@ -249,13 +249,21 @@ __device__ __forceinline__ void soft_caps(f32x16 &x, float scale_log2, const Chu
   }
 }
 
+// Whether there is a key among those that went into a row's sum of weights: else it is 0, by its bits.  (`sum > 0` would take a NaN, of a key's logit, for no key:
+// in one share the key would be seen, in several its whole share be left out.  And the compiler, which takes floats never to be NaN, would make that of the bits' comparison.)
+__device__ __forceinline__ bool saw_keys(float sum) {
+  uint32_t bits = __float_as_uint(sum);
+  asm("" : "+v"(bits));
+  return bits != 0u;
+}
+
 // Eight neighbouring elements of an output row, and its lse, from their unnormalised values, shift and sum.
 template <int D>
 __device__ __forceinline__ void chunk_write(const ChunkAttendParams &p, size_t row, int d0, const float (&o)[8], float top, float sum) {
-  const float inv = sum > 0.f ? 1.f / sum : 0.f;  // (a row that sees nothing: zeros, and -inf)
+  const float inv = saw_keys(sum) ? 1.f / sum : 0.f;  // (a row that sees nothing: zeros, and -inf)
   store_u32x4(p.out + row * D + d0, u32x4{bf16_pack(o[0] * inv, o[1] * inv), bf16_pack(o[2] * inv, o[3] * inv), bf16_pack(o[4] * inv, o[5] * inv),
                                           bf16_pack(o[6] * inv, o[7] * inv)});
-  if (p.lse && d0 == 0) p.lse[row] = sum > 0.f ? (top + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f : -INFINITY;
+  if (p.lse && d0 == 0) p.lse[row] = saw_keys(sum) ? (top + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f : -INFINITY;
 }
 
 // ---- many rows: 32 of them a wave, four waves, which share the keys through LDS ----------------------------------------
@@ -755,7 +763,7 @@ __device__ __forceinline__ void chunk_attend_rows(const ChunkAttendParams &p) {
     if (hf == 0) *reinterpret_cast<float2 *>(p.part_ml + 2 * prow) = float2{-nm, sum};
     return;
   }
-  const float inv = sum > 0.f ? 1.f / sum : 0.f;  // (a row that sees nothing: zeros, and -inf)
+  const float inv = saw_keys(sum) ? 1.f / sum : 0.f;  // (a row that sees nothing: zeros, and -inf)
   char *const turn = sm + wave * (32 * 2 * D);
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt)
@@ -770,7 +778,7 @@ __device__ __forceinline__ void chunk_attend_rows(const ChunkAttendParams &p) {
     return (uint32_t)((ri - i0) * c.Hq + (rr - ri * c.G));
   };
   if (p.lse && hf == 0 && row0 + col < R)
-    (p.lse + first_row)[row_from(row0 + col)] = sum > 0.f ? (__builtin_amdgcn_logf(sum) - nm) * 0.6931471805599453f : -INFINITY;
+    (p.lse + first_row)[row_from(row0 + col)] = saw_keys(sum) ? (__builtin_amdgcn_logf(sum) - nm) * 0.6931471805599453f : -INFINITY;
   wave_lds_fence();
   uint16_t *const out = p.out + first_row * D;
 #pragma unroll
@@ -1133,7 +1141,7 @@ __global__ __launch_bounds__(kMergeThreads) void chunk_merge_kernel(const ChunkA
     }
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
-      if (s0 + s >= shares || !(ml[s].y > 0.f)) continue;  // (a share without a key that the row sees)
+      if (s0 + s >= shares || !saw_keys(ml[s].y)) continue;  // (a share without a key that the row sees)
       const float next = fmaxf(top, ml[s].x), f = fast_exp2(top - next), w = fast_exp2(ml[s].x - next);
       top = next;
       sum = sum * f + ml[s].y * w;
@@ -1171,7 +1179,7 @@ __global__ __launch_bounds__(kMergeThreads) void forms_merge_few_kernel(const Ch
   float top = -INFINITY, sum = 0.f, o[8] = {};
 #pragma unroll
   for (int s = 0; s < 4; ++s) {
-    if (s >= shares || !(ml[s].y > 0.f)) continue;  // (a share without a key that the row sees)
+    if (s >= shares || !saw_keys(ml[s].y)) continue;  // (a share without a key that the row sees)
     const float next = fmaxf(top, ml[s].x), f = fast_exp2(top - next), w = fast_exp2(ml[s].x - next);
     top = next;
     sum = sum * f + ml[s].y * w;
@@ -1216,12 +1224,12 @@ __global__ __launch_bounds__(kMergeThreads) void forms_merge_kernel(const ChunkA
   float top = -INFINITY, sum = 0.f, o[8] = {};
 #pragma unroll
   for (int s = 0; s < EACH; ++s)
-    if (PARTS * s + part < shares && ml[s].y > 0.f) top = fmaxf(top, ml[s].x);  // (else a share without a key that the row sees)
+    if (PARTS * s + part < shares && saw_keys(ml[s].y)) top = fmaxf(top, ml[s].x);  // (else a share without a key that the row sees)
 #pragma unroll
   for (int d = LPR; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
 #pragma unroll
   for (int s = 0; s < EACH; ++s) {
-    if (PARTS * s + part >= shares || !(ml[s].y > 0.f)) continue;
+    if (PARTS * s + part >= shares || !saw_keys(ml[s].y)) continue;
     const float w = fast_exp2(ml[s].x - top);
     sum += ml[s].y * w;
 #pragma unroll

@@ -48,6 +48,18 @@ struct ChunkRows {
   int all_lo[ROWS / kSbChunk], all_hi[ROWS / kSbChunk], any_lo[ROWS / kSbChunk], any_hi[ROWS / kSbChunk];
 };
 
+// What a row adds to its logits: minus its lse, in log2 units.  A row that has seen a NaN, whose lse is one, gives NaN to all slots that it sees and nothing to the
+// others: hidden logits are -inf, which a NaN added to them would not leave, so it adds what takes every other weight to infinity (v_min_f32 of a NaN and a number is
+// the number), and a sum that is infinite, of weights of 1 at most, is NaN.  (A row without a key it sees, whose lse is -inf, adds the same to nothing but -inf.)
+constexpr float kNanRow = 3e38f;
+__device__ __forceinline__ float row_addend(float lse) { return fminf(lse * -1.4426950408889634f, kNanRow); }
+// (by its bits, and the number out of the compiler's sight: to it floats are never NaN)
+__device__ __forceinline__ float received(float sum) {
+  uint32_t nan = 0x7fc00000u;
+  asm("" : "+v"(nan));
+  return __uint_as_float(__float_as_uint(sum) == 0x7f800000u ? nan : __float_as_uint(sum));
+}
+
 // One row of a unit a thread: fetched, then put among the others' (32 neighbouring threads have a chunk).
 template <bool SHAPED>
 struct ChunkRow {
@@ -72,8 +84,7 @@ __device__ __forceinline__ void chunk_put_row(ChunkRows<SHAPED, BIASED, ROWS> &r
                                               int base, int at) {
   const bool real = row.r < R;
   const int r = real ? row.r : R - 1, i = chunk_token(r, p.g_magic);
-  // (a row without a key it sees has no weights: its comparisons say so.  Rows behind the last see nothing)
-  rows.minus_l[at] = row.l == -INFINITY ? 0.f : row.l * -1.4426950408889634f;
+  rows.minus_l[at] = row_addend(row.l);  // (rows behind the last see nothing)
   if (SHAPED) {
     int lo;
     uint32_t span;
@@ -276,7 +287,7 @@ __device__ __forceinline__ void chunk_scores(const ChunkScoreParams &p) {
   float tot[kSbTiles];
 #pragma unroll
   for (int kt = 0; kt < kSbTiles; ++kt) tot[kt] = sum[kt] + __shfl_xor(sum[kt], 32);
-  const float v = hf == 0 ? tot[0] : tot[1];
+  const float v = received(hf == 0 ? tot[0] : tot[1]);
   const int slot = key0 + 32 * hf + col;
   if (slot < n && slot >= skip) {
     float *d = p.dst + (size_t)unit * c.cap + slot;
@@ -378,6 +389,7 @@ __device__ __forceinline__ void chunk_scores_few(const ChunkScoreParams &p) {
     float v = 0.f;
 #pragma unroll
     for (int w = 0; w < kCfWaves; ++w) v += sm_sum[w][lane];
+    v = received(v);
     float *d = p.dst + (size_t)unit * c.cap + slot;
     *d = p.accumulate ? *d + v : v;
   }

@@ -319,8 +319,7 @@ __global__ __launch_bounds__(kTsWaves * 64) void coded_token_scores_kernel(const
   for (int e = 0; e < 4; ++e) {
     const int r = 4 * quad + e, at = r < R ? r : R - 1, i = chunk_token(at, p.g_magic);
     const size_t token = (size_t)b * p.T + i;
-    const float l = p.lse[token * c.Hq + (size_t)h * c.G + (at - i * c.G)];
-    minus_l[e] = l == -INFINITY ? 0.f : l * -1.4426950408889634f;
+    minus_l[e] = row_addend(p.lse[token * c.Hq + (size_t)h * c.G + (at - i * c.G)]);
     if (SHAPED) {
       own[e] = pos[base + i];
       chunk_interval(p.shape, token, own[e], lo[e], span[e]);
@@ -363,6 +362,7 @@ __global__ __launch_bounds__(kTsWaves * 64) void coded_token_scores_kernel(const
   const int slot = key0 + lane;
   if (slot < n && slot >= skip) {
     float *d = p.dst + (size_t)unit * c.cap + slot;
+    got = received(got);
     *d = p.accumulate ? *d + got : got;
   }
 }
