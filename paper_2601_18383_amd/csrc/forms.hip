@@ -232,6 +232,9 @@ int dynts_tree_keep(dynts_ctx *ctx, int32_t layer, int32_t n_tokens, const int32
   if (overlap(n_kept, each, leaf, each) || (n_taken && overlap(n_kept, each, n_taken, each))) return DYNTS_EINVAL;
   const size_t rows = (size_t)c.Nb * n_tokens * c.Hq;
   if ((q_kept && overlap(q_kept, rows * c.D * 2, q, rows * c.D * 2)) || (lse_kept && overlap(lse_kept, rows * 4, lse, rows * 4))) return DYNTS_EINVAL;
+  // (an update owed by a single step counts slots that move now, if the draft, or its end, was appended by such steps)
+  const int owed = dynts_update_scores(ctx, layer, stream);
+  if (owed != DYNTS_OK) return owed;
   const dynts::TreeKeepParams p{c, seen, leaf, n_taken, n_kept, q, lse, q_kept, lse_kept, n_tokens, (n_tokens + 31) / 32};
   // (a gathering workgroup for eight kept tokens, four at most)
   const unsigned gather = q_kept || lse_kept ? (n_tokens > 24 ? 4 : (n_tokens + 7) / 8) : 0;
