@@ -813,6 +813,10 @@ def main():
                     help="also run three plain 1 GiB device copies (a kernel of known traffic, for scaling "
                          "rocprofv3's FETCH_SIZE / WRITE_SIZE counters)")
     args = ap.parse_args()
+    if args.codes and (not (args.chunk or args.draft) or args.predictor or args.score_block):
+        ap.error("--codes is for --chunk and --draft: the other runs know caches of bf16 alone")
+    if args.chunk and args.draft:
+        ap.error("--chunk and --draft are two runs")
     if args.launch_shape:
         args.launch_shape = tuple(int(x) for x in args.launch_shape.split(","))
     if args.gpus != 1:
