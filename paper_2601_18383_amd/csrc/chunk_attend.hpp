@@ -1024,9 +1024,11 @@ __device__ __forceinline__ void chunk_attend_few(const ChunkAttendParams &p) {
         if (TREE) {
           s[e] = sees >> (8 * (e >> 2) + (e & 3)) & 1u ? s[e] * p.scale_log2 : -INFINITY;
         } else if (SHAPED) {
-          float x = capped ? s[e] : s[e] * p.scale_log2;
+          // (which of the two products is rounded, the logit's or the bias's, is fixed here: the compiler's choice would change with the code around it, and results with
+          // that by a step of the logit)
           const int kp = sm_pos[wave][key];
-          x -= slope * fabsf((float)(own - kp));
+          const float d = fabsf((float)(own - kp)), by = capped ? 1.f : p.scale_log2;
+          const float x = CODE || e == 0 ? fmaf(s[e], by, -(slope * d)) : fmaf(-slope, d, s[e] * by);
           s[e] = (uint32_t)(kp - lo) <= span ? x : -INFINITY;
         } else {
           s[e] = t + key <= lim ? s[e] * p.scale_log2 : -INFINITY;
