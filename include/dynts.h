@@ -328,7 +328,10 @@ int dynts_predict_scores(const dynts_predictor *w, const uint16_t *h, int32_t ba
  *     stream-ordered with respect to each other).
  * Arrays that are written overlap no other argument.  Outputs are bf16, as what a projection reads next, and the weights are rounded to bf16 for their
  * product with V, half a step of 2^-8 each (a single step keeps 16 bits of a weight and returns fp32); sums, products, statistics and the weights that
- * slots receive are fp32. */
+ * slots receive are fp32.
+ * A token's weights of rows that it does not see are 0, and 0 times a NaN or an infinity is NaN: rows of V that are hidden from a token, those of the chunk's
+ * later tokens among them, have to be finite, or elements of its output are NaN where theirs are not.  (On codes one element of 2^126 and more makes 32 such.)
+ * Rows of K need not: hidden logits are -inf whatever they were. */
 
 /* What is done to the logits of a chunk, in this order (s the scaled product of a query at position p and a key at
  * position j; positions are those of the `pos` array, not slots: evictions leave gaps in them):
@@ -338,8 +341,7 @@ int dynts_predict_scores(const dynts_predictor *w, const uint16_t *h, int32_t ba
  *   hidden keys      s = -inf unless max(first[b][i], p - window + 1) <= j <= last[b][i]
  * first, last: positions token i of the chunk sees from and up to (`last` may lie behind the token's own position: a
  * prefix whose tokens see each other; `first` at the start of a document keeps documents apart).  Positions are taken to
- * be 0 or more and below 2^31 - 1.  A token that sees nothing gets zeros and lse = -inf.  Rows of V that are hidden from a token have
- * to be finite; rows of K need not.
+ * be 0 or more and below 2^31 - 1.  A token that sees nothing gets zeros and lse = -inf.
  * n_tokens = 1 is the form for single tokens, and the only one: dynts_decode_step, dynts_decode_loop and dynts_score_block know no shaping.  A model that
  * has one pays a score launch a token, and has no runs of steps and no logits kept for a trigger. */
 typedef struct dynts_shaping {
@@ -404,7 +406,8 @@ int dynts_chunk_step(dynts_ctx *ctx, int32_t layer, const uint16_t *q, const uin
  * [L][Nb][Hkv][cap][d / 32], or pools [n_pages][64][d] with scales [n_pages][64][d / 32]; everything else as there.
  * 16-byte aligned; pools zero-filled before first use.  Chunks (dynts_chunk_append, _attend, _scores, _step; n_tokens = 1 is the form for single tokens, question = 1 fills a prompt), drafts
  * (dynts_tree_*), dynts_read_rows, dynts_select_evict, dynts_compact and dynts_update_scores (which has nothing to do) serve it; the new tokens of a
- * chunk see each other's rows as the cache holds them.  The other calls on rows return DYNTS_ECODES: dynts_prefill, dynts_append, dynts_decode_attend,
+ * chunk see each other's rows as the cache holds them.  Roundings are those of chunks, one token or many: outputs in bf16 and weights rounded to bf16, where
+ * dynts_decode_step on a bf16 cache has fp32 and 16 bits.  The other calls on rows return DYNTS_ECODES: dynts_prefill, dynts_append, dynts_decode_attend,
  * dynts_decode_attend_update, dynts_decode_step, dynts_decode_step_static, dynts_hint_trigger, dynts_score_block, dynts_decode_loop. */
 #define DYNTS_CODE_E4M3 1
 #define DYNTS_CODE_INT8 2

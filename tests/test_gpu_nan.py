@@ -137,3 +137,38 @@ def test_whole_steps(B, kind, Hq, Hkv, d, n_old, n_new):
         _check(x.lse[b, :m], r["lse"], r["lse_tol"], rows, "lse[%d]" % b)
         _check(x.c.S[0, b, :, :a + m], r["recv"], r["recv_tol"], slots, "received[%d]" % b)
     assert int(x.c.status.item()) == 0
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("Hq,Hkv,d,n_old,n_new", SHAPES)
+def test_values(B, kind, Hq, Hkv, d, n_old, n_new):
+    """A NaN in a row of V: in that element (on codes its block) of the tokens that see the row, and in none of the others' elements, lse and weights.  (That element of
+    tokens that do not see the row, those before it in the same chunk, is not told: hidden rows of V have to be finite.)"""
+    x = Draft(B, kind, Hq, Hkv, d, n_old, n_new, seed=34, append=False)
+    x.k_new[x.k_new.isnan()] = 0.0
+    x.v_new[x.v_new.isnan()] = 0.0
+    places = [(b % Hkv, m // 2) if m else None for b, m in enumerate(n_new)]
+    elements = torch.zeros(d, dtype=torch.bool)
+    if _code(kind):
+        elements[32:64] = True
+    else:
+        elements[37] = True
+    for b, place in enumerate(places):
+        if place:
+            h, at = place
+            x.v_new[b, at, h, 37] = math.nan
+            x.V[b, h, n_old[b] + at, elements] = 0  # (of what it is compared with, these elements are left out)
+    B.dynts_chunk_step(x.c.ctx, 0, x.q.to(DEV), x.k_new, x.v_new, x.out, x.scratch, lse=x.lse, n_new=x.n)
+    G = Hq // Hkv
+    for b, (a, m) in enumerate(zip(n_old, n_new)):
+        r, rows, slots = _attend(x, b, None)
+        _check(x.lse[b, :m], r["lse"], r["lse_tol"], rows, "lse[%d]" % b)
+        _check(x.c.S[0, b, :, :a + m], r["recv"], r["recv_tol"], slots, "received[%d]" % b)
+        rest = torch.ones((m, Hq, d), dtype=torch.bool)
+        if places[b]:
+            h, at = places[b]
+            heads = slice(h * G, (h + 1) * G)
+            assert torch.all(x.out[b, at:m, heads][:, :, elements.to(DEV)].isnan())
+            rest[:, heads] = ~elements
+        plain.check(x.out[b, :m].double().cpu()[rest], r["out"][rest], r["out_tol"][rest], "out[%d]" % b)
+    assert int(x.c.status.item()) == 0
