@@ -1117,7 +1117,8 @@ __global__ __launch_bounds__(kFewThreads, D == 64 && MASK != kShaped ? 4 : 2) vo
   chunk_attend_few<D, MASK, CODE>(p);
 }
 
-// The shares of a row together.  grid (ceil(T * G / kMergeRows), units), D / 8 threads a row.
+// The shares of a row together.  grid (ceil(T * G / kMergeRows), units), D / 8 threads a row.  Sums are looked at by their bits, as in saw_keys; loaded as such, they cost
+// the test nothing more.
 constexpr int kMergeThreads = 256;
 template <int D>
 __global__ __launch_bounds__(kMergeThreads) void chunk_merge_kernel(const ChunkAttendParams p, int block_rows) {
@@ -1132,21 +1133,21 @@ __global__ __launch_bounds__(kMergeThreads) void chunk_merge_kernel(const ChunkA
   const size_t first = (size_t)unit * p.n_split * p.Rpad + r;
   float top = -INFINITY, sum = 0.f, o[8] = {};
   for (int s0 = 0; s0 < shares; s0 += 4) {  // four shares' loads at a time
-    float2 ml[4];
+    uint2 ml[4];
     f32x4 a[4], z[4];
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
       const size_t prow = first + (size_t)(s0 + s < shares ? s0 + s : s0) * p.Rpad;
-      ml[s] = *reinterpret_cast<const float2 *>(p.part_ml + 2 * prow);
+      ml[s] = *reinterpret_cast<const uint2 *>(p.part_ml + 2 * prow);
       a[s] = *reinterpret_cast<const f32x4 *>(p.part_o + prow * D + d0);
       z[s] = *reinterpret_cast<const f32x4 *>(p.part_o + prow * D + d0 + 4);
     }
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
-      if (s0 + s >= shares || !saw_keys(ml[s].y)) continue;  // (a share without a key that the row sees)
-      const float next = fmaxf(top, ml[s].x), f = fast_exp2(top - next), w = fast_exp2(ml[s].x - next);
+      if (s0 + s >= shares || !ml[s].y) continue;  // (a share without a key that the row sees)
+      const float next = fmaxf(top, __uint_as_float(ml[s].x)), f = fast_exp2(top - next), w = fast_exp2(__uint_as_float(ml[s].x) - next);
       top = next;
-      sum = sum * f + ml[s].y * w;
+      sum = sum * f + __uint_as_float(ml[s].y) * w;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         o[j] = o[j] * f + a[s][j] * w;
@@ -1165,12 +1166,12 @@ __global__ __launch_bounds__(kMergeThreads) void forms_merge_few_kernel(const Ch
   const int unit = blockIdx.y, b = unit / c.Hkv, h = unit - b * c.Hkv;
   const int r = blockIdx.x * (kMergeThreads / (D / 8)) + threadIdx.x / (D / 8), d0 = 8 * (threadIdx.x % (D / 8));
   if (r >= p.T * c.G) return;
-  float2 ml[4];
+  uint2 ml[4];
   f32x4 a[4], z[4];
 #pragma unroll
   for (int s = 0; s < 4; ++s) {
     const size_t prow = ((size_t)unit * p.n_split + (s < p.n_split ? s : 0)) * p.Rpad + r;
-    ml[s] = *reinterpret_cast<const float2 *>(p.part_ml + 2 * prow);
+    ml[s] = *reinterpret_cast<const uint2 *>(p.part_ml + 2 * prow);
     a[s] = *reinterpret_cast<const f32x4 *>(p.part_o + prow * D + d0);
     z[s] = *reinterpret_cast<const f32x4 *>(p.part_o + prow * D + d0 + 4);
   }
@@ -1181,10 +1182,10 @@ __global__ __launch_bounds__(kMergeThreads) void forms_merge_few_kernel(const Ch
   float top = -INFINITY, sum = 0.f, o[8] = {};
 #pragma unroll
   for (int s = 0; s < 4; ++s) {
-    if (s >= shares || !saw_keys(ml[s].y)) continue;  // (a share without a key that the row sees)
-    const float next = fmaxf(top, ml[s].x), f = fast_exp2(top - next), w = fast_exp2(ml[s].x - next);
+    if (s >= shares || !ml[s].y) continue;  // (a share without a key that the row sees)
+    const float next = fmaxf(top, __uint_as_float(ml[s].x)), f = fast_exp2(top - next), w = fast_exp2(__uint_as_float(ml[s].x) - next);
     top = next;
-    sum = sum * f + ml[s].y * w;
+    sum = sum * f + __uint_as_float(ml[s].y) * w;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       o[j] = o[j] * f + a[s][j] * w;
@@ -1207,15 +1208,15 @@ __global__ __launch_bounds__(kMergeThreads) void forms_merge_kernel(const ChunkA
   const int r = blockIdx.x * (kMergeThreads / 64) + threadIdx.x / 64, part = lane / LPR, d0 = 8 * (lane % LPR);
   if (r >= p.T * c.G) return;
   const size_t first = (size_t)unit * p.n_split * p.Rpad + r;
-  float2 ml[EACH];
+  uint2 ml[EACH];
   f32x4 a[EACH], z[EACH];
 #pragma unroll
   for (int s = 0; s < EACH; ++s) {
     const int share = PARTS * s + part;
-    ml[s] = float2{0.f, 0.f};
+    ml[s] = uint2{0u, 0u};
     if (share >= p.n_split) continue;
     const size_t prow = first + (size_t)share * p.Rpad;
-    ml[s] = *reinterpret_cast<const float2 *>(p.part_ml + 2 * prow);
+    ml[s] = *reinterpret_cast<const uint2 *>(p.part_ml + 2 * prow);
     a[s] = *reinterpret_cast<const f32x4 *>(p.part_o + prow * D + d0);
     z[s] = *reinterpret_cast<const f32x4 *>(p.part_o + prow * D + d0 + 4);
   }
@@ -1226,14 +1227,14 @@ __global__ __launch_bounds__(kMergeThreads) void forms_merge_kernel(const ChunkA
   float top = -INFINITY, sum = 0.f, o[8] = {};
 #pragma unroll
   for (int s = 0; s < EACH; ++s)
-    if (PARTS * s + part < shares && saw_keys(ml[s].y)) top = fmaxf(top, ml[s].x);  // (else a share without a key that the row sees)
+    if (PARTS * s + part < shares && ml[s].y) top = fmaxf(top, __uint_as_float(ml[s].x));  // (else a share without a key that the row sees)
 #pragma unroll
   for (int d = LPR; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
 #pragma unroll
   for (int s = 0; s < EACH; ++s) {
-    if (PARTS * s + part >= shares || !saw_keys(ml[s].y)) continue;
-    const float w = fast_exp2(ml[s].x - top);
-    sum += ml[s].y * w;
+    if (PARTS * s + part >= shares || !ml[s].y) continue;
+    const float w = fast_exp2(__uint_as_float(ml[s].x) - top);
+    sum += __uint_as_float(ml[s].y) * w;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       o[j] += a[s][j] * w;
