@@ -456,9 +456,9 @@ int dynts_tree_step(dynts_ctx *ctx, int32_t layer, const uint16_t *q, const uint
                     const float *s_new, int32_t n_tokens, const int32_t *n_new, const uint32_t *seen, int32_t *n_taken,
                     uint16_t *out, float *lse, void *scratch, size_t scratch_bytes, void *stream);
 
-/* Of the last n_taken[b] (NULL: n_tokens) tokens in the cache those stay that token leaf[b] sees, in order, right behind what lay before the draft;
- * leaf[b] = -1: none.  Applies an outstanding score accumulation first.  Scores move with them, positions are those of a chunk, both lengths and the pages follow; rows behind the new length
- * keep what they held.  n_kept int32 [Nb] receives the number that stays.  q_kept and lse_kept (NULL, or of the shapes of q and
+/* Of the last n_taken[b] (NULL: n_tokens; no more than the sequence has) tokens in the cache those stay that token leaf[b] sees, in order, right
+ * behind what lay before the draft; leaf[b] = -1: none.  Applies an outstanding score accumulation first.  Scores move with the rows, positions are those of a
+ * chunk, both lengths and the pages follow; rows behind the new length keep what they held.  n_kept int32 [Nb] receives the number that stays.  q_kept and lse_kept (NULL, or of the shapes of q and
  * lse, those of dynts_tree_step) receive the rows of q and lse of the tokens that stay, one after the other; rows behind them are left
  * alone: dynts_chunk_scores takes them with n_new = n_kept.  A leaf that is not one of the n_taken[b] tokens keeps none and latches bit 4
  * (value 16) in the status word. */

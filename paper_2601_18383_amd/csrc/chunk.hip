@@ -62,7 +62,8 @@ constexpr long long kMostPartials = 65536;
 //   many rows, W = 64, 4500 slots 1 / 4 / 8 / 16: 94.9 / 41.6 / 37.3 / 37.1, 1000 1 / 2: 24.8 / 28.1; W = 128 of 1000 1 / 2 / 4: 25.4 / 30.5 / 31.4; W = 256 of 4500
 //     1 / 2 / 4: 97.8 / 84.7 / 84.4, of 1000 25.6 / 33.2 / 33.2; W = 16 of 16000 8 / 16 / 31: 50.9 / 35.4 / 36.4
 //
-// Caches of codes by the same rule.  us, few / many (e4m3; whole numbers up to a fourth more):
+// Caches of codes by the same rule, which is wrong for 64 rows of very many units on long caches alone (512 units, below).  us, few / many (e4m3; whole numbers up to a
+// fourth more):
 //   head_dim 128, 8 units: 4500 slots R = 512 27.2 / 28.3, R = 1024 38.1 / 36.8; 16000 slots R = 128 25.9 / 28.8, R = 256 37.3 / 34.3; 32 units: 1500 slots R = 256 17.4 /
 //     24.1, R = 512 32.8 / 30.3, 4500 R = 256 36.2 / 35.2, 16000 R = 64 39.8 / 50.6, R = 128 66.4 / 56.0; 128 units: 500 slots R = 64 10.9 / 16.2, R = 128 19.9 / 17.1, 4500
 //     R = 64 42.5 / 54.2, R = 128 77.6 / 60.4; 512 units: 500 slots R = 64 37.1 / 26.8, 1500 70.5 / 69.4, 4500 163 / 185
@@ -86,7 +87,8 @@ ChunkPlan chunk_plan(const dynts_config &c, int n_tokens, int slots, bool far_ca
   // Codes become bf16 in every row block anew; shaped, or of more blocks than this, they are unpacked before.  us by the blocks of a unit, unpacked / not: e4m3, head_dim 128,
   // 128 units of 2500 slots 8 / 12 / 16 / 24: 217 291 374 554 / 186 273 361 556, 8 units of 16000 8 / 24 / 64: 98 238 523 / 80 243 578; whole numbers 128 units 8 / 12 / 16: 217
   // 293 376 / 201 295 396; head_dim 64, 32 units of 2500 8 / 12: 43.5 55.9 / 36.3 62.2, 128 of 1000 8 / 12 / 24: 54.9 77.4 140 / 49.5 75.4 143, whole numbers 55 79 141 / 55
-  // 79 158.
+  // 79 158.  Shaped, of two evils: the kernel of many rows with a shaping has no form for codes, and the layer is unpacked whole, also slots that a window hides from all
+  // rows.  512 tokens, window 1024, 4 heads a group of 128, bf16 cache / codes: 8 units of 1536 slots 35.2 / 40.3, of 16384 34.3 / 48.6; 32 units 45.2 / 55.1, 44.6 / 118.5.
   const int most_blocks = c.head_dim == 128 ? (code == DYNTS_CODE_E4M3 ? 20 : 10) : code == DYNTS_CODE_E4M3 ? 10 : 8;
   pl.unpack = code && !pl.few && (shaped || W > units * most_blocks);
   pl.groups = !pl.few && W <= 256 && (tree || (code && !pl.unpack));

@@ -1159,7 +1159,8 @@ __global__ __launch_bounds__(kMergeThreads) void chunk_merge_kernel(const ChunkA
   chunk_write<D>(p, ((size_t)b * p.T + i) * c.Hq + (size_t)h * c.G + (r - i * c.G), d0, o, top, sum);
 }
 
-// The same for up to four shares of drafts and of caches of codes: all are asked for at once, before it is known how many there are.
+// The same for up to four shares of drafts and of caches of codes: all are asked for at once, before it is known how many there are.  (Chunks on bf16 caches
+// keep the one above for any number of shares: the next one, for more than four, adds in another order, and would change their last bits.)
 template <int D>
 __global__ __launch_bounds__(kMergeThreads) void forms_merge_few_kernel(const ChunkAttendParams p, int block_rows) {
   const ChunkCache &c = p.c;

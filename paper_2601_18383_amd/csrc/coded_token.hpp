@@ -60,7 +60,7 @@ struct TokenLds {
 // barrier before the end, where the waves' outputs are joined.  Two workgroups a compute unit, but one where shaped rows of 128 need the registers (158; with 128 and spills
 // 512 slots of 128 units 12.4 us instead of 9.5, 16000 140 instead of 99).
 // us with eight waves / sixteen / chunk_attend_few's 32 rows (e4m3, head_dim 128): 8 units of 16000 slots 15.9 / 16.9 / 17.3, 128 of 500 7.8 / 9.4 / 9.2, of 2464 19.8 /
-// 20.3 / 22.2, 512 of 500 14.5 / 18.9 / - , of 2464 60 / 63 / 68: 346 MB, 5.8 TB/s (a large copy reaches 5.1, these caches lie in the memory-side cache in part).
+// 20.3 / 22.2, 512 of 500 14.5 / 18.9 / - , of 2464 60 / 63 / 68: 333 MB, 5.5 TB/s (a large copy reaches 5.1, these caches lie in the memory-side cache in part).
 template <int D, int MASK, int CODE, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, MASK == kShaped && D == 128 ? 2 : 4) void coded_token_kernel(const ChunkAttendParams p) {
   using Lds = TokenLds<D>;

@@ -1,7 +1,7 @@
 // Caches of 8-bit codes.  A block of 32 neighbouring elements of a row shares a scale, a power of two:
 //   value = code * 2^(s - 127),   s the block's scale byte, the least (27 at least) with   max |x| <= top * 2^(s - 127),
-// top 448 for e4m3 (a float of 4 bits of exponent and 3 of mantissa), 127 for whole numbers; codes are rounded to nearest, ties to even: off by half a step of
-// 2^-4 of the value (e4m3), by half of 2^(s - 127) (whole numbers).  A block that holds an infinity, a NaN or 2^126 and more has s = 255, and reads as NaN.
+// top 448 for e4m3 (a float of 4 bits of exponent and 3 of mantissa), 127 for whole numbers; codes are rounded to nearest, ties to even: off by
+// 2^-4 of the value at most, small ones by 2^-10 of 2^(s - 127) (e4m3), or by half of 2^(s - 127) (whole numbers).  A block that holds an infinity, a NaN or 2^126 and more has s = 255, and reads as NaN.
 //
 // A code has at most eight significant bits and the scale none: every value is exact in bf16, so the kernels that read a cache
 // of codes are those of bf16 caches with the codes turned into bf16 on the way, and nothing about their arithmetic changes.
